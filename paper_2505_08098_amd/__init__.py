@@ -10,3 +10,5 @@ holds the seeded synthetic inputs.
 from .binding import (F3SError, Plan, PlanInfo, backward, forward,  # noqa: F401
                       forward_typed, load_library, probe_gather, probe_rows, probe_stream,
                       run, run_raw, run_trace, status_string, wall_clock_khz)
+from .dense import (Cache, CrossPlan, cache_attend, cache_read, cache_write,  # noqa: F401
+                    cross_backward, cross_forward)

@@ -1,0 +1,177 @@
+// f3s_cache_attend: checks, the division of the work, workspace.
+#include <math.h>
+
+#include "attend.h"
+
+namespace f3s {
+f3s_status_t check_cache(const f3s_cache_t *c);
+}
+
+namespace {
+
+using f3s::AttendArgs;
+
+// Workgroups that a pass over the keys aims at: 256 compute units with four
+// workgroups of four waves each.
+constexpr int64_t kWorkgroups = 1024;
+
+constexpr size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+struct Layout {
+    int64_t own_rows, prefix_rows;   // partial rows
+    size_t ml, desc, bytes;          // byte offsets behind part_o, and the sum
+};
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Everything of the arguments that follows from the sizes; false if a size is
+// beyond what the kernels count with.
+bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_new,
+            int32_t n_heads, int32_t prefix_len, AttendArgs *a, Layout *w)
+{
+    const int64_t g = n_heads / c.n_kv_heads;
+    const int64_t rows = n_new * g, all = rows * n_seqs;
+    const int64_t cap = (int64_t)max_pages * c.page_size;
+    if (all * c.n_kv_heads > 0x7FFFFFFF || cap > 0x7FFFFFFF ||
+        (double)cap / f3s::kUnit * n_seqs + n_seqs > 1e9)
+        return false;
+    a->n_seqs = n_seqs;
+    a->n_new = n_new;
+    a->max_pages = max_pages;
+    a->prefix_len = prefix_len;
+    a->rows = (int32_t)rows;
+    a->row_blocks = (int32_t)ceil_div(rows, f3s::kFewRows);
+    const int64_t cap_units = ceil_div(cap, f3s::kUnit);
+    a->direct = prefix_len == 0 && cap_units <= f3s::kLeastUnits;
+    int64_t share = ceil_div(kWorkgroups, (int64_t)c.n_kv_heads * a->row_blocks);
+    // (no more than the table has places for)
+    const int64_t most = ceil_div(cap_units * n_seqs, f3s::kLeastUnits);
+    if (share > most) share = most;
+    if (share < 1) share = 1;
+    a->share = (int32_t)share;
+    a->own_items = a->direct || cap_units <= f3s::kLeastUnits ? n_seqs
+                                                              : (int32_t)(share + n_seqs);
+    a->prefix_blocks = (int32_t)ceil_div(all, f3s::kFewRows);
+    a->prefix_splits = a->prefix_chunk = 0;
+    if (prefix_len) {
+        const int64_t units = ceil_div(prefix_len, f3s::kUnit);
+        const int64_t want = ceil_div(kWorkgroups, (int64_t)c.n_kv_heads * a->prefix_blocks);
+        const int64_t per = f3s::units_per_item(units, (int32_t)want);
+        a->prefix_chunk = (int32_t)(per * f3s::kUnit);
+        a->prefix_splits = (int32_t)ceil_div(units, per);
+    }
+    const int64_t items = (int64_t)a->own_items * c.n_kv_heads;
+    w->own_rows = a->direct ? 0 : items * rows;
+    w->prefix_rows = (int64_t)a->prefix_splits * c.n_kv_heads * all;
+    a->prefix_part = w->own_rows;
+    const int64_t n = w->own_rows + w->prefix_rows;
+    if (items * a->row_blocks +
+            (int64_t)a->prefix_splits * c.n_kv_heads * a->prefix_blocks > 0x7FFFFFFF)
+        return false;
+    w->ml = round256((size_t)n * c.d * 4);
+    w->desc = w->ml + round256((size_t)n * 8);
+    w->bytes = a->direct ? 0 : w->desc + round256((size_t)n_seqs * 8);
+    return true;
+}
+
+bool sizes_ok(const f3s_cache_t *c, int32_t max_pages, int32_t n_seqs, int32_t n_new,
+              int32_t n_heads, int32_t prefix_len)
+{
+    return c && c->n_kv_heads >= 1 && c->page_size >= 1 && c->d >= 1 && max_pages >= 0 &&
+           n_seqs >= 0 && n_new >= 0 && n_heads >= 1 && n_heads % c->n_kv_heads == 0 &&
+           prefix_len >= 0;
+}
+
+bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+bool overlaps(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return na && nb && x < y + nb && y < x + na;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t f3s_cache_attend_workspace_bytes(const f3s_cache_t *cache, int32_t max_pages,
+                                        int32_t n_seqs, int32_t n_new, int32_t n_heads,
+                                        int32_t prefix_len)
+{
+    AttendArgs a = {};
+    Layout w;
+    if (!sizes_ok(cache, max_pages, n_seqs, n_new, n_heads, prefix_len) || n_seqs == 0 ||
+        n_new == 0 || !divide(*cache, max_pages, n_seqs, n_new, n_heads, prefix_len, &a, &w))
+        return 0;
+    return w.bytes;
+}
+
+f3s_status_t f3s_cache_attend(const f3s_cache_t *cache, const void *Q, f3s_dtype_t dtype,
+                              void *O, float *lse, const int32_t *table, int32_t max_pages,
+                              const int32_t *lens, int32_t n_seqs, int32_t n_new,
+                              int32_t n_heads, const int32_t *prefix, int32_t prefix_len,
+                              float scale, void *workspace, size_t workspace_bytes,
+                              hipStream_t stream)
+{
+    using f3s::set_status;
+    if (f3s_status_t st = f3s::check_cache(cache)) return set_status(st);
+    if (!sizes_ok(cache, max_pages, n_seqs, n_new, n_heads, prefix_len) || !isfinite(scale))
+        return set_status(F3S_ERR_INVALID_VALUE);
+    if (dtype != F3S_DTYPE_F16 && dtype != F3S_DTYPE_BF16)
+        return set_status(F3S_ERR_UNSUPPORTED);
+    if (n_seqs == 0 || n_new == 0) return F3S_OK;
+    if (!Q || !O || !lse || !lens || (max_pages && !table) || (prefix_len && !prefix) ||
+        !aligned(Q, 16) || !aligned(O, 16) || !aligned(lse, 4) || !aligned(lens, 4) ||
+        !aligned(table, 4) || !aligned(prefix, 4))
+        return set_status(F3S_ERR_INVALID_VALUE);
+    AttendArgs a = {};
+    Layout w;
+    if (!divide(*cache, max_pages, n_seqs, n_new, n_heads, prefix_len, &a, &w))
+        return set_status(F3S_ERR_TOO_LARGE);
+    if (w.bytes && (!workspace || !aligned(workspace, 256) || workspace_bytes < w.bytes))
+        return set_status(F3S_ERR_INVALID_VALUE);
+    const int64_t tokens = (int64_t)n_seqs * n_new;
+    const size_t qb = (size_t)tokens * n_heads * cache->d * 2, lb = (size_t)tokens * n_heads * 4;
+    const size_t cb = (size_t)cache->n_pages * cache->n_kv_heads * cache->page_size;
+    const struct {
+        const void *p;
+        size_t n;
+    } in[] = {{Q, qb},
+              {cache->k, cb * cache->d},
+              {cache->v, cb * cache->d},
+              {cache->k_exp, cb},
+              {cache->v_exp, cb},
+              {table, (size_t)n_seqs * max_pages * 4},
+              {lens, (size_t)n_seqs * 4},
+              {workspace, w.bytes}};
+    for (const auto &x : in)
+        if (overlaps(O, qb, x.p, x.n) || overlaps(lse, lb, x.p, x.n))
+            return set_status(F3S_ERR_INVALID_VALUE);
+    if (overlaps(O, qb, lse, lb)) return set_status(F3S_ERR_INVALID_VALUE);
+    a.table = table;
+    a.lens = lens;
+    a.prefix = prefix;
+    a.few.Q = Q;
+    a.few.O = O;
+    a.few.lse = lse;
+    a.few.q = {n_heads, n_heads / cache->n_kv_heads};
+    a.few.n_kv = cache->n_kv_heads;
+    a.few.sl2 = (float)(fabs((double)scale) * 1.4426950408889634);
+    a.few.flip = signbit(scale) ? 0x80008000u : 0u;
+    a.few.k = (const uint8_t *)cache->k;
+    a.few.v = (const uint8_t *)cache->v;
+    a.few.k_exp = cache->k_exp;
+    a.few.v_exp = cache->v_exp;
+    a.few.n_pages = cache->n_pages;
+    a.few.page_shift = __builtin_ctz(cache->page_size);
+    if (w.bytes) {
+        a.few.part_o = (float *)workspace;
+        a.few.part_ml = (float *)((char *)workspace + w.ml);
+        a.desc = (int2 *)((char *)workspace + w.desc);
+    }
+    return set_status(f3s::status_of(dtype == F3S_DTYPE_BF16
+                                         ? f3s::launch_attend_bf16(a, cache->d, stream)
+                                         : f3s::launch_attend_f16(a, cache->d, stream)));
+}
+
+}  // extern "C"

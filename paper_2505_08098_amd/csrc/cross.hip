@@ -1,0 +1,267 @@
+// f3s_cross_plan, f3s_cross_forward, f3s_cross_backward: the division of a
+// ragged batch among workgroups, checks, workspace.
+#include <math.h>
+#include <string.h>
+
+#include <new>
+#include <vector>
+
+#include "cross_few.h"
+
+namespace {
+
+using f3s::DenseItem;
+using f3s::DenseMerge;
+using f3s::set_status;
+
+// Workgroups of four waves that fill the GPU (256 compute units).
+constexpr int64_t kFewWorkgroups = 1024;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
+bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+bool overlaps(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return na && nb && x < y + nb && y < x + na;
+}
+
+// One side of a pass: the rows that get results, in ranges of one sequence,
+// each with the rows of the other side that it walks.
+struct Range {
+    int64_t row, rows, other, others;
+};
+
+// A pass divided into items of `tile` rows and, while that leaves fewer than
+// about `want` workgroups, of parts of the other side (at least `least` rows
+// of it, in multiples of `unit`).
+struct Division {
+    std::vector<DenseItem> items;
+    std::vector<DenseMerge> merges;
+    int64_t parts = 0;
+    int32_t merge_rows = 0;
+
+    void make(const std::vector<Range> &ranges, int32_t heads, int64_t tile, int64_t unit,
+              int64_t least, int64_t want)
+    {
+        int64_t total = 0;
+        for (const Range &r : ranges)
+            total += ceil_div(r.rows, tile) * ceil_div(r.others, unit) * heads;
+        int64_t per = ceil_div(total, want);  // units of an item
+        if (per < ceil_div(least, unit)) per = ceil_div(least, unit);
+        for (const Range &r : ranges) {
+            const int64_t units = ceil_div(r.others, unit);
+            const int64_t n = units <= per ? 1 : ceil_div(units, per);
+            for (int32_t h = 0; h < heads; ++h) {
+                for (int64_t at = 0; at < r.rows; at += tile) {
+                    const int32_t rows = (int32_t)(r.rows - at < tile ? r.rows - at : tile);
+                    const int32_t row = (int32_t)(r.row + at);
+                    if (n > 1) {
+                        merges.push_back({h, row, rows, (int32_t)parts, rows, (int32_t)n, {}});
+                        if (rows > merge_rows) merge_rows = rows;
+                    }
+                    for (int64_t k = 0; k < n; ++k) {
+                        const int64_t b = units * k / n * unit;
+                        int64_t e = units * (k + 1) / n * unit;
+                        if (e > r.others) e = r.others;
+                        items.push_back({h, row, rows, (int32_t)(r.other + b), (int32_t)(e - b),
+                                         n > 1 ? (int32_t)parts : -1, {}});
+                        if (n > 1) parts += rows;
+                    }
+                }
+            }
+        }
+    }
+    bool fits() const
+    {
+        return parts <= 0x7FFFFFFF && items.size() <= 0x7FFFFFFF &&
+               (int64_t)merges.size() * merge_rows <= 0x7FFFFFFF;
+    }
+};
+
+f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int32_t *q_len,
+                           const int32_t *k_len, int32_t n, int32_t n_heads, int32_t n_kv,
+                           int32_t d, f3s_status_t *st)
+{
+    *st = F3S_ERR_INVALID_VALUE;
+    if (!q_ptr || !k_ptr || n < 0 || n_kv < 1 || n_heads < 1 || n_heads % n_kv) return nullptr;
+    if (d < 32 || d > f3s::kMaxD || d % 32 != 0) {
+        *st = F3S_ERR_UNSUPPORTED;
+        return nullptr;
+    }
+    if (q_ptr[0] != 0 || k_ptr[0] != 0) return nullptr;
+    const int64_t g = n_heads / n_kv;
+    std::vector<Range> fwd;
+    int64_t longest = 0;
+    for (int32_t b = 0; b < n; ++b) {
+        if (q_ptr[b + 1] < q_ptr[b] || k_ptr[b + 1] < k_ptr[b]) return nullptr;
+        const int64_t q = q_ptr[b + 1] - (int64_t)q_ptr[b], k = k_ptr[b + 1] - (int64_t)k_ptr[b];
+        const int64_t ql = q_len ? q_len[b] : q, kl = k_len ? k_len[b] : k;
+        if (ql < 0 || ql > q || kl < 0 || kl > k) return nullptr;
+        // (rows that are padding walk nothing: their results are zeros)
+        if (ql) fwd.push_back({q_ptr[b] * g, ql * g, k_ptr[b], kl});
+        if (ql < q) fwd.push_back({(q_ptr[b] + ql) * g, (q - ql) * g, 0, 0});
+        if (ql * g > longest) longest = ql * g;
+    }
+    *st = F3S_ERR_TOO_LARGE;
+    if (q_ptr[n] * g > 0x7FFFFFFF || (double)q_ptr[n] * n_heads / 16 + n_heads > 2147483647.0)
+        return nullptr;
+    Division f;
+    f.make(fwd, n_kv, f3s::kFewRows, 64, 256, kFewWorkgroups);
+    if (!f.fits()) return nullptr;
+
+    f3s_cross_plan_s *p = new f3s_cross_plan_s;
+    p->n_heads = n_heads;
+    p->n_kv = n_kv;
+    p->g = (int32_t)g;
+    p->d = d;
+    p->q_rows = q_ptr[n];
+    p->k_rows = k_ptr[n];
+    p->n_fwd = (int32_t)f.items.size();
+    p->n_fwd_merge = (int32_t)f.merges.size();
+    p->fwd_merge_rows = f.merge_rows;
+    p->fwd_parts = f.parts;
+    const struct {
+        const void *src;
+        size_t bytes;
+        void **dst;
+    } lists[] = {
+        {f.items.data(), f.items.size() * sizeof(DenseItem), (void **)&p->fwd},
+        {f.merges.data(), f.merges.size() * sizeof(DenseMerge), (void **)&p->fwd_merge},
+    };
+    size_t bytes = 0;
+    for (const auto &l : lists) bytes += round256(l.bytes);
+    std::vector<char> host(bytes);
+    hipError_t e = hipGetDevice(&p->device);
+    if (e == hipSuccess && bytes) e = f3s::limited_malloc(&p->store, bytes);
+    if (e == hipSuccess && bytes) {
+        size_t at = 0;
+        for (const auto &l : lists) {
+            if (l.bytes) memcpy(host.data() + at, l.src, l.bytes);
+            *l.dst = (char *)p->store + at;
+            at += round256(l.bytes);
+        }
+        e = hipMemcpy(p->store, host.data(), bytes, hipMemcpyHostToDevice);
+    }
+    *st = f3s::status_of(e);
+    if (e != hipSuccess) {
+        f3s_cross_destroy(p);
+        return nullptr;
+    }
+    return p;
+}
+
+bool on_device(const f3s_cross_plan_s *p, hipStream_t stream)
+{
+    int dev = -1;
+    const hipError_t e = stream ? hipStreamGetDevice(stream, &dev) : hipGetDevice(&dev);
+    return e == hipSuccess && dev == p->device;
+}
+
+// Partial rows of d floats, then their records of `record` floats.
+size_t parts_bytes(int64_t rows, int32_t d, int32_t record)
+{
+    return rows ? round256((size_t)rows * d * 4) + round256((size_t)rows * record * 4) : 0;
+}
+
+bool workspace_ok(const void *w, size_t have, size_t need)
+{
+    return need == 0 || (w && aligned(w, 256) && have >= need);
+}
+
+}  // namespace
+
+extern "C" {
+
+f3s_cross_plan_t f3s_cross_plan(const int32_t *q_ptr, const int32_t *k_ptr,
+                                const int32_t *q_len, const int32_t *k_len, int32_t n_seqs,
+                                int32_t n_heads, int32_t n_kv_heads, int32_t d)
+{
+    f3s_status_t st;
+    f3s_cross_plan_t p = nullptr;
+    try {
+        p = make_plan(q_ptr, k_ptr, q_len, k_len, n_seqs, n_heads, n_kv_heads, d, &st);
+    } catch (...) {  // (std::bad_alloc, std::length_error)
+        st = F3S_ERR_OUT_OF_MEMORY;
+    }
+    set_status(st);
+    return p;
+}
+
+void f3s_cross_destroy(f3s_cross_plan_t p)
+{
+    if (!p) return;
+    if (p->store) (void)hipFree(p->store);
+    delete p;
+}
+
+size_t f3s_cross_forward_workspace_bytes(f3s_cross_plan_t p)
+{
+    return p ? parts_bytes(p->fwd_parts, p->d, 2) : 0;
+}
+
+f3s_status_t f3s_cross_forward(f3s_cross_plan_t p, const void *Q, const void *K,
+                               const void *V, f3s_dtype_t dtype, void *O, float *lse,
+                               float scale, void *workspace, size_t workspace_bytes,
+                               hipStream_t stream)
+{
+    if (!p || !isfinite(scale)) return set_status(F3S_ERR_INVALID_VALUE);
+    if (dtype != F3S_DTYPE_F16 && dtype != F3S_DTYPE_BF16)
+        return set_status(F3S_ERR_UNSUPPORTED);
+    if (p->q_rows == 0) return F3S_OK;
+    if (!on_device(p, stream)) return set_status(F3S_ERR_INVALID_VALUE);
+    if (!Q || !O || !lse || (p->k_rows && (!K || !V)) || !aligned(Q, 16) || !aligned(K, 16) ||
+        !aligned(V, 16) || !aligned(O, 16) || !aligned(lse, 4))
+        return set_status(F3S_ERR_INVALID_VALUE);
+    const size_t need = f3s_cross_forward_workspace_bytes(p);
+    if (!workspace_ok(workspace, workspace_bytes, need))
+        return set_status(F3S_ERR_INVALID_VALUE);
+    const size_t qb = (size_t)p->q_rows * p->n_heads * p->d * 2;
+    const size_t kb = (size_t)p->k_rows * p->n_kv * p->d * 2;
+    const size_t lb = (size_t)p->q_rows * p->n_heads * 4;
+    const struct {
+        const void *p;
+        size_t n;
+    } in[] = {{Q, qb}, {K, kb}, {V, kb}, {workspace, need}};
+    for (const auto &x : in)
+        if (overlaps(O, qb, x.p, x.n) || overlaps(lse, lb, x.p, x.n))
+            return set_status(F3S_ERR_INVALID_VALUE);
+    if (overlaps(O, qb, lse, lb)) return set_status(F3S_ERR_INVALID_VALUE);
+    f3s::FewArgs a = {};
+    a.Q = Q;
+    a.K = K;
+    a.V = V;
+    a.O = O;
+    a.lse = lse;
+    a.q = {p->n_heads, p->g};
+    a.n_kv = p->n_kv;
+    a.sl2 = (float)(fabs((double)scale) * 1.4426950408889634);
+    a.flip = signbit(scale) ? 0x80008000u : 0u;
+    a.part_o = (float *)workspace;
+    a.part_ml = (float *)((char *)workspace + round256((size_t)p->fwd_parts * p->d * 4));
+    const bool bf16 = dtype == F3S_DTYPE_BF16;
+    hipError_t e = bf16 ? f3s::launch_cross_few_bf16(*p, a, stream)
+                        : f3s::launch_cross_few_f16(*p, a, stream);
+    if (e == hipSuccess && p->n_fwd_merge) {
+        const f3s::CrossMergeArgs m = {p->fwd_merge, a.part_o, a.part_ml, O, lse, a.q, 0};
+        e = bf16 ? f3s::launch_cross_merge_bf16(*p, m, stream)
+                 : f3s::launch_cross_merge_f16(*p, m, stream);
+    }
+    return set_status(f3s::status_of(e));
+}
+
+size_t f3s_cross_backward_workspace_bytes(f3s_cross_plan_t p)
+{
+    return 0;
+}
+
+f3s_status_t f3s_cross_backward(f3s_cross_plan_t plan, const void *Q, const void *K,
+                                const void *V, f3s_dtype_t dtype, const void *O,
+                                const void *dO, const float *lse, void *dQ, void *dK,
+                                void *dV, float scale, void *workspace,
+                                size_t workspace_bytes, hipStream_t stream)
+{
+    return set_status(F3S_ERR_UNSUPPORTED);
+}
+
+}  // extern "C"

@@ -1,0 +1,21 @@
+// Cross attention of few query rows, bf16 (see few_rows.h).
+#include "cross_few.h"
+
+namespace f3s {
+
+hipError_t launch_cross_few_bf16(const f3s_cross_plan_s &p, const FewArgs &a, hipStream_t s)
+{
+#define F3S_CALL(D) launch_cross_few_d<D, kInBF16>(p, a, s)
+    F3S_FOR_D(p.d, F3S_CALL)
+#undef F3S_CALL
+}
+
+hipError_t launch_cross_merge_bf16(const f3s_cross_plan_s &p, const CrossMergeArgs &a,
+                                  hipStream_t s)
+{
+#define F3S_CALL(D) launch_cross_merge_d<D, kInBF16>(p, a, s)
+    F3S_FOR_D(p.d, F3S_CALL)
+#undef F3S_CALL
+}
+
+}  // namespace f3s

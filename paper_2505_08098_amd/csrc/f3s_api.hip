@@ -8,6 +8,7 @@
 #include <new>
 #include <vector>
 
+#include "dense_common.h"
 #include "f3s_internal.h"
 #include "f3s_probe.h"
 
@@ -37,6 +38,20 @@ size_t alloc_limit()
     const char *e = getenv("F3S_ALLOC_LIMIT_BYTES");
     return e && *e ? (size_t)strtoull(e, nullptr, 10) : ~(size_t)0;
 }
+
+// (for the library's other entry points)
+}  // namespace
+
+namespace f3s {
+f3s_status_t set_status(f3s_status_t s) { return s == F3S_OK ? s : fail(s); }
+f3s_status_t status_of(hipError_t e) { return from_hip(e); }
+hipError_t limited_malloc(void **p, size_t bytes)
+{
+    return bytes > alloc_limit() ? hipErrorOutOfMemory : hipMalloc(p, bytes);
+}
+}  // namespace f3s
+
+namespace {
 
 // One device allocation carved into 256-byte aligned pieces (the scratch of
 // one f3s_plan call, or a plan's arrays); sizing pass first (add), then one

@@ -1,0 +1,348 @@
+"""Dense attention beside the sparse operator: cross attention over a ragged
+batch, and attention over an 8-bit key/value cache (include/f3s_cross.h,
+include/f3s_cache.h).  Argument marshalling only, like ``binding``.
+
+    plan = f3s.CrossPlan(q_ptr, k_ptr, heads, kv_heads, d)     # once per batch
+    O, lse = f3s.cross_forward(plan, Q, K, V)
+    dQ, dK, dV = f3s.cross_backward(plan, Q, K, V, O, dO, lse)
+
+    cache = f3s.Cache.empty(n_pages, page_size, kv_heads, d)
+    f3s.cache_write(cache, K, V, table, lens)                  # the newest tokens
+    O, lse = f3s.cache_attend(cache, Q, table, lens, prefix=pages, prefix_len=n)
+"""
+import contextlib
+import ctypes
+import math
+
+import torch
+
+from .binding import (_DTYPE_CODE, F3S_OK, F3SError, _BuildOn, _check_device_tensor,
+                      load_library)
+from . import binding as _binding
+
+_LIB = None
+_vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+_HALF = (torch.float16, torch.bfloat16)
+
+
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_exp", _vp), ("v_exp", _vp), ("n_pages", _i32),
+                ("n_kv_heads", _i32), ("page_size", _i32), ("d", _i32)]
+
+
+def _lib():
+    global _LIB
+    if _LIB is None:
+        L = load_library()
+        cache = ctypes.POINTER(_CacheStruct)
+        for name, res, args in (
+                ("f3s_cross_plan", _vp, [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32]),
+                ("f3s_cross_destroy", None, [_vp]),
+                ("f3s_cross_forward_workspace_bytes", _sz, [_vp]),
+                ("f3s_cross_backward_workspace_bytes", _sz, [_vp]),
+                ("f3s_cross_forward", ctypes.c_int,
+                 [_vp] * 4 + [_i32, _vp, _vp, ctypes.c_float, _vp, _sz, _vp]),
+                ("f3s_cross_backward", ctypes.c_int,
+                 [_vp] * 4 + [_i32] + [_vp] * 6 + [ctypes.c_float, _vp, _sz, _vp]),
+                ("f3s_cache_write", ctypes.c_int,
+                 [cache, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _i32, _vp]),
+                ("f3s_cache_read", ctypes.c_int,
+                 [cache, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _i32, _vp]),
+                ("f3s_cache_attend", ctypes.c_int,
+                 [cache, _vp, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _vp, _i32,
+                  ctypes.c_float, _vp, _sz, _vp]),
+                ("f3s_cache_attend_workspace_bytes", _sz, [cache] + [_i32] * 5)):
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = res, args
+        _LIB = L
+    return _LIB
+
+
+@contextlib.contextmanager
+def _switch(device, stream):
+    with torch.cuda.device(device):
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            yield
+
+
+_NOTHING = contextlib.nullcontext()
+
+
+def _on(device, stream):
+    """The device and stream of a call made current, so that results and
+    workspaces are the stream's own memory (torch hands a stream's freed memory
+    to that stream's later work only)."""
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the operands on {device}")
+    if stream is None and torch.cuda.current_device() == device.index:
+        return _NOTHING
+    return _switch(device, stream)
+
+
+def _call(name, *args):
+    rc = getattr(_lib(), name)(*args)
+    if rc != F3S_OK:
+        raise F3SError(rc, name)
+
+
+def _check(t, name, dtype, device, shape):
+    _check_device_tensor(t, name, dtype, device)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
+def _dtype_of(t, name):
+    if not isinstance(t, torch.Tensor) or t.dtype not in _HALF:
+        raise TypeError(f"{name} must be a float16 or bfloat16 device tensor")
+    return t.dtype
+
+
+def _result(t, name, shape, dtype, device):
+    """The caller's tensor for a result, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _check(t, name, dtype, device, shape)
+    return t
+
+
+def _workspace(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _host_ints(x, name):
+    import numpy as np
+    a = np.asarray(x)
+    if a.ndim != 1 or (a.size and a.dtype.kind not in "iu"):
+        raise ValueError(f"{name} must be a host sequence of whole numbers")
+    if a.size and (a.min() < 0 or a.max() > 2**31 - 1):
+        raise ValueError(f"{name} must lie in [0, 2^31)")
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
+# ---- cross attention ----------------------------------------------------------
+
+class CrossPlan:
+    """f3s_cross_plan: the work of a ragged batch.  Sequence b has the rows
+    q_ptr[b] .. q_ptr[b+1] - 1 of Q and k_ptr[b] .. k_ptr[b+1] - 1 of K and V
+    (host sequences of ints, first 0); with q_len / k_len only the first of
+    them, the others being padding.  ``heads`` query heads share ``kv_heads``
+    key heads (default: as many), ``d`` values each."""
+
+    def __init__(self, q_ptr, k_ptr, heads, kv_heads=None, d=64, q_len=None, k_len=None,
+                 device="cuda"):
+        self._h = None
+        L = _lib()
+        q, k = _host_ints(q_ptr, "q_ptr"), _host_ints(k_ptr, "k_ptr")
+        if q.size < 1 or k.size != q.size:
+            raise ValueError("q_ptr and k_ptr must hold one entry more than sequences")
+        lens = [None if x is None else _host_ints(x, n)
+                for x, n in ((q_len, "q_len"), (k_len, "k_len"))]
+        if any(x is not None and x.size != q.size - 1 for x in lens):
+            raise ValueError("q_len and k_len must hold one entry per sequence")
+        device = torch.device(device)
+        if device.type != "cuda":
+            raise ValueError("the plan's device must be a GPU")
+        if device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        ptr = lambda a: None if a is None else a.ctypes.data_as(_vp)
+        kv_heads = heads if kv_heads is None else kv_heads
+        with _BuildOn(device):
+            h = L.f3s_cross_plan(ptr(q), ptr(k), ptr(lens[0]), ptr(lens[1]), q.size - 1,
+                                 int(heads), int(kv_heads), int(d))
+        if not h:
+            raise F3SError(L.f3s_last_error(), "f3s_cross_plan")
+        self._h = h
+        self.device = device
+        self.heads, self.kv_heads, self.d = int(heads), int(kv_heads), int(d)
+        self.q_shape = (int(q[-1]), self.heads, self.d)
+        self.k_shape = (int(k[-1]), self.kv_heads, self.d)
+        self._forward_bytes = L.f3s_cross_forward_workspace_bytes(h)
+        self._backward_bytes = L.f3s_cross_backward_workspace_bytes(h)
+
+    @property
+    def handle(self):
+        if self._h is None:
+            raise RuntimeError("plan was destroyed")
+        return self._h
+
+    def close(self):
+        if self._h is not None:
+            _lib().f3s_cross_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+
+def _cross_operands(plan, Q, K, V):
+    dtype = _dtype_of(Q, "Q")
+    _check(Q, "Q", dtype, plan.device, plan.q_shape)
+    _check(K, "K", dtype, plan.device, plan.k_shape)
+    _check(V, "V", dtype, plan.device, plan.k_shape)
+    return dtype
+
+
+def cross_forward(plan, Q, K, V, scale=None, out=None, lse=None, stream=None):
+    """f3s_cross_forward: O = softmax(scale Q K^T) V within each sequence of
+    the plan.  Q [rows, heads, d], K and V [rows, kv_heads, d], fp16 or bf16.
+    Returns (O, lse): O like Q, lse fp32 [rows, heads]."""
+    dtype = _cross_operands(plan, Q, K, V)
+    if scale is None:
+        scale = 1.0 / math.sqrt(plan.d)
+    with _on(plan.device, stream):
+        out = _result(out, "out", plan.q_shape, dtype, plan.device)
+        lse = _result(lse, "lse", plan.q_shape[:2], torch.float32, plan.device)
+        ws = _workspace(plan._forward_bytes, plan.device)
+        _call("f3s_cross_forward", plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+              _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(), float(scale), _ptr(ws),
+              plan._forward_bytes, _binding._raw_stream(plan.device.index))
+    return out, lse
+
+
+def cross_backward(plan, Q, K, V, O, dO, lse, scale=None, stream=None):
+    """f3s_cross_backward: (dQ, dK, dV), of the operands' shapes and type, for
+    dO = dL/dO and the forward's O and lse."""
+    dtype = _cross_operands(plan, Q, K, V)
+    _check(O, "O", dtype, plan.device, plan.q_shape)
+    _check(dO, "dO", dtype, plan.device, plan.q_shape)
+    _check(lse, "lse", torch.float32, plan.device, plan.q_shape[:2])
+    if scale is None:
+        scale = 1.0 / math.sqrt(plan.d)
+    with _on(plan.device, stream):
+        dQ = torch.empty(plan.q_shape, dtype=dtype, device=plan.device)
+        dK, dV = (torch.empty(plan.k_shape, dtype=dtype, device=plan.device)
+                  for _ in range(2))
+        ws = _workspace(plan._backward_bytes, plan.device)
+        _call("f3s_cross_backward", plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+              _DTYPE_CODE[dtype], O.data_ptr(), dO.data_ptr(), lse.data_ptr(), dQ.data_ptr(),
+              dK.data_ptr(), dV.data_ptr(), float(scale), _ptr(ws), plan._backward_bytes,
+              _binding._raw_stream(plan.device.index))
+    return dQ, dK, dV
+
+
+# ---- the cache -------------------------------------------------------------------
+
+class Cache:
+    """Pages of keys and values in 8 bits: codes ``k`` and ``v``
+    (float8_e4m3fn, [pages, kv_heads, page_size, d]) and a power of two for
+    each row, ``k_exp`` and ``v_exp`` (uint8, [pages, kv_heads, page_size]:
+    value = code * 2^(exp - 127)).  The tensors are the caller's and may be
+    moved or copied like any others."""
+
+    def __init__(self, k, v, k_exp, v_exp):
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("k must be a [pages, kv_heads, page_size, d] device tensor")
+        for t, n in ((k, "k"), (v, "v")):
+            _check_device_tensor(t, n, torch.float8_e4m3fn, k.device)
+        for t, n in ((k_exp, "k_exp"), (v_exp, "v_exp")):
+            _check_device_tensor(t, n, torch.uint8, k.device)
+        if v.shape != k.shape or k_exp.shape != k.shape[:3] or v_exp.shape != k.shape[:3]:
+            raise ValueError("k and v must share one shape, k_exp and v_exp its first three")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.device = k.device
+        self.n_pages, self.kv_heads, self.page_size, self.d = k.shape
+        if self.n_pages > 2**31 - 1:
+            raise ValueError("more than 2^31 - 1 pages")
+        self._struct = _CacheStruct(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(),
+                                    v_exp.data_ptr(), self.n_pages, self.kv_heads,
+                                    self.page_size, self.d)
+        self._ref = ctypes.byref(self._struct)
+
+    @classmethod
+    def empty(cls, n_pages, page_size, kv_heads, d, device="cuda"):
+        """A cache of new pages, all zeros."""
+        shape = (int(n_pages), int(kv_heads), int(page_size), int(d))
+        codes = [torch.zeros(shape, dtype=torch.uint8, device=device)
+                 .view(torch.float8_e4m3fn) for _ in range(2)]
+        powers = [torch.zeros(shape[:3], dtype=torch.uint8, device=device) for _ in range(2)]
+        return cls(*codes, *powers)
+
+
+def _sequences(cache, table, lens):
+    """(number of sequences, pages of a table row), checked."""
+    _check_device_tensor(table, "table", torch.int32, cache.device)
+    _check_device_tensor(lens, "lens", torch.int32, cache.device)
+    if table.dim() != 2 or lens.dim() != 1 or table.shape[0] != lens.shape[0]:
+        raise ValueError("table must be [sequences, pages], lens [sequences]")
+    return table.shape
+
+
+def cache_write(cache, K, V, table, lens, stream=None):
+    """f3s_cache_write: the newest rows of every sequence, K and V [sequences,
+    n, kv_heads, d] in fp16 or bf16, quantised into the pages of ``table``
+    (int32 [sequences, pages]).  ``lens`` (int32) are the sequences' lengths
+    with these rows; row t goes to position lens[b] - n + t."""
+    B, pages = _sequences(cache, table, lens)
+    dtype = _dtype_of(K, "K")
+    if K.dim() != 4:
+        raise ValueError("K must be [sequences, n, kv_heads, d]")
+    n = K.shape[1]
+    for t, name in ((K, "K"), (V, "V")):
+        _check(t, name, dtype, cache.device, (B, n, cache.kv_heads, cache.d))
+    with _on(cache.device, stream):
+        _call("f3s_cache_write", cache._ref, K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
+              table.data_ptr(), pages, lens.data_ptr(), B, n,
+              _binding._raw_stream(cache.device.index))
+
+
+def cache_read(cache, table, lens, n, dtype=torch.float16, stream=None):
+    """f3s_cache_read: the ``n`` newest rows of every sequence, (K, V) of
+    ``dtype`` (float16, bfloat16 or float32), [sequences, n, kv_heads, d]."""
+    B, pages = _sequences(cache, table, lens)
+    if dtype not in _HALF + (torch.float32,):
+        raise TypeError("dtype must be float16, bfloat16 or float32")
+    shape = (B, int(n), cache.kv_heads, cache.d)
+    with _on(cache.device, stream):
+        K, V = (torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
+        _call("f3s_cache_read", cache._ref, K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
+              table.data_ptr(), pages, lens.data_ptr(), B, int(n),
+              _binding._raw_stream(cache.device.index))
+    return K, V
+
+
+def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, out=None,
+                 lse=None, stream=None):
+    """f3s_cache_attend: the newest tokens of every sequence, Q [sequences, n,
+    heads, d] in fp16 or bf16, attend to the first ``prefix_len`` tokens of the
+    pages ``prefix`` (int32, shared by all sequences) and to their own cached
+    keys up to themselves.  Returns (O, lse): O like Q, lse fp32 [sequences, n,
+    heads]."""
+    B, pages = _sequences(cache, table, lens)
+    dtype = _dtype_of(Q, "Q")
+    if Q.dim() != 4 or Q.shape[2] < 1 or Q.shape[2] % cache.kv_heads:
+        raise ValueError("Q must be [sequences, n, heads, d], heads a multiple of kv_heads")
+    n, heads = Q.shape[1:3]
+    _check(Q, "Q", dtype, cache.device, (B, n, heads, cache.d))
+    prefix_len = int(prefix_len)
+    if prefix_len < 0 or (prefix is None) != (prefix_len == 0):
+        raise ValueError("prefix and a positive prefix_len come together")
+    if prefix is not None:
+        _check_device_tensor(prefix, "prefix", torch.int32, cache.device)
+        if prefix.dim() != 1 or prefix.numel() * cache.page_size < prefix_len:
+            raise ValueError("prefix must name enough pages for prefix_len tokens")
+    if scale is None:
+        scale = 1.0 / math.sqrt(cache.d)
+    sizes = (pages, B, n, heads)
+    with _on(cache.device, stream):
+        out = _result(out, "out", Q.shape, dtype, cache.device)
+        lse = _result(lse, "lse", Q.shape[:3], torch.float32, cache.device)
+        nbytes = _lib().f3s_cache_attend_workspace_bytes(cache._ref, *sizes, prefix_len)
+        ws = _workspace(nbytes, cache.device)
+        _call("f3s_cache_attend", cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype],
+              out.data_ptr(), lse.data_ptr(), table.data_ptr(), pages, lens.data_ptr(), B, n,
+              heads, _ptr(prefix), prefix_len, float(scale), _ptr(ws), nbytes,
+              _binding._raw_stream(cache.device.index))
+    return out, lse
