@@ -16,7 +16,8 @@ SOURCES = ["f3s_api.hip", "plan_kernels.hip", "fused3s.hip", "fused3s_bf16.hip",
            "backward.hip", "backward_bf16.hip", "backward_noalloc.hip", "probe.hip",
            "transpose.hip", "worklist.hip", "radix.hip", "cache.hip", "attend.hip",
            "attend_f16.hip", "attend_bf16.hip", "cross.hip", "cross_few_f16.hip",
-           "cross_few_bf16.hip"]
+           "cross_few_bf16.hip", "cross_many_f16.hip", "cross_many_bf16.hip",
+           "cross_backward_f16.hip", "cross_backward_bf16.hip"]
 
 # The plan and transposition sources are compiled as relocatable device code
 # and linked into ONE device code object: the runtime loads a code object on

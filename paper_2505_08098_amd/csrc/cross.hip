@@ -6,6 +6,7 @@
 #include <new>
 #include <vector>
 
+#include "cross_backward.h"
 #include "cross_few.h"
 
 namespace {
@@ -16,6 +17,9 @@ using f3s::set_status;
 
 // Workgroups of four waves that fill the GPU (256 compute units).
 constexpr int64_t kFewWorkgroups = 1024;
+constexpr int64_t kManyWorkgroups = 512;
+// Query rows of a key head up to which a sequence counts as short.
+constexpr int64_t kFewLongest = 32;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
@@ -65,7 +69,7 @@ struct Division {
                         int64_t e = units * (k + 1) / n * unit;
                         if (e > r.others) e = r.others;
                         items.push_back({h, row, rows, (int32_t)(r.other + b), (int32_t)(e - b),
-                                         n > 1 ? (int32_t)parts : -1, {}});
+                                         n > 1 ? (int32_t)parts : -1, (int32_t)k, 0});
                         if (n > 1) parts += rows;
                     }
                 }
@@ -91,7 +95,7 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
     }
     if (q_ptr[0] != 0 || k_ptr[0] != 0) return nullptr;
     const int64_t g = n_heads / n_kv;
-    std::vector<Range> fwd;
+    std::vector<Range> fwd, keys;
     int64_t longest = 0;
     for (int32_t b = 0; b < n; ++b) {
         if (q_ptr[b + 1] < q_ptr[b] || k_ptr[b + 1] < k_ptr[b]) return nullptr;
@@ -101,14 +105,22 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
         // (rows that are padding walk nothing: their results are zeros)
         if (ql) fwd.push_back({q_ptr[b] * g, ql * g, k_ptr[b], kl});
         if (ql < q) fwd.push_back({(q_ptr[b] + ql) * g, (q - ql) * g, 0, 0});
+        if (kl) keys.push_back({k_ptr[b], kl, q_ptr[b] * g, ql * g});
+        if (kl < k) keys.push_back({k_ptr[b] + kl, k - kl, 0, 0});
         if (ql * g > longest) longest = ql * g;
     }
     *st = F3S_ERR_TOO_LARGE;
     if (q_ptr[n] * g > 0x7FFFFFFF || (double)q_ptr[n] * n_heads / 16 + n_heads > 2147483647.0)
         return nullptr;
-    Division f;
-    f.make(fwd, n_kv, f3s::kFewRows, 64, 256, kFewWorkgroups);
-    if (!f.fits()) return nullptr;
+    Division f, dq, dkv;
+    const bool few = longest <= kFewLongest;
+    if (few)
+        f.make(fwd, n_kv, f3s::kFewRows, 64, 256, kFewWorkgroups);
+    else
+        f.make(fwd, n_kv, f3s::kManyRows, 64, 256, kManyWorkgroups);
+    dq.make(fwd, n_kv, f3s::kManyRows, 64, 256, kManyWorkgroups);
+    dkv.make(keys, n_kv, f3s::kManyRows, 64, 256, kManyWorkgroups);
+    if (!f.fits() || !dq.fits() || !dkv.fits()) return nullptr;
 
     f3s_cross_plan_s *p = new f3s_cross_plan_s;
     p->n_heads = n_heads;
@@ -117,10 +129,19 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
     p->d = d;
     p->q_rows = q_ptr[n];
     p->k_rows = k_ptr[n];
+    p->few = few;
     p->n_fwd = (int32_t)f.items.size();
     p->n_fwd_merge = (int32_t)f.merges.size();
     p->fwd_merge_rows = f.merge_rows;
     p->fwd_parts = f.parts;
+    p->n_dq = (int32_t)dq.items.size();
+    p->n_dq_merge = (int32_t)dq.merges.size();
+    p->dq_merge_rows = dq.merge_rows;
+    p->dq_parts = dq.parts;
+    p->n_dkv = (int32_t)dkv.items.size();
+    p->n_dkv_merge = (int32_t)dkv.merges.size();
+    p->dkv_merge_rows = dkv.merge_rows;
+    p->dkv_parts = dkv.parts;
     const struct {
         const void *src;
         size_t bytes;
@@ -128,6 +149,10 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
     } lists[] = {
         {f.items.data(), f.items.size() * sizeof(DenseItem), (void **)&p->fwd},
         {f.merges.data(), f.merges.size() * sizeof(DenseMerge), (void **)&p->fwd_merge},
+        {dq.items.data(), dq.items.size() * sizeof(DenseItem), (void **)&p->dq},
+        {dq.merges.data(), dq.merges.size() * sizeof(DenseMerge), (void **)&p->dq_merge},
+        {dkv.items.data(), dkv.items.size() * sizeof(DenseItem), (void **)&p->dkv},
+        {dkv.merges.data(), dkv.merges.size() * sizeof(DenseMerge), (void **)&p->dkv_merge},
     };
     size_t bytes = 0;
     for (const auto &l : lists) bytes += round256(l.bytes);
@@ -162,6 +187,15 @@ bool on_device(const f3s_cross_plan_s *p, hipStream_t stream)
 size_t parts_bytes(int64_t rows, int32_t d, int32_t record)
 {
     return rows ? round256((size_t)rows * d * 4) + round256((size_t)rows * record * 4) : 0;
+}
+
+// |scale| log2 e.  Scores that are left out are -inf and stay so under a factor
+// that is not 0: a scale of 0 counts as 2^-120, which turns every finite score
+// of an f16 or bf16 product below 2^100 into 0 as well.
+float base2_scale(float scale)
+{
+    const float s = (float)(fabs((double)scale) * 1.4426950408889634);
+    return s < 0x1p-120f ? 0x1p-120f : s;
 }
 
 bool workspace_ok(const void *w, size_t have, size_t need)
@@ -235,13 +269,14 @@ f3s_status_t f3s_cross_forward(f3s_cross_plan_t p, const void *Q, const void *K,
     a.lse = lse;
     a.q = {p->n_heads, p->g};
     a.n_kv = p->n_kv;
-    a.sl2 = (float)(fabs((double)scale) * 1.4426950408889634);
+    a.sl2 = base2_scale(scale);
     a.flip = signbit(scale) ? 0x80008000u : 0u;
     a.part_o = (float *)workspace;
     a.part_ml = (float *)((char *)workspace + round256((size_t)p->fwd_parts * p->d * 4));
     const bool bf16 = dtype == F3S_DTYPE_BF16;
-    hipError_t e = bf16 ? f3s::launch_cross_few_bf16(*p, a, stream)
-                        : f3s::launch_cross_few_f16(*p, a, stream);
+    auto launch = p->few ? (bf16 ? f3s::launch_cross_few_bf16 : f3s::launch_cross_few_f16)
+                         : (bf16 ? f3s::launch_cross_many_bf16 : f3s::launch_cross_many_f16);
+    hipError_t e = launch(*p, a, stream);
     if (e == hipSuccess && p->n_fwd_merge) {
         const f3s::CrossMergeArgs m = {p->fwd_merge, a.part_o, a.part_ml, O, lse, a.q, 0};
         e = bf16 ? f3s::launch_cross_merge_bf16(*p, m, stream)
@@ -252,16 +287,70 @@ f3s_status_t f3s_cross_forward(f3s_cross_plan_t p, const void *Q, const void *K,
 
 size_t f3s_cross_backward_workspace_bytes(f3s_cross_plan_t p)
 {
-    return 0;
+    if (!p) return 0;
+    return round256((size_t)p->q_rows * p->n_heads * 8) + parts_bytes(p->dq_parts, p->d, 0) +
+           parts_bytes(p->dkv_parts, 2 * p->d, 0);
 }
 
-f3s_status_t f3s_cross_backward(f3s_cross_plan_t plan, const void *Q, const void *K,
+f3s_status_t f3s_cross_backward(f3s_cross_plan_t p, const void *Q, const void *K,
                                 const void *V, f3s_dtype_t dtype, const void *O,
                                 const void *dO, const float *lse, void *dQ, void *dK,
                                 void *dV, float scale, void *workspace,
                                 size_t workspace_bytes, hipStream_t stream)
 {
-    return set_status(F3S_ERR_UNSUPPORTED);
+    if (!p || !isfinite(scale)) return set_status(F3S_ERR_INVALID_VALUE);
+    if (dtype != F3S_DTYPE_F16 && dtype != F3S_DTYPE_BF16)
+        return set_status(F3S_ERR_UNSUPPORTED);
+    if (p->q_rows == 0 && p->k_rows == 0) return F3S_OK;
+    if (!on_device(p, stream)) return set_status(F3S_ERR_INVALID_VALUE);
+    const size_t qb = (size_t)p->q_rows * p->n_heads * p->d * 2;
+    const size_t kb = (size_t)p->k_rows * p->n_kv * p->d * 2;
+    const size_t lb = (size_t)p->q_rows * p->n_heads * 4;
+    const size_t need = f3s_cross_backward_workspace_bytes(p);
+    if (!workspace_ok(workspace, workspace_bytes, need))
+        return set_status(F3S_ERR_INVALID_VALUE);
+    struct Span {
+        const void *p;
+        size_t n;
+    };
+    const Span in[] = {{Q, qb}, {K, kb}, {V, kb}, {O, qb}, {dO, qb}, {lse, lb},
+                       {workspace, need}};
+    const Span out[] = {{dQ, qb}, {dK, kb}, {dV, kb}};
+    for (const Span &x : in)
+        if ((x.n && !x.p) || !aligned(x.p, x.p == lse ? 4 : 16))
+            return set_status(F3S_ERR_INVALID_VALUE);
+    for (const Span &x : out) {
+        if ((x.n && !x.p) || !aligned(x.p, 16)) return set_status(F3S_ERR_INVALID_VALUE);
+        for (const Span &y : in)
+            if (overlaps(x.p, x.n, y.p, y.n)) return set_status(F3S_ERR_INVALID_VALUE);
+        for (const Span &y : out)
+            if (&x != &y && overlaps(x.p, x.n, y.p, y.n))
+                return set_status(F3S_ERR_INVALID_VALUE);
+    }
+    f3s::CrossBwdArgs a = {};
+    a.Q = Q;
+    a.K = K;
+    a.V = V;
+    a.O = O;
+    a.G = dO;
+    a.lse = lse;
+    a.dQ = dQ;
+    a.dK = dK;
+    a.dV = dV;
+    a.q = {p->n_heads, p->g};
+    a.n_kv = p->n_kv;
+    a.sl2 = base2_scale(scale);
+    a.scale = scale;
+    a.flip = signbit(scale) ? 0x80008000u : 0u;
+    char *w = (char *)workspace;
+    a.stats = (float2 *)w;
+    w += round256((size_t)p->q_rows * p->n_heads * 8);
+    a.part_dq = (float *)w;
+    w += parts_bytes(p->dq_parts, p->d, 0);
+    a.part_dkv = (float *)w;
+    return set_status(f3s::status_of(dtype == F3S_DTYPE_BF16
+                                         ? f3s::launch_cross_backward_bf16(*p, a, stream)
+                                         : f3s::launch_cross_backward_f16(*p, a, stream)));
 }
 
 }  // extern "C"

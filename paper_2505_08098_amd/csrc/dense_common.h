@@ -20,10 +20,11 @@ struct QueryRows {
     int32_t n_heads;  // query heads
     int32_t g;        // query heads per key head
 };
+// (r < 2^31: a 64-bit division takes some 50 instructions more)
 __device__ __forceinline__ int64_t query_row(const QueryRows &q, int kh, int64_t r)
 {
-    const int64_t t = r / q.g;
-    return t * q.n_heads + (int64_t)kh * q.g + (r - t * q.g);
+    const uint32_t t = (uint32_t)r / (uint32_t)q.g;
+    return (int64_t)t * q.n_heads + kh * q.g + ((uint32_t)r - t * (uint32_t)q.g);
 }
 
 // One workgroup's share of a forward or backward pass over a ragged batch.
@@ -36,7 +37,8 @@ struct DenseItem {
     int32_t other;    // first row of the other side
     int32_t others;   // rows of the other side (0: the results are zeros)
     int32_t part;     // first partial row, -1: the results are final
-    int32_t pad[2];
+    int32_t piece;    // which part of a split range
+    int32_t pad;
 };
 static_assert(sizeof(DenseItem) == 32, "DenseItem must be 32 bytes");
 

@@ -114,6 +114,16 @@ __device__ __forceinline__ _Float16 to16(float x)
         return (_Float16)x;
 }
 
+// Its value.
+template <int kIn>
+__device__ __forceinline__ float from16(_Float16 x)
+{
+    if constexpr (kIn == kInBF16)
+        return (float)__builtin_bit_cast(__bf16, x);
+    else
+        return (float)x;
+}
+
 __device__ __forceinline__ float sum_xor16_32(float v)
 {
     int b = __builtin_bit_cast(int, v);

@@ -1,0 +1,275 @@
+// Attention of many query rows to a range of keys: forward of cross attention
+// (f3s_cross_forward).
+//
+// A workgroup of four waves has up to 128 query rows, 32 to a wave, and walks
+// the keys in tiles of 64 (d > 128: 32) that all four use: K and V tiles pass through LDS in
+// two buffers, the next one filled while the last is worked on, with one
+// barrier a tile.  With 128 rows a tile of K and V (4 d bytes a key) feeds
+// 512 d operations a key: the matrix units and the softmax's vector
+// instructions are the bound, not memory.
+//
+// S^T = K Q^T with the 32x32x16 product: a lane holds one query row and half
+// of a tile's keys, which is at once the operand layout of O^T += V^T P^T (V
+// read transposed from LDS), so the probabilities never leave their lane.  The
+// running maximum needs one exchange a tile, between the two halves of a wave;
+// sums stay in the lane until the end.
+#pragma once
+
+#include "few_rows.h"
+
+namespace f3s {
+
+constexpr int kManyRows = 128;  // query rows of a workgroup
+constexpr int kManyThreads = 256;
+// Rows of the other side in a tile (wide rows: fewer, or the registers that
+// hold the next tile on its way into LDS would spill).
+constexpr int many_keys(int d) { return d <= 128 ? 64 : 32; }
+
+// D(32x32, fp32) += A(32x16) B(16x32), f16 or bf16.  Lane l holds A row l % 32
+// and B column l % 32 with reduction slots 8 (l / 32) .. + 7, and of D column
+// l % 32 the rows 8 (r / 4) + 4 (l / 32) + r % 4, r = 0 .. 15 (checked on the GPU).
+template <int kIn>
+__device__ __forceinline__ f16v mfma32(h8 a, h8 b, f16v c)
+{
+    if constexpr (kIn == kInBF16) {
+        typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a),
+                                                       __builtin_bit_cast(b8, b), c, 0, 0, 0);
+    } else {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+}
+
+__device__ __forceinline__ f16v zero16()
+{
+    f16v z;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) z[k] = 0.f;
+    return z;
+}
+
+// A tile of one head's rows in LDS, row-major with padded rows.
+template <int D, int kPad>
+struct ManyTile {
+    static constexpr int kRows = many_keys(D);
+    static constexpr int kStride = 2 * D + kPad;       // bytes
+    static constexpr int kBytes = kRows * kStride;
+    static constexpr int kPieces = D / 8;              // 16-byte pieces of a row
+    static constexpr int kLoads = (kRows * kPieces + kManyThreads - 1) / kManyThreads;
+    static constexpr bool kEven = kRows * kPieces % kManyThreads == 0;
+    // Row of a thread's j-th piece (behind the tile where the division is not even).
+    static __device__ __forceinline__ int row_of(int j)
+    {
+        return ((int)threadIdx.x + kManyThreads * j) / kPieces;
+    }
+
+    // Pieces of rows first .. first + kRows - 1 of a [rows, heads, D] array (from `end`
+    // on the last row again: whatever stands behind may not be finite, and 0
+    // times it is added).
+    static __device__ __forceinline__ void load(u4 (&r)[kLoads], const void *x, int64_t base,
+                                                int heads, int head, int first, int end)
+    {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int f = (int)threadIdx.x + kManyThreads * j, row = row_of(j);
+            const int64_t at = base + min(first + row, end - 1);
+            r[j] = *reinterpret_cast<const u4 *>(
+                reinterpret_cast<const uint8_t *>(x) + (at * heads + head) * (2 * D) +
+                (f - row * kPieces) * 16);
+        }
+    }
+    static __device__ __forceinline__ void store(uint8_t *tile, const u4 (&r)[kLoads])
+    {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int f = (int)threadIdx.x + kManyThreads * j, row = row_of(j);
+            if (kEven || row < kRows)
+                *reinterpret_cast<u4 *>(tile + row * kStride + (f - row * kPieces) * 16) = r[j];
+        }
+    }
+    // Operand with the tile's rows row .. row + 31 and elements 16 c .. + 15.
+    static __device__ __forceinline__ h8 rows32(const uint8_t *tile, int row, int c, int lane)
+    {
+        return *reinterpret_cast<const h8 *>(tile + (row + (lane & 31)) * kStride + 32 * c +
+                                             16 * (lane >> 5));
+    }
+    // Operand with elements d .. d + 31 as rows and the tile's rows row .. + 15 as
+    // reduction slots, in the order in which a lane holds them of an S^T
+    // accumulator: 4 h + 0..3 and 8 + 4 h + 0..3 (h: the lane's half).
+    static __device__ __forceinline__ h8 cols32(const uint8_t *tile, int row, int d, int lane)
+    {
+        const int s = lane & 15;
+        const _Float16 *p = reinterpret_cast<const _Float16 *>(
+            tile + (row + 4 * (lane >> 5) + (s >> 2)) * kStride +
+            2 * (d + 16 * (lane >> 4 & 1) + 4 * (s & 3)));
+        return cat44(lds_read_tr(p), lds_read_tr(p + 8 * kStride / 2));
+    }
+};
+
+// 32 rows of one head as an operand (row row + lane % 32; zeros from `rows` on).
+template <int D>
+__device__ __forceinline__ void load_rows32(h8 (&x)[D / 16], const void *src, int64_t at,
+                                            bool there, uint32_t flip, int lane)
+{
+    const _Float16 *p = reinterpret_cast<const _Float16 *>(src) + at * D + 8 * (lane >> 5);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+        u4 v = *reinterpret_cast<const u4 *>(p + 16 * c);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = there ? v[k] ^ flip : 0u;
+        x[c] = __builtin_bit_cast(h8, v);
+    }
+}
+
+// Eight of an accumulator's values as an operand of 16 reduction slots.
+template <int kIn>
+__device__ __forceinline__ h8 pack8(const f16v &x, int half)
+{
+    h8 p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = to16<kIn>(x[8 * half + e]);
+    return p;
+}
+
+__device__ __forceinline__ float sum_xor32(float v)
+{
+    const int b = __builtin_bit_cast(int, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return __builtin_bit_cast(float, (int)r[0]) + __builtin_bit_cast(float, (int)r[1]);
+}
+
+// Waves per SIMD that the registers leave room for.
+constexpr int many_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
+
+template <int D, int kIn>
+__global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
+    FewArgs a, const DenseItem *items)
+{
+    using TK = ManyTile<D, 16>;
+    using TV = ManyTile<D, 32>;
+    constexpr int kKeys = TK::kRows, kBlocks = kKeys / 32;
+    __shared__ __attribute__((aligned(16))) uint8_t s_k[2][TK::kBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t s_v[2][TV::kBytes];
+    const DenseItem it = items[blockIdx.x];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int mine = 32 * wave + (lane & 31);  // this lane's query row
+    const bool there = mine < it.rows;
+    const bool busy = 32 * wave < it.rows;     // (the wave has rows at all)
+
+    h8 q[D / 16];
+    load_rows32<D>(q, a.Q, query_row(a.q, it.head, (int64_t)it.row + (there ? mine : 0)), there,
+                   a.flip, lane);
+    f16v o[D / 32];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = zero16();
+    float m_run = -INFINITY, l_run = 0.f;
+
+    u4 kr[TK::kLoads], vr[TV::kLoads];
+    const int n = (it.others + kKeys - 1) / kKeys;
+    auto load = [&](int t) {
+        TK::load(kr, a.K, it.other, a.n_kv, it.head, kKeys * t, it.others);
+        TV::load(vr, a.V, it.other, a.n_kv, it.head, kKeys * t, it.others);
+    };
+    auto store = [&](int t) {
+        TK::store(s_k[t & 1], kr);
+        TV::store(s_v[t & 1], vr);
+    };
+    if (n > 0) {
+        load(0);
+        store(0);
+        load(n > 1 ? 1 : 0);
+    }
+    for (int t = 0; t < n; ++t) {
+        __syncthreads();
+        if (t + 1 < n) {
+            store(t + 1);
+            load(min(t + 2, n - 1));
+        }
+        if (!busy) continue;
+        const uint8_t *k = s_k[t & 1], *v = s_v[t & 1];
+        f16v s[kBlocks];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) s[b] = zero16();
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+                s[b] = mfma32<kIn>(TK::rows32(k, 32 * b, c, lane), q[c], s[b]);
+        }
+        const int left = it.others - kKeys * t;
+        if (left < kKeys) {
+#pragma unroll
+            for (int e = 0; e < 16 * kBlocks; ++e) {
+                const int key = 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * (lane >> 5) + (e & 3);
+                if (key >= left) s[e >> 4][e & 15] = -INFINITY;
+            }
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 16 * kBlocks; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
+        mx = max_xor32(mx) * a.sl2;
+        const float m_new = fmaxf(m_run, mx);
+        const float m_ref = m_new == -INFINITY ? 0.f : m_new;
+        if (__ballot(m_new > m_run)) {
+            const float alpha = __builtin_amdgcn_exp2f(m_run - m_ref);
+            l_run *= alpha;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) o[d] *= alpha;
+            m_run = m_new;
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16 * kBlocks; ++e) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], a.sl2, -m_ref));
+            s[e >> 4][e & 15] = p;
+            sum += p;
+        }
+        l_run += sum;
+#pragma unroll
+        for (int c = 0; c < 2 * kBlocks; ++c) {
+            const h8 p = pack8<kIn>(s[c >> 1], c & 1);
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+                o[d] = mfma32<kIn>(TV::cols32(v, 16 * c, 32 * d, lane), p, o[d]);
+        }
+    }
+    const float l = sum_xor32(l_run);
+    if (!there) return;
+    const int col = 4 * (lane >> 5);
+    if (it.part >= 0) {
+        float *to = a.part_o + ((int64_t)it.part + mine) * D + col;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<f4 *>(to + 32 * d + 8 * k) =
+                    f4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]};
+        if (col == 0) {
+            a.part_ml[2 * ((int64_t)it.part + mine)] = m_run;
+            a.part_ml[2 * ((int64_t)it.part + mine) + 1] = l;
+        }
+        return;
+    }
+    const int64_t at = query_row(a.q, it.head, (int64_t)it.row + mine);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            store4<kIn>(a.O, at * D + 32 * d + 8 * k + col,
+                        f4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * inv);
+    if (col == 0) a.lse[at] = natural_lse(m_run, l);
+}
+
+template <int D, int kIn>
+hipError_t launch_cross_many_d(const f3s_cross_plan_s &p, const FewArgs &a, hipStream_t s)
+{
+    if (p.n_fwd) k_cross_many<D, kIn><<<p.n_fwd, kManyThreads, 0, s>>>(a, p.fwd);
+    return hipGetLastError();
+}
+
+hipError_t launch_cross_many_f16(const f3s_cross_plan_s &p, const FewArgs &a, hipStream_t s);
+hipError_t launch_cross_many_bf16(const f3s_cross_plan_s &p, const FewArgs &a, hipStream_t s);
+
+}  // namespace f3s

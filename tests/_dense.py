@@ -2,7 +2,8 @@
 16-bit results may be off, for the tests.
 
 Bounds are per element.  u is half a step of the result's type relative to the
-value (bf16 2^-8, fp16 2^-11).  A result is rounded once (u |result|); the
+value (bf16 2^-8, fp16 2^-11); fp16 values below 2^-14 are multiples of 2^-24, so
+that half a step there is 2^-25 (``tiny``).  A result is rounded once (u |result|); the
 probabilities (and score gradients) are rounded to 16 bits before their
 product (u times the sum of the magnitudes); 32-bit sums add N * 2^-24 of the
 sum of magnitudes for N terms in a row."""
@@ -15,6 +16,11 @@ F32 = 2.0 ** -24
 
 def half_step(dtype):
     return torch.finfo(dtype).eps / 2
+
+
+def tiny(u):
+    """Half a step between the smallest values of the type whose half step is u."""
+    return 2.0 ** -25 if u < 2.0 ** -10 else 2.0 ** -134
 
 
 def attention(Q, K, V, scale, u, up=None, seen=None, floor=None):
@@ -39,7 +45,7 @@ def attention(Q, K, V, scale, u, up=None, seen=None, floor=None):
     ep = 2 * worst + (terms + 8) * F32
     absO = P @ V.abs()
     O = P @ V
-    O_tol = (up + ep[:, None]) * absO + u * O.abs() + 2.0 ** -24 * u
+    O_tol = (up + ep[:, None]) * absO + u * O.abs() + tiny(u) + tiny(up) * V.abs().sum(0)
     if floor is not None:
         O_tol = O_tol + floor.sum(0)
     lse_tol = worst + (terms + 8) * F32 + 4 * F32 * torch.where(lse == -math.inf, 0.0, lse.abs())
@@ -61,7 +67,7 @@ def gradients(Q, K, V, G, scale, u, f):
     edP = (d + 4) * F32 * (G.abs() @ V.abs().T)
     ed = (G.abs() * f["O_tol"]).sum(1, keepdim=True) \
         + (d + 4) * F32 * (G.abs() * f["O"].abs()).sum(1, keepdim=True)
-    edS = u * dS.abs() + P * (edP + ed) + eP * (dP - delta).abs() + 2.0 ** -24 * (u > 2 ** -10 and 0.0 or 1.0)
+    edS = u * dS.abs() + P * (edP + ed) + eP * (dP - delta).abs() + tiny(u)
     n, m = P.shape
     sums_q, sums_k = (m / 32 + 64) * F32, (n / 32 + 64) * F32
     s = abs(scale)
@@ -69,7 +75,7 @@ def gradients(Q, K, V, G, scale, u, f):
         dQ=scale * dS @ K, dK=scale * dS.T @ Q, dV=P.T @ G,
         dQ_tol=s * ((edS + sums_q * dS.abs()) @ K.abs()),
         dK_tol=s * ((edS + sums_k * dS.abs()).T @ Q.abs()),
-        dV_tol=(u * P + eP + sums_k * P + 2.0 ** -25).T @ G.abs())
+        dV_tol=(u * P + eP + sums_k * P + tiny(u)).T @ G.abs())
 
 
 def close(got, want, tol, what):

@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from _dense import attention, close, gradients, half_step
+from _dense import attention, close, gradients, half_step, tiny
 
 pytestmark = pytest.mark.gpu
 
@@ -66,7 +66,7 @@ def _case(gpu, dtype, d, kv, g, q_len, k_len, padded=False, scale=None, grad=Tru
     close(lse, want["lse"], tol["lse"], "lse")
     if grad:
         for n, x in zip(("dQ", "dK", "dV"), grads):
-            close(x, want[n], tol[n] + u * want[n].abs() + 2.0 ** -24 * u, n)
+            close(x, want[n], tol[n] + u * want[n].abs() + tiny(u), n)
     return plan, dev, O, lse, grads
 
 
@@ -88,3 +88,10 @@ CASES = [
 @pytest.mark.parametrize("d,kv,g,q,k", CASES)
 def test_forward(gpu, dtype, padded, d, kv, g, q, k):
     _case(gpu, dtype, d, kv, g, q, k, padded=padded, grad=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("padded", [False, True])
+@pytest.mark.parametrize("d,kv,g,q,k", CASES)
+def test_gradients(gpu, dtype, padded, d, kv, g, q, k):
+    _case(gpu, dtype, d, kv, g, q, k, padded=padded, seed=1)
