@@ -28,7 +28,8 @@ typedef struct f3s_cross_plan_s *f3s_cross_plan_t;
  * units; one plan serves every layer, forward and backward.
  *   q_ptr, k_ptr   HOST int32[n_seqs + 1], first 0, non-decreasing
  *   q_len, k_len   HOST int32[n_seqs] or NULL, 0 <= len[b] <= ptr[b+1] - ptr[b]
- *   n_heads        query heads, a multiple of n_kv_heads >= 1
+ *   n_heads        query heads, a multiple of n_kv_heads >= 1, at most 65535
+ *                  (else F3S_ERR_UNSUPPORTED)
  *   d              multiple of 32, 32 <= d <= 256 (else F3S_ERR_UNSUPPORTED)
  * The plan copies what it needs.  Synchronous on the current device's null
  * stream.  NULL on error (f3s_last_error); F3S_ERR_TOO_LARGE if the batch

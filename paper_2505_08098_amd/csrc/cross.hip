@@ -89,7 +89,8 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
 {
     *st = F3S_ERR_INVALID_VALUE;
     if (!q_ptr || !k_ptr || n < 0 || n_kv < 1 || n_heads < 1 || n_heads % n_kv) return nullptr;
-    if (d < 32 || d > f3s::kMaxD || d % 32 != 0) {
+    // (a tile's 64 rows of all heads have to lie within 4 GiB)
+    if (d < 32 || d > f3s::kMaxD || d % 32 != 0 || n_heads > 65535) {
         *st = F3S_ERR_UNSUPPORTED;
         return nullptr;
     }
@@ -267,7 +268,7 @@ f3s_status_t f3s_cross_forward(f3s_cross_plan_t p, const void *Q, const void *K,
     a.V = V;
     a.O = O;
     a.lse = lse;
-    a.q = {p->n_heads, p->g};
+    a.q = f3s::query_rows(p->n_heads, p->g);
     a.n_kv = p->n_kv;
     a.sl2 = base2_scale(scale);
     a.flip = signbit(scale) ? 0x80008000u : 0u;
@@ -337,7 +338,7 @@ f3s_status_t f3s_cross_backward(f3s_cross_plan_t p, const void *Q, const void *K
     a.dQ = dQ;
     a.dK = dK;
     a.dV = dV;
-    a.q = {p->n_heads, p->g};
+    a.q = f3s::query_rows(p->n_heads, p->g);
     a.n_kv = p->n_kv;
     a.sl2 = base2_scale(scale);
     a.scale = scale;

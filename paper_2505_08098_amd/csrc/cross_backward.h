@@ -62,13 +62,14 @@ __device__ __forceinline__ void store_row(const f16v (&x)[(D1 - D0) / 32], float
 }
 
 constexpr int dq_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
-constexpr int dkv_waves(int d) { return d <= 64 ? 2 : 1; }
+constexpr int dq_tile(int d) { return d <= 32 || (d > 64 && d <= 128) ? 64 : 32; }
+constexpr int dkv_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
 
 template <int D, int kIn>
 __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwdArgs a,
                                                                         const DenseItem *items)
 {
-    using T = ManyTile<D, 32>;
+    using T = ManyTile<D, dq_tile(D)>;
     constexpr int kTile = T::kRows;
     __shared__ __attribute__((aligned(16))) uint8_t s_k[2][T::kBytes];
     __shared__ __attribute__((aligned(16))) uint8_t s_v[2][T::kBytes];
@@ -80,17 +81,23 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
     const bool busy = 32 * wave < it.rows;
     const int64_t at = query_row(a.q, it.head, (int64_t)it.row + (there ? mine : 0));
 
-    u4 kr[T::kLoads], vr[T::kLoads];
-    const int n = (it.others + kTile - 1) / kTile;
-    auto load = [&](int t) {
-        T::load(kr, a.K, it.other, a.n_kv, it.head, kTile * t, it.others);
-        T::load(vr, a.V, it.other, a.n_kv, it.head, kTile * t, it.others);
+    T tk, tv;
+    const uint32_t row_bytes = (uint32_t)a.n_kv * (2 * D);
+    const uint64_t base = (uint64_t)it.other * row_bytes + (uint32_t)it.head * (2 * D);
+    const uint8_t *const K = reinterpret_cast<const uint8_t *>(a.K) + base;
+    const uint8_t *const V = reinterpret_cast<const uint8_t *>(a.V) + base;
+    auto fetch = [&](int t) {
+        const int first = kTile * t, last = it.others - 1 - first;
+        const uint64_t at = (uint64_t)first * row_bytes;
+        // (behind the range: the last row again)
+        auto offset = [&](int row) { return (uint32_t)min(row, last) * row_bytes; };
+        tk.fetch(s_k[t & 1], K + at, offset);
+        tv.fetch(s_v[t & 1], V + at, offset);
     };
-    auto store = [&](int t) {
-        T::store(s_k[t & 1], kr);
-        T::store(s_v[t & 1], vr);
+    auto put = [&](int t) {
+        tk.put(s_k[t & 1]);
+        tv.put(s_v[t & 1]);
     };
-    if (n > 0) load(0);
 
     h8 q[D / 16], g[D / 16];
     load_rows32<D>(q, a.Q, at, there, a.flip, lane);
@@ -111,21 +118,14 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
     f16v dq[D / 32];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) dq[d] = zero16();
-    if (n > 0) {
-        store(0);
-        load(n > 1 ? 1 : 0);
-    }
-    for (int t = 0; t < n; ++t) {
-        __syncthreads();
-        if (t + 1 < n) {
-            store(t + 1);
-            load(min(t + 2, n - 1));
-        }
-        if (!busy) continue;
+    auto work = [&](int t) {
+        if (!busy) return;
         const uint8_t *k = s_k[t & 1], *v = s_v[t & 1];
         const int left = it.others - kTile * t;
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
+            // (one block of 32 at a time: two at once do not fit the registers)
+            if (D > 64) __builtin_amdgcn_sched_barrier(0);
             f16v s = zero16(), dp = zero16();
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
@@ -148,17 +148,27 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
                     dq[d] = mfma32<kIn>(T::cols32(k, 32 * b + 16 * c, 32 * d, lane), ds, dq[d]);
             }
         }
-    }
+        products_done();
+    };
+    walk_tiles<T::kDirect>((it.others + kTile - 1) / kTile, fetch, put, work);
     if (there)
         store_row<D, kIn, 0, D>(dq, a.scale, a.dQ, at,
                           it.part >= 0 ? a.part_dq + ((int64_t)it.part + mine) * D : nullptr,
                           lane);
 }
 
+// d = 96 and 128: the sums of dK and dV leave no room for both K and V beside
+// them if two waves are to share a SIMD, which is worth more (d = 128, 16 heads
+// over 4, 2 x 4,050 x 4,050: @@ us against @@ with one); V's rows stay in LDS.
+constexpr bool dkv_v_in_lds(int d) { return d > 32 && d <= 128; }
+constexpr int dkv_tile(int d) { return d <= 32 ? 64 : 32; }
+
 template <int D>
 struct DkvTiles {
-    using T = ManyTile<D, 32>;
+    using T = ManyTile<D, dkv_tile(D)>;
+    using V = ManyTile<D, kManyRows>;
     __attribute__((aligned(16))) uint8_t q[2][T::kBytes], g[2][T::kBytes];
+    __attribute__((aligned(16))) uint8_t v[dkv_v_in_lds(D) ? V::kBytes : 16];
     __attribute__((aligned(16))) float lse[2][T::kRows], delta[2][T::kRows];
 };
 
@@ -168,10 +178,13 @@ template <int D, int kIn, int D0, int D1>
 __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem &it,
                                           DkvTiles<D> &s)
 {
-    using T = ManyTile<D, 32>;
+    using T = typename DkvTiles<D>::T;
+    using TV = typename DkvTiles<D>::V;
+    constexpr bool kVInLds = dkv_v_in_lds(D);
     constexpr int kTile = T::kRows;
     auto &s_q = s.q, &s_g = s.g;
     auto &s_lse = s.lse, &s_delta = s.delta;
+    const uint8_t *const s_v = s.v;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int mine = 32 * wave + (lane & 31);
@@ -179,60 +192,65 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
     const bool busy = 32 * wave < it.rows;
     const int64_t at = ((int64_t)it.row + (there ? mine : 0)) * a.n_kv + it.head;
 
-    u4 qr[T::kLoads], gr[T::kLoads];
+    T tq, tg;
     float2 sr = {0.f, 0.f};
-    const int n = (it.others + kTile - 1) / kTile;
-    auto load = [&](int t) {
-#pragma unroll
-        for (int j = 0; j < T::kLoads; ++j) {
-            const int f = (int)threadIdx.x + kManyThreads * j, row = T::row_of(j);
-            const int64_t r = query_row(
-                a.q, it.head, (int64_t)it.other + min(kTile * t + row, it.others - 1));
-            const int64_t byte = r * (2 * D) + (f - row * T::kPieces) * 16;
-            qr[j] = *reinterpret_cast<const u4 *>(reinterpret_cast<const uint8_t *>(a.Q) + byte);
-            gr[j] = *reinterpret_cast<const u4 *>(reinterpret_cast<const uint8_t *>(a.G) + byte);
-        }
+    auto fetch = [&](int t) {
+        // offsets from the first row's token on
+        const uint32_t first = (uint32_t)it.other + kTile * t;
+        const int last = it.others - 1 - kTile * t;  // (behind it: the last row again)
+        const uint32_t token = row_token(a.q, first);
+        auto offset = [&](int row) {
+            const uint32_t r = first + (uint32_t)min(row, last), k = row_token(a.q, r) - token;
+            return r - token * (uint32_t)a.q.g + k * (uint32_t)(a.q.n_heads - a.q.g);
+        };
+        const uint64_t at = (uint64_t)token * a.q.n_heads + (uint32_t)(it.head * a.q.g);
+        auto bytes = [&](int row) { return offset(row) * (2 * D); };
+        tq.fetch(s_q[t & 1], reinterpret_cast<const uint8_t *>(a.Q) + at * (2 * D), bytes);
+        tg.fetch(s_g[t & 1], reinterpret_cast<const uint8_t *>(a.G) + at * (2 * D), bytes);
         if (threadIdx.x < kTile) {
-            const int row = kTile * t + (int)threadIdx.x;
-            sr = a.stats[query_row(a.q, it.head, (int64_t)it.other + min(row, it.others - 1))];
-            if (row >= it.others) sr.x = INFINITY;  // (P = 0)
+            sr = a.stats[at + offset((int)threadIdx.x)];
+            if ((int)threadIdx.x > last) sr.x = INFINITY;  // (P = 0)
         }
     };
-    auto store = [&](int t) {
-        T::store(s_q[t & 1], qr);
-        T::store(s_g[t & 1], gr);
+    auto put = [&](int t) {
+        tq.put(s_q[t & 1]);
+        tg.put(s_g[t & 1]);
         if (threadIdx.x < kTile) {
             s_lse[t & 1][threadIdx.x] = sr.x;
             s_delta[t & 1][threadIdx.x] = sr.y;
         }
     };
-    if (n > 0) load(0);
-    h8 k[D / 16], v[D / 16];
+    h8 k[D / 16], v[kVInLds ? 1 : D / 16];
     load_rows32<D>(k, a.K, at, there, a.flip, lane);  // (the sign on the rows that stay)
-    load_rows32<D>(v, a.V, at, there, 0u, lane);
+    if constexpr (kVInLds) {
+        for (int f = threadIdx.x; f < kManyRows * TV::kPieces; f += kManyThreads) {
+            const int row = f / TV::kPieces, piece = f % TV::kPieces;
+            const int64_t r = ((int64_t)it.row + min(row, it.rows - 1)) * a.n_kv + it.head;
+            *reinterpret_cast<u4 *>(s.v + row * TV::kStride +
+                                    (piece ^ TV::swizzle(row & 31)) * 16) =
+                *reinterpret_cast<const u4 *>(reinterpret_cast<const uint8_t *>(a.V) +
+                                              r * (2 * D) + piece * 16);
+        }
+    } else {
+        load_rows32<D>(v, a.V, at, there, 0u, lane);
+    }
     constexpr int kCols = (D1 - D0) / 32;
     f16v dk[kCols], dv[kCols];
 #pragma unroll
     for (int d = 0; d < kCols; ++d) dk[d] = dv[d] = zero16();
-    if (n > 0) {
-        store(0);
-        load(n > 1 ? 1 : 0);
-    }
-    for (int t = 0; t < n; ++t) {
-        __syncthreads();
-        if (t + 1 < n) {
-            store(t + 1);
-            load(min(t + 2, n - 1));
-        }
-        if (!busy) continue;
+    auto work = [&](int t) {
+        if (!busy) return;
         const uint8_t *q = s_q[t & 1], *g = s_g[t & 1];
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
-            f16v s = zero16(), dp = zero16();
+            // (one block of 32 at a time: two at once do not fit the registers)
+            if (kTile > 32) __builtin_amdgcn_sched_barrier(0);
+            f16v x = zero16(), dp = zero16();
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
-                s = mfma32<kIn>(T::rows32(q, 32 * b, c, lane), k[c], s);
-                dp = mfma32<kIn>(T::rows32(g, 32 * b, c, lane), v[c], dp);
+                x = mfma32<kIn>(T::rows32(q, 32 * b, c, lane), k[c], x);
+                dp = mfma32<kIn>(T::rows32(g, 32 * b, c, lane),
+                                 kVInLds ? TV::rows32(s_v, 32 * wave, c, lane) : v[c], dp);
             }
             f16v p;
 #pragma unroll
@@ -242,15 +260,15 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
                 const f4 w = *reinterpret_cast<const f4 *>(&s_delta[t & 1][row]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x =
-                        __builtin_amdgcn_exp2f(fmaf(s[4 * r + e], a.sl2, -l[e]));
-                    p[4 * r + e] = x;
-                    s[4 * r + e] = x * (dp[4 * r + e] - w[e]);
+                    const float y =
+                        __builtin_amdgcn_exp2f(fmaf(x[4 * r + e], a.sl2, -l[e]));
+                    p[4 * r + e] = y;
+                    x[4 * r + e] = y * (dp[4 * r + e] - w[e]);
                 }
             }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const h8 pp = pack8<kIn>(p, c), ds = pack8<kIn>(s, c);
+                const h8 pp = pack8<kIn>(p, c), ds = pack8<kIn>(x, c);
 #pragma unroll
                 for (int d = 0; d < kCols; ++d) {
                     const int row = 32 * b + 16 * c, col = D0 + 32 * d;
@@ -259,7 +277,9 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
                 }
             }
         }
-    }
+        products_done();
+    };
+    walk_tiles<T::kDirect>((it.others + kTile - 1) / kTile, fetch, put, work);
     if (!there) return;
     float *part = it.part >= 0 ? a.part_dkv + ((int64_t)it.part + mine) * (2 * D) : nullptr;
     store_row<D, kIn, D0, D1>(dk, a.scale, a.dK, at, part, lane);
@@ -271,14 +291,15 @@ __global__ __launch_bounds__(kManyThreads, dkv_waves(D)) void k_cross_dkv(
     CrossBwdArgs a, const DenseItem *items)
 {
     __shared__ DkvTiles<D> tiles;
+    const DenseItem it = items[D <= 128 ? blockIdx.x : blockIdx.x >> 1];
     if constexpr (D <= 128) {
-        cross_dkv<D, kIn, 0, D>(a, items[blockIdx.x], tiles);
+        cross_dkv<D, kIn, 0, D>(a, it, tiles);
     } else {
         constexpr int kHalf = (D / 2 + 31) / 32 * 32;
         if (blockIdx.x & 1)
-            cross_dkv<D, kIn, kHalf, D>(a, items[blockIdx.x >> 1], tiles);
+            cross_dkv<D, kIn, kHalf, D>(a, it, tiles);
         else
-            cross_dkv<D, kIn, 0, kHalf>(a, items[blockIdx.x >> 1], tiles);
+            cross_dkv<D, kIn, 0, kHalf>(a, it, tiles);
     }
 }
 

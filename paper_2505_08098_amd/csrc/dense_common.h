@@ -19,12 +19,25 @@ typedef __attribute__((address_space(3))) i2v lds_i2;
 struct QueryRows {
     int32_t n_heads;  // query heads
     int32_t g;        // query heads per key head
+    uint32_t mul;     // r / g = (2 r * mul) >> 32 >> shift for every r < 2^31:
+    int32_t shift;    // mul = ceil(2^(31 + shift) / g), shift = ceil(log2 g)
 };
-// (r < 2^31: a 64-bit division takes some 50 instructions more)
+inline QueryRows query_rows(int32_t n_heads, int32_t g)
+{
+    int shift = 0;
+    while ((1ll << shift) < g) ++shift;
+    const uint64_t two = 1ull << (31 + shift);
+    return {n_heads, g, (uint32_t)((two + (uint64_t)g - 1) / (uint64_t)g), shift};
+}
+__host__ __device__ inline uint32_t row_token(const QueryRows &q, uint32_t r)
+{
+    return (uint32_t)((uint64_t)(2 * r) * q.mul >> 32) >> q.shift;
+}
+// The row of Q, as [tokens * n_heads, d], of row r (< 2^31).
 __device__ __forceinline__ int64_t query_row(const QueryRows &q, int kh, int64_t r)
 {
-    const uint32_t t = (uint32_t)r / (uint32_t)q.g;
-    return (int64_t)t * q.n_heads + kh * q.g + ((uint32_t)r - t * (uint32_t)q.g);
+    const uint32_t t = row_token(q, (uint32_t)r);
+    return (int64_t)t * (uint32_t)(q.n_heads - q.g) + (uint32_t)r + (uint32_t)(kh * q.g);
 }
 
 // One workgroup's share of a forward or backward pass over a ragged batch.

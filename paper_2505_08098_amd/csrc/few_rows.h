@@ -104,6 +104,18 @@ __device__ __forceinline__ f4 mfma16(h8 a, h8 b, f4 c)
         return mfma16x16x32(a, b, c);
 }
 
+// Ends a loop body whose last instructions are matrix products: 19 wait states,
+// after which their results may be read.  The compiler keeps that distance
+// itself, but was seen to miss it where two paths of different length lead from
+// the last product to the first read behind the loop (the last register of an
+// accumulator was read too early).
+__device__ __forceinline__ void products_done()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 3");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // x rounded to the 16-bit type, as raw bits in an f16 register.
 template <int kIn>
 __device__ __forceinline__ _Float16 to16(float x)
@@ -380,6 +392,7 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
             }
             o[d] = mfma16<kPV>(vt, pf, o[d]);
         }
+        products_done();
     }
 
     // the four waves' states meet: scaled to the common maximum and summed

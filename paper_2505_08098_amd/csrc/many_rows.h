@@ -48,63 +48,129 @@ __device__ __forceinline__ f16v zero16()
     return z;
 }
 
-// A tile of one head's rows in LDS, row-major with padded rows.
-template <int D, int kPad>
+// A tile of one head's rows in LDS, and how it gets there.
+//
+// d a power of two: the loads write LDS themselves (16 bytes a lane), which
+// takes no registers.  A wave's load fills 1 KB in lane order, so rows cannot be
+// padded; instead the 16-byte pieces of a row change places, piece p of row r
+// standing at p ^ swizzle(r), such that the lanes of an operand read (8 rows of
+// one piece, or 4 rows of two neighbouring ones) meet different banks.
+// Other d: through registers, into padded rows.
+template <int D, int R = many_keys(D)>
 struct ManyTile {
-    static constexpr int kRows = many_keys(D);
-    static constexpr int kStride = 2 * D + kPad;       // bytes
-    static constexpr int kBytes = kRows * kStride;
+    static constexpr bool kDirect = (D & (D - 1)) == 0;
+    static constexpr int kRows = R;
     static constexpr int kPieces = D / 8;              // 16-byte pieces of a row
+    static constexpr int kStride = 2 * D + (kDirect ? 0 : 32);  // bytes
+    static constexpr int kBytes = kRows * kStride;
     static constexpr int kLoads = (kRows * kPieces + kManyThreads - 1) / kManyThreads;
     static constexpr bool kEven = kRows * kPieces % kManyThreads == 0;
-    // Row of a thread's j-th piece (behind the tile where the division is not even).
-    static __device__ __forceinline__ int row_of(int j)
+    static_assert(!kDirect || kEven, "");
+
+    static __device__ __forceinline__ int swizzle(int row)
     {
-        return ((int)threadIdx.x + kManyThreads * j) / kPieces;
+        if constexpr (!kDirect) return 0;
+        // (256 bytes are all banks; every block of 32 rows alike)
+        const int r = kPieces >= 16 ? row : (row & 31) / (16 / kPieces);
+        return ((r & 7) << 1 | (r >> 3 & 1)) & (kPieces - 1);
     }
 
-    // Pieces of rows first .. first + kRows - 1 of a [rows, heads, D] array (from `end`
-    // on the last row again: whatever stands behind may not be finite, and 0
-    // times it is added).
-    static __device__ __forceinline__ void load(u4 (&r)[kLoads], const void *x, int64_t base,
-                                                int heads, int head, int first, int end)
+    u4 r[kDirect ? 1 : kLoads];
+
+    // Start bringing in the rows that stand offset(0 .. kRows - 1) bytes (below
+    // 2^32) behind base, which is the same for all lanes: into the tile (kDirect:
+    // it is there after settle() of every wave and a barrier), or into registers
+    // for put().
+    template <typename F>
+    __device__ __forceinline__ void fetch(uint8_t *tile, const uint8_t *base, F offset)
     {
+        if constexpr (kDirect) {
+            const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int f = (int)threadIdx.x + kManyThreads * j, row = row_of(j);
-            const int64_t at = base + min(first + row, end - 1);
-            r[j] = *reinterpret_cast<const u4 *>(
-                reinterpret_cast<const uint8_t *>(x) + (at * heads + head) * (2 * D) +
-                (f - row * kPieces) * 16);
+            for (int j = 0; j < kLoads; ++j) {
+                const int f = (int)threadIdx.x + kManyThreads * j, row = f / kPieces;
+                const int piece = f % kPieces ^ swizzle(row);
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void *)(base + (offset(row) + piece * 16)),
+                    (__attribute__((address_space(3))) void *)(tile + 1024 * wave + 4096 * j),
+                    16, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int f = (int)threadIdx.x + kManyThreads * j;
+                const int row = kEven ? f / kPieces : min(f / kPieces, kRows - 1);
+                r[j] = *reinterpret_cast<const u4 *>(base + (offset(row) + f % kPieces * 16));
+            }
         }
     }
-    static __device__ __forceinline__ void store(uint8_t *tile, const u4 (&r)[kLoads])
+    __device__ __forceinline__ void put(uint8_t *tile)
     {
+        if constexpr (!kDirect) {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int f = (int)threadIdx.x + kManyThreads * j, row = row_of(j);
-            if (kEven || row < kRows)
-                *reinterpret_cast<u4 *>(tile + row * kStride + (f - row * kPieces) * 16) = r[j];
+            for (int j = 0; j < kLoads; ++j) {
+                const int f = (int)threadIdx.x + kManyThreads * j, row = f / kPieces;
+                if (kEven || row < kRows)
+                    *reinterpret_cast<u4 *>(tile + row * kStride + f % kPieces * 16) = r[j];
+            }
         }
     }
-    // Operand with the tile's rows row .. row + 31 and elements 16 c .. + 15.
+    // Operand with the tile's rows row .. row + 31 and elements 16 c .. + 15
+    // (row a multiple of 32).
     static __device__ __forceinline__ h8 rows32(const uint8_t *tile, int row, int c, int lane)
     {
-        return *reinterpret_cast<const h8 *>(tile + (row + (lane & 31)) * kStride + 32 * c +
-                                             16 * (lane >> 5));
+        const int i = lane & 31;
+        return *reinterpret_cast<const h8 *>(tile + row * kStride + i * kStride +
+                                             ((2 * c + (lane >> 5)) ^ swizzle(i)) * 16);
     }
     // Operand with elements d .. d + 31 as rows and the tile's rows row .. + 15 as
-    // reduction slots, in the order in which a lane holds them of an S^T
-    // accumulator: 4 h + 0..3 and 8 + 4 h + 0..3 (h: the lane's half).
+    // reduction slots (d a multiple of 32, row of 16), in the order in which a lane
+    // holds them of an S^T accumulator: 4 h + 0..3 and 8 + 4 h + 0..3 (h: the
+    // lane's half).
     static __device__ __forceinline__ h8 cols32(const uint8_t *tile, int row, int d, int lane)
     {
-        const int s = lane & 15;
-        const _Float16 *p = reinterpret_cast<const _Float16 *>(
-            tile + (row + 4 * (lane >> 5) + (s >> 2)) * kStride +
-            2 * (d + 16 * (lane >> 4 & 1) + 4 * (s & 3)));
-        return cat44(lds_read_tr(p), lds_read_tr(p + 8 * kStride / 2));
+        const int s = lane & 15, i = 4 * (lane >> 5) + (s >> 2);
+        const int piece = d / 8 + 2 * (lane >> 4 & 1) + (s >> 1 & 1);
+        const uint8_t *p = tile + row * kStride + 8 * (s & 1);
+        const uint8_t *lo = p + i * kStride + (piece ^ swizzle(row % 32 + i)) * 16;
+        const uint8_t *hi = p + (i + 8) * kStride + (piece ^ swizzle(row % 32 + i + 8)) * 16;
+        return cat44(lds_read_tr(reinterpret_cast<const _Float16 *>(lo)),
+                     lds_read_tr(reinterpret_cast<const _Float16 *>(hi)));
     }
 };
+
+// This wave's direct loads have arrived (vmcnt(0); the compiler does not wait for
+// loads that write LDS by itself).
+__device__ __forceinline__ void settle() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
+// The walk over n tiles: fetch(t) starts tile t on its way into buffer t & 1,
+// put(t) takes there what waits in registers; work(t) uses it.  While a tile is
+// worked on the next one arrives.
+template <bool kDirect, typename Fetch, typename Put, typename Work>
+__device__ __forceinline__ void walk_tiles(int n, Fetch fetch, Put put, Work work)
+{
+    if (n > 0) {
+        fetch(0);
+        put(0);
+        if constexpr (!kDirect) fetch(n > 1 ? 1 : 0);
+    }
+    for (int t = 0; t < n; ++t) {
+        if constexpr (kDirect) settle();
+        __syncthreads();  // tile t is there, and nobody reads the other buffer
+        const bool more = t + 1 < n;
+        if constexpr (kDirect) {
+            if (more) fetch(t + 1);
+            work(t);
+            if (more) put(t + 1);
+        } else {
+            if (more) {
+                put(t + 1);
+                fetch(min(t + 2, n - 1));
+            }
+            work(t);
+        }
+    }
+}
 
 // 32 rows of one head as an operand (row row + lane % 32; zeros from `rows` on).
 template <int D>
@@ -145,11 +211,10 @@ template <int D, int kIn>
 __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
     FewArgs a, const DenseItem *items)
 {
-    using TK = ManyTile<D, 16>;
-    using TV = ManyTile<D, 32>;
-    constexpr int kKeys = TK::kRows, kBlocks = kKeys / 32;
-    __shared__ __attribute__((aligned(16))) uint8_t s_k[2][TK::kBytes];
-    __shared__ __attribute__((aligned(16))) uint8_t s_v[2][TV::kBytes];
+    using T = ManyTile<D>;
+    constexpr int kKeys = T::kRows, kBlocks = kKeys / 32;
+    __shared__ __attribute__((aligned(16))) uint8_t s_k[2][T::kBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t s_v[2][T::kBytes];
     const DenseItem it = items[blockIdx.x];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -165,28 +230,26 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
     for (int d = 0; d < D / 32; ++d) o[d] = zero16();
     float m_run = -INFINITY, l_run = 0.f;
 
-    u4 kr[TK::kLoads], vr[TV::kLoads];
-    const int n = (it.others + kKeys - 1) / kKeys;
-    auto load = [&](int t) {
-        TK::load(kr, a.K, it.other, a.n_kv, it.head, kKeys * t, it.others);
-        TV::load(vr, a.V, it.other, a.n_kv, it.head, kKeys * t, it.others);
+    T tk, tv;
+    const uint32_t row_bytes = (uint32_t)a.n_kv * (2 * D);
+    const uint64_t base = (uint64_t)it.other * row_bytes + (uint32_t)it.head * (2 * D);
+    const uint8_t *const K = reinterpret_cast<const uint8_t *>(a.K) + base;
+    const uint8_t *const V = reinterpret_cast<const uint8_t *>(a.V) + base;
+    auto fetch = [&](int t) {
+        // rows behind the range: its last one again (whatever stands there may
+        // not be finite, and 0 times it is added)
+        const int first = kKeys * t, last = it.others - 1 - first;
+        const uint64_t at = (uint64_t)first * row_bytes;
+        auto offset = [&](int row) { return (uint32_t)min(row, last) * row_bytes; };
+        tk.fetch(s_k[t & 1], K + at, offset);
+        tv.fetch(s_v[t & 1], V + at, offset);
     };
-    auto store = [&](int t) {
-        TK::store(s_k[t & 1], kr);
-        TV::store(s_v[t & 1], vr);
+    auto put = [&](int t) {
+        tk.put(s_k[t & 1]);
+        tv.put(s_v[t & 1]);
     };
-    if (n > 0) {
-        load(0);
-        store(0);
-        load(n > 1 ? 1 : 0);
-    }
-    for (int t = 0; t < n; ++t) {
-        __syncthreads();
-        if (t + 1 < n) {
-            store(t + 1);
-            load(min(t + 2, n - 1));
-        }
-        if (!busy) continue;
+    auto work = [&](int t) {
+        if (!busy) return;
         const uint8_t *k = s_k[t & 1], *v = s_v[t & 1];
         f16v s[kBlocks];
 #pragma unroll
@@ -195,7 +258,7 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
         for (int c = 0; c < D / 16; ++c) {
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
-                s[b] = mfma32<kIn>(TK::rows32(k, 32 * b, c, lane), q[c], s[b]);
+                s[b] = mfma32<kIn>(T::rows32(k, 32 * b, c, lane), q[c], s[b]);
         }
         const int left = it.others - kKeys * t;
         if (left < kKeys) {
@@ -231,9 +294,11 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
             const h8 p = pack8<kIn>(s[c >> 1], c & 1);
 #pragma unroll
             for (int d = 0; d < D / 32; ++d)
-                o[d] = mfma32<kIn>(TV::cols32(v, 16 * c, 32 * d, lane), p, o[d]);
+                o[d] = mfma32<kIn>(T::cols32(v, 16 * c, 32 * d, lane), p, o[d]);
         }
-    }
+        products_done();
+    };
+    walk_tiles<T::kDirect>((it.others + kKeys - 1) / kKeys, fetch, put, work);
     const float l = sum_xor32(l_run);
     if (!there) return;
     const int col = 4 * (lane >> 5);
