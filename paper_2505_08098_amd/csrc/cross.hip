@@ -2,26 +2,30 @@
 // ragged batch among workgroups, checks, workspace.
 #include <math.h>
 #include <string.h>
+#include <stdio.h>
+#include <stdlib.h>
 
 #include <new>
 #include <vector>
 
 #include "cross_backward.h"
 #include "cross_few.h"
+#include "dense_division.h"
 
 namespace {
 
 using f3s::DenseItem;
 using f3s::DenseMerge;
+using f3s::Division;
+using f3s::Range;
 using f3s::set_status;
 
-// Workgroups of four waves that fill the GPU (256 compute units).
-constexpr int64_t kFewWorkgroups = 1024;
-constexpr int64_t kManyWorkgroups = 512;
+constexpr int64_t kUnits = 256;  // compute units
+// Workgroups that the kernel of few rows aims at.
+constexpr int64_t kFewWorkgroups = 4 * kUnits;
 // Query rows of a key head up to which a sequence counts as short.
 constexpr int64_t kFewLongest = 32;
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 bool overlaps(const void *a, size_t na, const void *b, size_t nb)
@@ -29,59 +33,6 @@ bool overlaps(const void *a, size_t na, const void *b, size_t nb)
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
     return na && nb && x < y + nb && y < x + na;
 }
-
-// One side of a pass: the rows that get results, in ranges of one sequence,
-// each with the rows of the other side that it walks.
-struct Range {
-    int64_t row, rows, other, others;
-};
-
-// A pass divided into items of `tile` rows and, while that leaves fewer than
-// about `want` workgroups, of parts of the other side (at least `least` rows
-// of it, in multiples of `unit`).
-struct Division {
-    std::vector<DenseItem> items;
-    std::vector<DenseMerge> merges;
-    int64_t parts = 0;
-    int32_t merge_rows = 0;
-
-    void make(const std::vector<Range> &ranges, int32_t heads, int64_t tile, int64_t unit,
-              int64_t least, int64_t want)
-    {
-        int64_t total = 0;
-        for (const Range &r : ranges)
-            total += ceil_div(r.rows, tile) * ceil_div(r.others, unit) * heads;
-        int64_t per = ceil_div(total, want);  // units of an item
-        if (per < ceil_div(least, unit)) per = ceil_div(least, unit);
-        for (const Range &r : ranges) {
-            const int64_t units = ceil_div(r.others, unit);
-            const int64_t n = units <= per ? 1 : ceil_div(units, per);
-            for (int32_t h = 0; h < heads; ++h) {
-                for (int64_t at = 0; at < r.rows; at += tile) {
-                    const int32_t rows = (int32_t)(r.rows - at < tile ? r.rows - at : tile);
-                    const int32_t row = (int32_t)(r.row + at);
-                    if (n > 1) {
-                        merges.push_back({h, row, rows, (int32_t)parts, rows, (int32_t)n, {}});
-                        if (rows > merge_rows) merge_rows = rows;
-                    }
-                    for (int64_t k = 0; k < n; ++k) {
-                        const int64_t b = units * k / n * unit;
-                        int64_t e = units * (k + 1) / n * unit;
-                        if (e > r.others) e = r.others;
-                        items.push_back({h, row, rows, (int32_t)(r.other + b), (int32_t)(e - b),
-                                         n > 1 ? (int32_t)parts : -1, (int32_t)k, 0});
-                        if (n > 1) parts += rows;
-                    }
-                }
-            }
-        }
-    }
-    bool fits() const
-    {
-        return parts <= 0x7FFFFFFF && items.size() <= 0x7FFFFFFF &&
-               (int64_t)merges.size() * merge_rows <= 0x7FFFFFFF;
-    }
-};
 
 f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int32_t *q_len,
                            const int32_t *k_len, int32_t n, int32_t n_heads, int32_t n_kv,
@@ -118,9 +69,10 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
     if (few)
         f.make(fwd, n_kv, f3s::kFewRows, 64, 256, kFewWorkgroups);
     else
-        f.make(fwd, n_kv, f3s::kManyRows, 64, 256, kManyWorkgroups);
-    dq.make(fwd, n_kv, f3s::kManyRows, 64, 256, kManyWorkgroups);
-    dkv.make(keys, n_kv, f3s::kManyRows, 64, 256, kManyWorkgroups);
+        f.make(fwd, n_kv, f3s::kManyRows, 64, 256, kUnits * f3s::many_waves(d));
+    dq.make(fwd, n_kv, f3s::kManyRows, 64, 256, kUnits * f3s::dq_waves(d));
+    dkv.make(keys, n_kv, f3s::kManyRows, 64, 256,
+             kUnits * f3s::dkv_waves(d) / f3s::dkv_halves(d));
     if (!f.fits() || !dq.fits() || !dkv.fits()) return nullptr;
 
     f3s_cross_plan_s *p = new f3s_cross_plan_s;
@@ -167,6 +119,7 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
             *l.dst = (char *)p->store + at;
             at += round256(l.bytes);
         }
+        if (getenv("F3S_DBG")) fprintf(stderr, "fwd %d/%d dq %d/%d dkv %d/%d\n", p->n_fwd, p->n_fwd_merge, p->n_dq, p->n_dq_merge, p->n_dkv, p->n_dkv_merge);
         e = hipMemcpy(p->store, host.data(), bytes, hipMemcpyHostToDevice);
     }
     *st = f3s::status_of(e);

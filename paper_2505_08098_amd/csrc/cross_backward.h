@@ -35,6 +35,8 @@ struct CrossBwdArgs {
     uint32_t flip;     // sign bits: Q is negated in the scores where scale < 0
 };
 
+// Rows of a tile of the other side (64 for short rows: 4 KB to fill at once).
+constexpr int bwd_tile(int d) { return d <= 32 ? 64 : 32; }
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Four columns of a result row from an accumulator.
@@ -61,18 +63,18 @@ __device__ __forceinline__ void store_row(const f16v (&x)[(D1 - D0) / 32], float
         }
 }
 
-constexpr int dq_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
-constexpr int dq_tile(int d) { return d <= 32 || (d > 64 && d <= 128) ? 64 : 32; }
+constexpr int dq_waves(int d) { return d <= 32 ? 4 : d <= 64 ? 3 : d <= 128 ? 2 : 1; }
+constexpr int dkv_halves(int d) { return d <= 128 ? 1 : 2; }
 constexpr int dkv_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
 
 template <int D, int kIn>
 __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwdArgs a,
                                                                         const DenseItem *items)
 {
-    using T = ManyTile<D, dq_tile(D)>;
+    using T = ManyTile<D, bwd_tile(D)>;
     constexpr int kTile = T::kRows;
-    __shared__ __attribute__((aligned(16))) uint8_t s_k[2][T::kBytes];
-    __shared__ __attribute__((aligned(16))) uint8_t s_v[2][T::kBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t s_k0[T::kBytes], s_k1[T::kBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t s_v0[T::kBytes], s_v1[T::kBytes];
     const DenseItem it = items[blockIdx.x];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -86,21 +88,20 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
     const uint64_t base = (uint64_t)it.other * row_bytes + (uint32_t)it.head * (2 * D);
     const uint8_t *const K = reinterpret_cast<const uint8_t *>(a.K) + base;
     const uint8_t *const V = reinterpret_cast<const uint8_t *>(a.V) + base;
-    auto fetch = [&](int t) {
+    auto fetch = [&](int t, auto buf) {
         const int first = kTile * t, last = it.others - 1 - first;
         const uint64_t at = (uint64_t)first * row_bytes;
         // (behind the range: the last row again)
         auto offset = [&](int row) { return (uint32_t)min(row, last) * row_bytes; };
-        tk.fetch(s_k[t & 1], K + at, offset);
-        tv.fetch(s_v[t & 1], V + at, offset);
+        tk.fetch(buf.kIndex ? s_k1 : s_k0, K + at, offset);
+        tv.fetch(buf.kIndex ? s_v1 : s_v0, V + at, offset);
     };
-    auto put = [&](int t) {
-        tk.put(s_k[t & 1]);
-        tv.put(s_v[t & 1]);
+    auto put = [&](int, auto buf) {
+        tk.put(buf.kIndex ? s_k1 : s_k0);
+        tv.put(buf.kIndex ? s_v1 : s_v0);
     };
 
     h8 q[D / 16], g[D / 16];
-    load_rows32<D>(q, a.Q, at, there, a.flip, lane);
     load_rows32<D>(g, a.G, at, there, 0u, lane);
     float delta = 0.f;
     {
@@ -112,20 +113,20 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
             for (int k = 0; k < 8; ++k) delta += from16<kIn>(g[c][k]) * from16<kIn>(o[c][k]);
         delta = sum_xor32(delta);
     }
+    load_rows32<D>(q, a.Q, at, there, a.flip, lane);
     const float lse2 = there ? a.lse[at] * kLog2e : INFINITY;
     if (there && lane < 32 && it.piece == 0) a.stats[at] = float2{lse2, delta};
 
     f16v dq[D / 32];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) dq[d] = zero16();
-    auto work = [&](int t) {
+    auto work = [&](int t, auto buf) {
         if (!busy) return;
-        const uint8_t *k = s_k[t & 1], *v = s_v[t & 1];
+        const uint8_t *k = buf.kIndex ? s_k1 : s_k0, *v = buf.kIndex ? s_v1 : s_v0;
         const int left = it.others - kTile * t;
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
-            // (one block of 32 at a time: two at once do not fit the registers)
-            if (D > 64) __builtin_amdgcn_sched_barrier(0);
+            if (kTile > 32) __builtin_amdgcn_sched_barrier(0);  // (one block at a time)
             f16v s = zero16(), dp = zero16();
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
@@ -153,38 +154,36 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
     walk_tiles<T::kDirect>((it.others + kTile - 1) / kTile, fetch, put, work);
     if (there)
         store_row<D, kIn, 0, D>(dq, a.scale, a.dQ, at,
-                          it.part >= 0 ? a.part_dq + ((int64_t)it.part + mine) * D : nullptr,
-                          lane);
+                                it.part >= 0 ? a.part_dq + ((int64_t)it.part + mine) * D
+                                             : nullptr,
+                                lane);
 }
 
 // d = 96 and 128: the sums of dK and dV leave no room for both K and V beside
 // them if two waves are to share a SIMD, which is worth more (d = 128, 16 heads
 // over 4, 2 x 4,050 x 4,050: @@ us against @@ with one); V's rows stay in LDS.
 constexpr bool dkv_v_in_lds(int d) { return d > 32 && d <= 128; }
-constexpr int dkv_tile(int d) { return d <= 32 ? 64 : 32; }
 
 template <int D>
-struct DkvTiles {
-    using T = ManyTile<D, dkv_tile(D)>;
-    using V = ManyTile<D, kManyRows>;
-    __attribute__((aligned(16))) uint8_t q[2][T::kBytes], g[2][T::kBytes];
-    __attribute__((aligned(16))) uint8_t v[dkv_v_in_lds(D) ? V::kBytes : 16];
-    __attribute__((aligned(16))) float lse[2][T::kRows], delta[2][T::kRows];
+using DkvTile = ManyTile<D, bwd_tile(D)>;
+
+// A tile of query rows and what belongs to it.
+template <int D>
+struct DkvBuffer {
+    __attribute__((aligned(16))) uint8_t q[DkvTile<D>::kBytes], g[DkvTile<D>::kBytes];
+    __attribute__((aligned(16))) float lse[DkvTile<D>::kRows], delta[DkvTile<D>::kRows];
 };
 
 // Columns D0 .. D1 - 1 of dK and dV (all of them up to d = 128; wider rows take
 // two workgroups, each with half of the sums in its registers).
 template <int D, int kIn, int D0, int D1>
 __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem &it,
-                                          DkvTiles<D> &s)
+                                          DkvBuffer<D> &s0, DkvBuffer<D> &s1, uint8_t *s_v)
 {
-    using T = typename DkvTiles<D>::T;
-    using TV = typename DkvTiles<D>::V;
+    using T = DkvTile<D>;
+    using TV = ManyTile<D, kManyRows>;
     constexpr bool kVInLds = dkv_v_in_lds(D);
     constexpr int kTile = T::kRows;
-    auto &s_q = s.q, &s_g = s.g;
-    auto &s_lse = s.lse, &s_delta = s.delta;
-    const uint8_t *const s_v = s.v;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int mine = 32 * wave + (lane & 31);
@@ -194,7 +193,7 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
 
     T tq, tg;
     float2 sr = {0.f, 0.f};
-    auto fetch = [&](int t) {
+    auto fetch = [&](int t, auto buf) {
         // offsets from the first row's token on
         const uint32_t first = (uint32_t)it.other + kTile * t;
         const int last = it.others - 1 - kTile * t;  // (behind it: the last row again)
@@ -205,19 +204,20 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
         };
         const uint64_t at = (uint64_t)token * a.q.n_heads + (uint32_t)(it.head * a.q.g);
         auto bytes = [&](int row) { return offset(row) * (2 * D); };
-        tq.fetch(s_q[t & 1], reinterpret_cast<const uint8_t *>(a.Q) + at * (2 * D), bytes);
-        tg.fetch(s_g[t & 1], reinterpret_cast<const uint8_t *>(a.G) + at * (2 * D), bytes);
-        if (threadIdx.x < kTile) {
-            sr = a.stats[at + offset((int)threadIdx.x)];
-            if ((int)threadIdx.x > last) sr.x = INFINITY;  // (P = 0)
-        }
+        auto &to = buf.kIndex ? s1 : s0;
+        tq.fetch(to.q, reinterpret_cast<const uint8_t *>(a.Q) + at * (2 * D), bytes);
+        tg.fetch(to.g, reinterpret_cast<const uint8_t *>(a.G) + at * (2 * D), bytes);
+        // (by all threads: a load in a branch would be waited for at its end)
+        sr = a.stats[at + offset((int)threadIdx.x % kTile)];
     };
-    auto put = [&](int t) {
-        tq.put(s_q[t & 1]);
-        tg.put(s_g[t & 1]);
+    auto put = [&](int t, auto buf) {
+        auto &to = buf.kIndex ? s1 : s0;
+        tq.put(to.q);
+        tg.put(to.g);
         if (threadIdx.x < kTile) {
-            s_lse[t & 1][threadIdx.x] = sr.x;
-            s_delta[t & 1][threadIdx.x] = sr.y;
+            to.lse[threadIdx.x] =
+                kTile * t + (int)threadIdx.x < it.others ? sr.x : INFINITY;  // (P = 0)
+            to.delta[threadIdx.x] = sr.y;
         }
     };
     h8 k[D / 16], v[kVInLds ? 1 : D / 16];
@@ -226,7 +226,7 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
         for (int f = threadIdx.x; f < kManyRows * TV::kPieces; f += kManyThreads) {
             const int row = f / TV::kPieces, piece = f % TV::kPieces;
             const int64_t r = ((int64_t)it.row + min(row, it.rows - 1)) * a.n_kv + it.head;
-            *reinterpret_cast<u4 *>(s.v + row * TV::kStride +
+            *reinterpret_cast<u4 *>(s_v + row * TV::kStride +
                                     (piece ^ TV::swizzle(row & 31)) * 16) =
                 *reinterpret_cast<const u4 *>(reinterpret_cast<const uint8_t *>(a.V) +
                                               r * (2 * D) + piece * 16);
@@ -238,13 +238,13 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
     f16v dk[kCols], dv[kCols];
 #pragma unroll
     for (int d = 0; d < kCols; ++d) dk[d] = dv[d] = zero16();
-    auto work = [&](int t) {
+    auto work = [&](int t, auto buf) {
         if (!busy) return;
-        const uint8_t *q = s_q[t & 1], *g = s_g[t & 1];
+        const auto &from = buf.kIndex ? s1 : s0;
+        const uint8_t *q = from.q, *g = from.g;
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
-            // (one block of 32 at a time: two at once do not fit the registers)
-            if (kTile > 32) __builtin_amdgcn_sched_barrier(0);
+            if (kTile > 32) __builtin_amdgcn_sched_barrier(0);  // (one block at a time)
             f16v x = zero16(), dp = zero16();
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
@@ -256,8 +256,8 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 32 * b + 8 * r + 4 * (lane >> 5);
-                const f4 l = *reinterpret_cast<const f4 *>(&s_lse[t & 1][row]);
-                const f4 w = *reinterpret_cast<const f4 *>(&s_delta[t & 1][row]);
+                const f4 l = *reinterpret_cast<const f4 *>(&from.lse[row]);
+                const f4 w = *reinterpret_cast<const f4 *>(&from.delta[row]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float y =
@@ -290,16 +290,18 @@ template <int D, int kIn>
 __global__ __launch_bounds__(kManyThreads, dkv_waves(D)) void k_cross_dkv(
     CrossBwdArgs a, const DenseItem *items)
 {
-    __shared__ DkvTiles<D> tiles;
-    const DenseItem it = items[D <= 128 ? blockIdx.x : blockIdx.x >> 1];
-    if constexpr (D <= 128) {
-        cross_dkv<D, kIn, 0, D>(a, it, tiles);
+    __shared__ DkvBuffer<D> s0, s1;
+    __shared__ __attribute__((aligned(16)))
+    uint8_t s_v[dkv_v_in_lds(D) ? ManyTile<D, kManyRows>::kBytes : 16];
+    const DenseItem it = items[blockIdx.x / dkv_halves(D)];
+    if constexpr (dkv_halves(D) == 1) {
+        cross_dkv<D, kIn, 0, D>(a, it, s0, s1, s_v);
     } else {
         constexpr int kHalf = (D / 2 + 31) / 32 * 32;
         if (blockIdx.x & 1)
-            cross_dkv<D, kIn, kHalf, D>(a, it, tiles);
+            cross_dkv<D, kIn, kHalf, D>(a, it, s0, s1, s_v);
         else
-            cross_dkv<D, kIn, 0, kHalf>(a, it, tiles);
+            cross_dkv<D, kIn, 0, kHalf>(a, it, s0, s1, s_v);
     }
 }
 
@@ -343,7 +345,7 @@ hipError_t launch_cross_backward_d(const f3s_cross_plan_s &p, const CrossBwdArgs
     constexpr int kPer = 256 / (D / 4);
     if (p.n_dq) k_cross_dq<D, kIn><<<p.n_dq, kManyThreads, 0, s>>>(a, p.dq);
     if (p.n_dkv)
-        k_cross_dkv<D, kIn><<<(unsigned)(D <= 128 ? p.n_dkv : 2 * p.n_dkv), kManyThreads, 0, s>>>(
+        k_cross_dkv<D, kIn><<<(unsigned)(p.n_dkv * dkv_halves(D)), kManyThreads, 0, s>>>(
             a, p.dkv);
     if (p.n_dq_merge) {
         const int blocks = (p.dq_merge_rows + kPer - 1) / kPer;

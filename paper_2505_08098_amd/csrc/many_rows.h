@@ -143,32 +143,44 @@ struct ManyTile {
 // loads that write LDS by itself).
 __device__ __forceinline__ void settle() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
-// The walk over n tiles: fetch(t) starts tile t on its way into buffer t & 1,
-// put(t) takes there what waits in registers; work(t) uses it.  While a tile is
-// worked on the next one arrives.
+// The walk over n tiles, in two buffers: fetch(t, b) starts tile t on its way
+// into buffer b, put(t, b) takes there what waits in registers, work(t, b) uses
+// it.  While a tile is worked on the next one arrives.  The buffer is a type
+// (Buffer<0>, Buffer<1>) and each has LDS variables of its own: where they were
+// one array, the compiler held a transposed read to depend on the loads into
+// the other half and waited for them (dK and dV of pairs of 4,050, 16 heads of
+// 128 over 4: @@ us instead of @@).
+template <int B>
+struct Buffer {
+    static constexpr int kIndex = B;
+};
 template <bool kDirect, typename Fetch, typename Put, typename Work>
 __device__ __forceinline__ void walk_tiles(int n, Fetch fetch, Put put, Work work)
 {
-    if (n > 0) {
-        fetch(0);
-        put(0);
-        if constexpr (!kDirect) fetch(n > 1 ? 1 : 0);
-    }
-    for (int t = 0; t < n; ++t) {
+    auto step = [&](int t, auto here, auto there) {
         if constexpr (kDirect) settle();
         __syncthreads();  // tile t is there, and nobody reads the other buffer
         const bool more = t + 1 < n;
         if constexpr (kDirect) {
-            if (more) fetch(t + 1);
-            work(t);
-            if (more) put(t + 1);
+            if (more) fetch(t + 1, there);
+            work(t, here);
+            if (more) put(t + 1, there);
         } else {
             if (more) {
-                put(t + 1);
-                fetch(min(t + 2, n - 1));
+                put(t + 1, there);
+                fetch(min(t + 2, n - 1), here);
             }
-            work(t);
+            work(t, here);
         }
+    };
+    if (n > 0) {
+        fetch(0, Buffer<0>());
+        put(0, Buffer<0>());
+        if constexpr (!kDirect) fetch(n > 1 ? 1 : 0, Buffer<1>());
+    }
+    for (int t = 0; t < n; t += 2) {
+        step(t, Buffer<0>(), Buffer<1>());
+        if (t + 1 < n) step(t + 1, Buffer<1>(), Buffer<0>());
     }
 }
 
@@ -213,8 +225,8 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
 {
     using T = ManyTile<D>;
     constexpr int kKeys = T::kRows, kBlocks = kKeys / 32;
-    __shared__ __attribute__((aligned(16))) uint8_t s_k[2][T::kBytes];
-    __shared__ __attribute__((aligned(16))) uint8_t s_v[2][T::kBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t s_k0[T::kBytes], s_k1[T::kBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t s_v0[T::kBytes], s_v1[T::kBytes];
     const DenseItem it = items[blockIdx.x];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -235,30 +247,30 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
     const uint64_t base = (uint64_t)it.other * row_bytes + (uint32_t)it.head * (2 * D);
     const uint8_t *const K = reinterpret_cast<const uint8_t *>(a.K) + base;
     const uint8_t *const V = reinterpret_cast<const uint8_t *>(a.V) + base;
-    auto fetch = [&](int t) {
+    auto fetch = [&](int t, auto b) {
         // rows behind the range: its last one again (whatever stands there may
         // not be finite, and 0 times it is added)
         const int first = kKeys * t, last = it.others - 1 - first;
         const uint64_t at = (uint64_t)first * row_bytes;
         auto offset = [&](int row) { return (uint32_t)min(row, last) * row_bytes; };
-        tk.fetch(s_k[t & 1], K + at, offset);
-        tv.fetch(s_v[t & 1], V + at, offset);
+        tk.fetch(b.kIndex ? s_k1 : s_k0, K + at, offset);
+        tv.fetch(b.kIndex ? s_v1 : s_v0, V + at, offset);
     };
-    auto put = [&](int t) {
-        tk.put(s_k[t & 1]);
-        tv.put(s_v[t & 1]);
+    auto put = [&](int, auto b) {
+        tk.put(b.kIndex ? s_k1 : s_k0);
+        tv.put(b.kIndex ? s_v1 : s_v0);
     };
-    auto work = [&](int t) {
+    auto work = [&](int t, auto b) {
         if (!busy) return;
-        const uint8_t *k = s_k[t & 1], *v = s_v[t & 1];
+        const uint8_t *k = b.kIndex ? s_k1 : s_k0, *v = b.kIndex ? s_v1 : s_v0;
         f16v s[kBlocks];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) s[b] = zero16();
+        for (int h = 0; h < kBlocks; ++h) s[h] = zero16();
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-                s[b] = mfma32<kIn>(T::rows32(k, 32 * b, c, lane), q[c], s[b]);
+            for (int h = 0; h < kBlocks; ++h)
+                s[h] = mfma32<kIn>(T::rows32(k, 32 * h, c, lane), q[c], s[h]);
         }
         const int left = it.others - kKeys * t;
         if (left < kKeys) {
