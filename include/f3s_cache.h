@@ -89,7 +89,9 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
  *              overlap in time need one each.  NULL if that is 0
  * Inputs must be finite.  The work is divided on the device, by the lengths
  * that it finds there: a captured call stays right when they change.  A prefix
- * is read once for many sequences.  Deterministic.  Asynchronous on `stream`;
+ * is read once for many sequences: for 16 query rows of a key head at a time,
+ * or, with many rows and much work, for 128 (environment F3S_PREFIX_ROWS=16 or
+ * 128 forces one).  Deterministic.  Asynchronous on `stream`;
  * no allocation, no synchronisation.
  */
 f3s_status_t f3s_cache_attend(const f3s_cache_t *cache, const void *Q, f3s_dtype_t dtype,

@@ -31,6 +31,9 @@ typedef struct f3s_cross_plan_s *f3s_cross_plan_t;
  *   n_heads        query heads, a multiple of n_kv_heads >= 1, at most 65535
  *                  (else F3S_ERR_UNSUPPORTED)
  *   d              multiple of 32, 32 <= d <= 256 (else F3S_ERR_UNSUPPORTED)
+ * The forward takes 16 query rows of a key head to a workgroup where no
+ * sequence has more than 8 (single tokens), else 128 (environment
+ * F3S_CROSS_ROWS=16 or 128, read here, forces one).
  * The plan copies what it needs.  Synchronous on the current device's null
  * stream.  NULL on error (f3s_last_error); F3S_ERR_TOO_LARGE if the batch
  * has 2^31 or more query rows per key head or work items.

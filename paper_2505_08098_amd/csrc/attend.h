@@ -23,7 +23,8 @@ struct AttendArgs {
     int32_t own_items;     // workgroups per key head and row block: share + n_seqs
     bool direct;           // one workgroup has all keys: no partial results
     // the prefix, all sequences' rows together
-    int32_t prefix_blocks;  // row blocks of a key head
+    bool prefix_many;       // by the kernel of many rows
+    int32_t prefix_blocks;  // row blocks (of 16, or 128) of a key head
     int32_t prefix_splits, prefix_chunk;
     int64_t prefix_part;   // first partial row
     int2 *desc;            // per sequence: its first item and their number
@@ -106,11 +107,11 @@ __device__ __forceinline__ OwnItem own_item(const AttendArgs &a, int i)
 }
 
 template <int D, int kIn>
-__global__ __launch_bounds__(64 * kFewWaves) void k_attend(AttendArgs a)
+__global__ __launch_bounds__(64 * kFewWaves, few_waves(D, true)) void k_attend(AttendArgs a)
 {
     FewItem it = {};
     int wg = (int)blockIdx.x;
-    const int n_prefix = a.prefix_splits * a.few.n_kv * a.prefix_blocks;
+    const int n_prefix = a.prefix_many ? 0 : a.prefix_splits * a.few.n_kv * a.prefix_blocks;
     if (wg < n_prefix) {
         const int rb = wg % a.prefix_blocks, sh = wg / a.prefix_blocks;
         it.head = sh % a.few.n_kv;
@@ -149,59 +150,50 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attend(AttendArgs a)
     few_rows<D, kIn, true>(a.few, it);
 }
 
-// Final results of every row from its partial ones: D / 4 threads to a row.
-template <int D, int kIn>
-__global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a)
+// Final results of every row from its partial ones.
+template <int D, int kIn, bool kSplit>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a)
 {
-    constexpr int kPer = 256 / (D / 4);  // rows of a workgroup
-    const int64_t out = (int64_t)blockIdx.x * kPer + threadIdx.x / (D / 4);
-    const int c = threadIdx.x % (D / 4) * 4;
+    constexpr int kPer = kSplit ? 1 : 256 / (D / 4);  // rows of a workgroup
+    const int64_t out =
+        (int64_t)blockIdx.x * kPer + (kSplit ? 0 : (int)threadIdx.x / (D / 4));
     const int64_t all = (int64_t)a.rows * a.n_seqs;  // of a key head
-    if (threadIdx.x >= kPer * (D / 4) || out >= all * a.few.n_kv) return;
+    if (!kSplit && ((int)threadIdx.x >= kPer * (D / 4) || out >= all * a.few.n_kv)) return;
     const int64_t token = out / a.few.q.n_heads;
     const int h = (int)(out - token * a.few.q.n_heads), kh = h / a.few.q.g;
     const int64_t r = token * a.few.q.g + (h - kh * a.few.q.g);
     const int b = (int)(token / a.n_new);
     const int2 d = a.desc[b];
-    float m = -INFINITY, l = 0.f;
-    f4 o = f4{0.f, 0.f, 0.f, 0.f};
-    merge_pieces<D>(a.few.part_o, a.few.part_ml,
-                    ((int64_t)d.x * a.few.n_kv + kh) * a.rows + (r - (int64_t)b * a.rows),
-                    (int64_t)a.few.n_kv * a.rows, d.y, c, m, l, o);
-    if (a.prefix_splits)
-        merge_pieces<D>(a.few.part_o, a.few.part_ml, a.prefix_part + kh * all + r,
-                        a.few.n_kv * all, a.prefix_splits, c, m, l, o);
-    store4<kIn>(a.few.O, out * D + c, o * (l == 0.f ? 0.f : 1.f / l));
-    if (c == 0) a.few.lse[out] = natural_lse(m, l);
+    const PartRows own = {((int64_t)d.x * a.few.n_kv + kh) * a.rows + (r - (int64_t)b * a.rows),
+                          (int64_t)a.few.n_kv * a.rows, d.y};
+    const PartRows prefix = {a.prefix_part + kh * all + r, a.few.n_kv * all, a.prefix_splits};
+    join_row<D, kIn, kSplit>(a.few.part_o, a.few.part_ml, own, prefix, out, a.few.O, a.few.lse);
 }
+
+template <int D, int kIn>
+hipError_t launch_attend_prefix_d(const AttendArgs &a, hipStream_t s);
 
 template <int D, int kIn>
 hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s)
 {
-    const int64_t grid = (int64_t)a.prefix_splits * a.few.n_kv * a.prefix_blocks +
-                         (int64_t)a.own_items * a.few.n_kv * a.row_blocks;
+    int64_t grid = (int64_t)a.own_items * a.few.n_kv * a.row_blocks;
+    if (a.prefix_many) {
+        const hipError_t e = launch_attend_prefix_d<D, kIn>(a, s);
+        if (e != hipSuccess) return e;
+    } else {
+        grid += (int64_t)a.prefix_splits * a.few.n_kv * a.prefix_blocks;
+    }
     k_attend<D, kIn><<<(unsigned)grid, 64 * kFewWaves, 0, s>>>(a);
     if (!a.direct) {
         constexpr int kPer = 256 / (D / 4);
         const int64_t rows = (int64_t)a.rows * a.n_seqs * a.few.n_kv;
-        k_attend_merge<D, kIn><<<(unsigned)((rows + kPer - 1) / kPer), 256, 0, s>>>(a);
+        if (rows <= kSplitJoins)
+            k_attend_join<D, kIn, true><<<(unsigned)rows, 256, 0, s>>>(a);
+        else
+            k_attend_join<D, kIn, false>
+                <<<(unsigned)((rows + kPer - 1) / kPer), 256, 0, s>>>(a);
     }
     return hipGetLastError();
-}
-
-template <int kIn>
-hipError_t launch_attend_type(const AttendArgs &a, int d, hipStream_t s)
-{
-    switch (d) {
-    case 32: return launch_attend_d<32, kIn>(a, s);
-    case 64: return launch_attend_d<64, kIn>(a, s);
-    case 96: return launch_attend_d<96, kIn>(a, s);
-    case 128: return launch_attend_d<128, kIn>(a, s);
-    case 160: return launch_attend_d<160, kIn>(a, s);
-    case 192: return launch_attend_d<192, kIn>(a, s);
-    case 224: return launch_attend_d<224, kIn>(a, s);
-    default: return launch_attend_d<256, kIn>(a, s);
-    }
 }
 
 hipError_t launch_attend_f16(const AttendArgs &a, int d, hipStream_t s);

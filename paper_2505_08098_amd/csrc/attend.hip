@@ -1,7 +1,8 @@
 // f3s_cache_attend: checks, the division of the work, workspace.
 #include <math.h>
+#include <stdlib.h>
 
-#include "attend.h"
+#include "attend_many.h"
 
 namespace f3s {
 f3s_status_t check_cache(const f3s_cache_t *c);
@@ -11,9 +12,20 @@ namespace {
 
 using f3s::AttendArgs;
 
-// Workgroups that a pass over the keys aims at: 256 compute units with four
-// workgroups of four waves each.
-constexpr int64_t kWorkgroups = 1024;
+constexpr int64_t kUnits = 256;  // compute units
+// Workgroups that the kernel of few rows aims at, two or three rounds of them, so
+// that what is left at the end is short.
+constexpr int64_t kWorkgroups = 8 * kUnits;
+// The prefix takes the kernel of many rows from more than this many query rows
+// of a key head on (below, its tiles would be half empty), and from so many
+// operations that its higher rate pays for a launch of its own (whole calls,
+// 8 key heads of 128: 128 rows and 16,384 keys, 8.6 G, 44.5 us instead of 53.4;
+// 256 rows and 4,096 keys, 4.3 G, 38.5 instead of 37.0).
+constexpr int64_t kFewPrefixRows = 64;
+constexpr double kManyWork = 6e9;
+// What a piece of the prefix costs beside its keys (queries, partial results),
+// in units of 64 keys.
+constexpr int64_t kPieceCost = 3;
 
 constexpr size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 
@@ -26,8 +38,9 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Everything of the arguments that follows from the sizes; false if a size is
 // beyond what the kernels count with.
+// prefix_rows: 16 or 128 query rows to a workgroup of the prefix, 0: by the rule.
 bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_new,
-            int32_t n_heads, int32_t prefix_len, AttendArgs *a, Layout *w)
+            int32_t n_heads, int32_t prefix_len, int prefix_rows, AttendArgs *a, Layout *w)
 {
     const int64_t g = n_heads / c.n_kv_heads;
     const int64_t rows = n_new * g, all = rows * n_seqs;
@@ -51,12 +64,39 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     a->share = (int32_t)share;
     a->own_items = a->direct || cap_units <= f3s::kLeastUnits ? n_seqs
                                                               : (int32_t)(share + n_seqs);
-    a->prefix_blocks = (int32_t)ceil_div(all, f3s::kFewRows);
+    if (prefix_rows)
+        a->prefix_many = prefix_rows == f3s::kManyRows;
+    else
+        a->prefix_many = all > kFewPrefixRows &&
+                         4.0 * (double)all * prefix_len * c.d * c.n_kv_heads > kManyWork;
+    a->prefix_many = a->prefix_many && prefix_len;
+    a->prefix_blocks =
+        (int32_t)ceil_div(all, a->prefix_many ? f3s::kManyRows : f3s::kFewRows);
     a->prefix_splits = a->prefix_chunk = 0;
     if (prefix_len) {
         const int64_t units = ceil_div(prefix_len, f3s::kUnit);
-        const int64_t want = ceil_div(kWorkgroups, (int64_t)c.n_kv_heads * a->prefix_blocks);
-        const int64_t per = f3s::units_per_item(units, (int32_t)want);
+        const int64_t one = (int64_t)c.n_kv_heads * a->prefix_blocks;  // workgroups, unsplit
+        int64_t per;
+        if (a->prefix_many) {
+            // pieces that fill their rounds, at most kMostChunk keys each
+            const int64_t slots = kUnits * f3s::many_waves(c.d);
+            double best = INFINITY;
+            per = units;
+            for (int64_t n = 1; n <= units; ++n) {
+                const int64_t p = ceil_div(units, n);
+                if (n > 1 && p < f3s::kLeastUnits) break;
+                if (p * f3s::kUnit > f3s::kMostChunk) continue;
+                const double t = (double)ceil_div(one * ceil_div(units, p), slots) *
+                                 (double)(p + kPieceCost);
+                if (t < best) {
+                    best = t;
+                    per = p;
+                }
+                if (one * n > 4 * slots) break;
+            }
+        } else {
+            per = f3s::units_per_item(units, (int32_t)ceil_div(kWorkgroups, one));
+        }
         a->prefix_chunk = (int32_t)(per * f3s::kUnit);
         a->prefix_splits = (int32_t)ceil_div(units, per);
     }
@@ -98,12 +138,19 @@ size_t f3s_cache_attend_workspace_bytes(const f3s_cache_t *cache, int32_t max_pa
                                         int32_t n_seqs, int32_t n_new, int32_t n_heads,
                                         int32_t prefix_len)
 {
-    AttendArgs a = {};
-    Layout w;
     if (!sizes_ok(cache, max_pages, n_seqs, n_new, n_heads, prefix_len) || n_seqs == 0 ||
-        n_new == 0 || !divide(*cache, max_pages, n_seqs, n_new, n_heads, prefix_len, &a, &w))
+        n_new == 0)
         return 0;
-    return w.bytes;
+    // (enough for both kernels of the prefix)
+    size_t most = 0;
+    for (int rows : {f3s::kFewRows, f3s::kManyRows}) {
+        AttendArgs a = {};
+        Layout w;
+        if (!divide(*cache, max_pages, n_seqs, n_new, n_heads, prefix_len, rows, &a, &w))
+            return 0;
+        if (w.bytes > most) most = w.bytes;
+    }
+    return most;
 }
 
 f3s_status_t f3s_cache_attend(const f3s_cache_t *cache, const void *Q, f3s_dtype_t dtype,
@@ -126,7 +173,9 @@ f3s_status_t f3s_cache_attend(const f3s_cache_t *cache, const void *Q, f3s_dtype
         return set_status(F3S_ERR_INVALID_VALUE);
     AttendArgs a = {};
     Layout w;
-    if (!divide(*cache, max_pages, n_seqs, n_new, n_heads, prefix_len, &a, &w))
+    const char *rows = getenv("F3S_PREFIX_ROWS");
+    if (!divide(*cache, max_pages, n_seqs, n_new, n_heads, prefix_len,
+                rows && *rows ? atoi(rows) : 0, &a, &w))
         return set_status(F3S_ERR_TOO_LARGE);
     if (w.bytes && (!workspace || !aligned(workspace, 256) || workspace_bytes < w.bytes))
         return set_status(F3S_ERR_INVALID_VALUE);

@@ -1,0 +1,269 @@
+// Attention of many query rows to the shared prefix of the 8-bit cache (the
+// first of f3s_cache_attend's passes where the batch has more than a few rows).
+//
+// The kernel of many_rows.h with another way into LDS: a tile's codes wait in
+// registers and are widened as they are stored, once for the 128 rows of the
+// workgroup, K to the queries' type and V to f16 (every code is exact in both).
+// A key's power of two multiplies its scores, a value's its probabilities,
+// relative to the tile's largest power and that to the largest so far, so that
+// P V runs in f16 whatever the values' size.
+#pragma once
+
+#include "attend.h"
+#include "many_rows.h"
+
+namespace f3s {
+
+// Keys that one workgroup walks at most: its pages' numbers wait in LDS.
+constexpr int kMostChunk = 4096;
+
+// Keys of a tile (the codes on their way leave no room for 64 of 128 values).
+constexpr int code_keys(int d) { return d <= 128 ? 64 : 32; }
+constexpr int code_sets(int d) { return code_keys(d) == 64 ? 1 : 2; }
+constexpr int prefix_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
+
+// One of the two buffers of a tile of cached keys.
+template <int D>
+struct CodeTile {
+    using T = ManyTile<D, code_keys(D)>;
+    __attribute__((aligned(16))) uint8_t k[T::kBytes], v[T::kBytes];
+    __attribute__((aligned(16))) float ck[T::kRows];  // power of a key, times |scale| log2 e
+    __attribute__((aligned(16))) float fv[T::kRows];  // power of a value / the tile's largest
+    uint32_t there[2];  // keys that are there, a bit each
+    int32_t top;        // the tile's largest power
+};
+
+// Largest of a wave's numbers, by lane moves of the vector unit (through LDS they
+// would hold up the wave that every other one waits for).
+__device__ __forceinline__ int wave_max(int v)
+{
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x121, 0xF, 0xF, false));  // row_ror:1
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x122, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x124, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x128, 0xF, 0xF, false));
+    auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((int)r[0], (int)r[1]);
+    r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max((int)r[0], (int)r[1]);
+}
+
+template <int D, int kIn>
+__global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix(AttendArgs a)
+{
+    using T = ManyTile<D, code_keys(D)>;
+    constexpr int kKeys = T::kRows, kBlocks = kKeys / 32;
+    constexpr int kCodes = D / 16;  // 16-byte pieces of a row of codes
+    constexpr int kLoads = (kKeys * kCodes + kManyThreads - 1) / kManyThreads;
+    constexpr bool kEven = kKeys * kCodes % kManyThreads == 0;
+    __shared__ CodeTile<D> s0, s1;
+    __shared__ int32_t s_pages[kMostChunk / 16];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int tile = (int)blockIdx.x % a.prefix_blocks, sh = (int)blockIdx.x / a.prefix_blocks;
+    const int head = sh % a.few.n_kv, split = sh / a.few.n_kv;
+    const int64_t all = (int64_t)a.rows * a.n_seqs;  // rows of the key head
+    const int rows = (int)(all - (int64_t)tile * kManyRows < kManyRows
+                               ? all - (int64_t)tile * kManyRows : kManyRows);
+    const int begin = split * a.prefix_chunk, end = min(a.prefix_len, begin + a.prefix_chunk);
+    const int shift = a.few.page_shift;
+    const int mine = 32 * wave + (lane & 31);
+    const bool there = mine < rows;
+    const bool busy = 32 * wave < rows;
+
+    const int page0 = begin >> shift;
+    for (int i = threadIdx.x; i < ((end - 1) >> shift) - page0 + 1; i += kManyThreads)
+        s_pages[i] = a.prefix[page0 + i];
+    __syncthreads();
+
+    h8 q[D / 16];
+    load_rows32<D>(q, a.few.Q,
+                   query_row(a.few.q, head, (int64_t)tile * kManyRows + (there ? mine : 0)),
+                   there, a.few.flip, lane);
+    f16v o[D / 32];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = zero16();
+    float m_run = -INFINITY, l_run = 0.f;
+    int ref = 0;  // o holds multiples of 2^(ref - 127)
+
+    // Two tiles are on their way at a time: one would have to come within the time
+    // that another is worked on (@@ us instead of @@ for 16,384 keys and 512
+    // rows of 128 per key head, 8 key heads).
+    constexpr int kSets = code_sets(D);
+    u4 kr[kSets][kLoads], vr[kSets][kLoads];
+    int ke[2] = {0, 0}, ve[2] = {0, 0};
+    bool ok[2] = {false, false};   // of the key that this thread looks after
+    uint32_t missing[2] = {0, 0};  // of its pieces
+    // Row of the cache of a key of the range, or -1.
+    auto place = [&](int key) -> int64_t {
+        if (key >= end) return -1;
+        const int page = s_pages[(key >> shift) - page0];
+        if (page < 0 || page >= a.few.n_pages) return -1;
+        return (((int64_t)page * a.few.n_kv + head) << shift) + (key & ((1 << shift) - 1));
+    };
+    auto fetch = [&](int t, auto b) {
+        constexpr int w = kSets > 1 ? decltype(b)::kIndex : 0;
+        const int first = begin + kKeys * t;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int f = (int)threadIdx.x + kManyThreads * j;
+            const int row = kEven ? f / kCodes : min(f / kCodes, kKeys - 1);
+            // (a key that is not there reads the cache's first row, and is left out)
+            const int64_t r = place(first + row);
+            const int64_t at = (r < 0 ? 0 : r) * D + f % kCodes * 16;
+            kr[w][j] = *reinterpret_cast<const u4 *>(a.few.k + at);
+            vr[w][j] = *reinterpret_cast<const u4 *>(a.few.v + at);
+            missing[w] = (j ? missing[w] : 0u) | (r < 0 ? 1u << j : 0u);
+        }
+        const int64_t r = place(first + (int)threadIdx.x % kKeys);
+        ok[w] = r >= 0;
+        ke[w] = a.few.k_exp[r < 0 ? 0 : r];
+        ve[w] = a.few.v_exp[r < 0 ? 0 : r];
+    };
+    auto put = [&](auto b) {
+        constexpr int w = kSets > 1 ? decltype(b)::kIndex : 0;
+        CodeTile<D> &to = b.kIndex ? s1 : s0;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int f = (int)threadIdx.x + kManyThreads * j, row = f / kCodes;
+            if (!kEven && row >= kKeys) continue;
+            const int c = f % kCodes, sw = T::swizzle(row & 31);
+            // (a value that is left out has to be finite: 0 times it is added)
+            if (missing[w] >> j & 1) vr[w][j] = u4{0, 0, 0, 0};
+            const u2 klo = {kr[w][j][0], kr[w][j][1]}, khi = {kr[w][j][2], kr[w][j][3]};
+            const u2 vlo = {vr[w][j][0], vr[w][j][1]}, vhi = {vr[w][j][2], vr[w][j][3]};
+            uint8_t *pk = to.k + row * T::kStride, *pv = to.v + row * T::kStride;
+            *reinterpret_cast<h8 *>(pk + ((2 * c) ^ sw) * 16) = codes_to<kIn>(klo);
+            *reinterpret_cast<h8 *>(pk + ((2 * c + 1) ^ sw) * 16) = codes_to<kIn>(khi);
+            *reinterpret_cast<h8 *>(pv + ((2 * c) ^ sw) * 16) = codes_to<kInF16>(vlo);
+            *reinterpret_cast<h8 *>(pv + ((2 * c + 1) ^ sw) * 16) = codes_to<kInF16>(vhi);
+        }
+        if (threadIdx.x < 64) {  // (of 32 keys: twice the same)
+            const int power = ok[w] ? ve[w] : 0, top = wave_max(power);
+            const uint64_t mask = __ballot(ok[w]);
+            if ((int)threadIdx.x < kKeys) {
+                to.ck[threadIdx.x] = fminf(__builtin_ldexpf(a.few.sl2, ke[w] - 127), 0x1.fffffep127f);
+                to.fv[threadIdx.x] = __builtin_ldexpf(1.f, power - top);
+            }
+            if (threadIdx.x == 0) {
+                to.there[0] = (uint32_t)mask;
+                to.there[1] = (uint32_t)(mask >> 32);
+                to.top = top;
+            }
+        }
+    };
+    auto work = [&](auto b) {
+        if (!busy) return;
+        const CodeTile<D> &from = b.kIndex ? s1 : s0;
+        f16v s[kBlocks];
+#pragma unroll
+        for (int h = 0; h < kBlocks; ++h) s[h] = zero16();
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+#pragma unroll
+            for (int h = 0; h < kBlocks; ++h)
+                s[h] = mfma32<kIn>(T::rows32(from.k, 32 * h, c, lane), q[c], s[h]);
+        }
+#pragma unroll
+        for (int r = 0; r < 4 * kBlocks; ++r) {
+            const f4 c = *reinterpret_cast<const f4 *>(&from.ck[8 * r + 4 * (lane >> 5)]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[r >> 2][4 * (r & 3) + e] *= c[e];
+        }
+        const uint32_t all_there = from.there[0] & (kBlocks > 1 ? from.there[1] : ~0u);
+        if (__builtin_amdgcn_readfirstlane(all_there) != ~0u) {
+#pragma unroll
+            for (int h = 0; h < kBlocks; ++h) {
+                const uint32_t mask = from.there[h] >> (4 * (lane >> 5));
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!(mask >> (8 * (e >> 2) + (e & 3)) & 1)) s[h][e] = -INFINITY;
+            }
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 16 * kBlocks; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
+        mx = max_xor32(mx);
+        const float m_new = fmaxf(m_run, mx);
+        const int top = __builtin_amdgcn_readfirstlane(from.top);
+        // (a maximum that has grown by less than 2^6 is not worth the products: the
+        // probabilities may as well be up to 64, in f16 with the same 11 bits)
+        if (__ballot(m_new > m_run + 6.f) || top > ref) {
+            float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+            l_run *= alpha;
+            alpha = __builtin_ldexpf(alpha, ref - max(top, ref));
+            ref = max(top, ref);
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) o[d] *= alpha;
+            m_run = m_new;
+        }
+        const float m_ref = m_run == -INFINITY ? 0.f : m_run;
+        const float less = __builtin_ldexpf(1.f, top - ref);
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4 * kBlocks; ++r) {
+            f4 f = *reinterpret_cast<const f4 *>(&from.fv[8 * r + 4 * (lane >> 5)]);
+            if (top < ref) f *= less;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 4 * (r & 3) + e;
+                const float p = __builtin_amdgcn_exp2f(s[r >> 2][i] - m_ref);
+                sum += p;
+                s[r >> 2][i] = p * f[e];
+            }
+        }
+        l_run += sum;
+#pragma unroll
+        for (int c = 0; c < 2 * kBlocks; ++c) {
+            const h8 p = pack8<kInF16>(s[c >> 1], c & 1);
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+                o[d] = mfma32<kInF16>(T::cols32(from.v, 16 * c, 32 * d, lane), p, o[d]);
+        }
+        products_done();
+    };
+    const int n = (end - begin + kKeys - 1) / kKeys;
+    auto step = [&](int t, auto here, auto next) {
+        __syncthreads();  // tile t is there, and nobody reads the other buffer
+        if (t + 1 < n) {
+            put(next);
+            fetch(min(t + 1 + kSets, n - 1), next);
+        }
+        work(here);
+    };
+    fetch(0, Buffer<0>());
+    if (kSets > 1) fetch(min(1, n - 1), Buffer<1>());
+    put(Buffer<0>());
+    fetch(min(kSets, n - 1), Buffer<0>());
+    for (int t = 0; t < n; t += 2) {
+        step(t, Buffer<0>(), Buffer<1>());
+        if (t + 1 < n) step(t + 1, Buffer<1>(), Buffer<0>());
+    }
+
+    const float l = sum_xor32(l_run);
+    if (!there) return;
+    const int64_t part = a.prefix_part + ((int64_t)split * a.few.n_kv + head) * all +
+                         (int64_t)tile * kManyRows + mine;
+    const int col = 4 * (lane >> 5);
+    float *to = a.few.part_o + part * D + col;
+    const float power = __builtin_ldexpf(1.f, ref - 127);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<f4 *>(to + 32 * d + 8 * k) =
+                f4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * power;
+    if (col == 0) {
+        a.few.part_ml[2 * part] = m_run;
+        a.few.part_ml[2 * part + 1] = l;
+    }
+}
+
+template <int D, int kIn>
+hipError_t launch_attend_prefix_d(const AttendArgs &a, hipStream_t s)
+{
+    const int64_t grid = (int64_t)a.prefix_splits * a.few.n_kv * a.prefix_blocks;
+    k_attend_prefix<D, kIn><<<(unsigned)grid, kManyThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace f3s

@@ -1,9 +1,8 @@
 // f3s_cross_plan, f3s_cross_forward, f3s_cross_backward: the division of a
 // ragged batch among workgroups, checks, workspace.
 #include <math.h>
-#include <string.h>
-#include <stdio.h>
 #include <stdlib.h>
+#include <string.h>
 
 #include <new>
 #include <vector>
@@ -23,8 +22,11 @@ using f3s::set_status;
 constexpr int64_t kUnits = 256;  // compute units
 // Workgroups that the kernel of few rows aims at.
 constexpr int64_t kFewWorkgroups = 4 * kUnits;
-// Query rows of a key head up to which a sequence counts as short.
-constexpr int64_t kFewLongest = 32;
+// Query rows of a key head up to which the forward takes the kernel of few rows:
+// one sequence's row over 100 keys takes 2.7 us with it and 3.8 with the other, 4
+// over 8,192 keys 8.6 and 10.8; 16 rows of 16 sequences over 2,048 keys 28.9 and
+// 26.7 (8 key heads of 128 in the last two).
+constexpr int64_t kFewLongest = 8;
 
 size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -65,7 +67,9 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
     if (q_ptr[n] * g > 0x7FFFFFFF || (double)q_ptr[n] * n_heads / 16 + n_heads > 2147483647.0)
         return nullptr;
     Division f, dq, dkv;
-    const bool few = longest <= kFewLongest;
+    const char *rows_env = getenv("F3S_CROSS_ROWS");
+    const bool few = rows_env && *rows_env ? atoi(rows_env) == f3s::kFewRows
+                                           : longest <= kFewLongest;
     if (few)
         f.make(fwd, n_kv, f3s::kFewRows, 64, 256, kFewWorkgroups);
     else
@@ -119,7 +123,6 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
             *l.dst = (char *)p->store + at;
             at += round256(l.bytes);
         }
-        if (getenv("F3S_DBG")) fprintf(stderr, "fwd %d/%d dq %d/%d dkv %d/%d\n", p->n_fwd, p->n_fwd_merge, p->n_dq, p->n_dq_merge, p->n_dkv, p->n_dkv_merge);
         e = hipMemcpy(p->store, host.data(), bytes, hipMemcpyHostToDevice);
     }
     *st = f3s::status_of(e);

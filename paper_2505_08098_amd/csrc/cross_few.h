@@ -16,7 +16,8 @@ struct CrossMergeArgs {
 };
 
 template <int D, int kIn>
-__global__ __launch_bounds__(64 * kFewWaves) void k_cross_few(FewArgs a, const DenseItem *items)
+__global__ __launch_bounds__(64 * kFewWaves, few_waves(D, false)) void k_cross_few(
+    FewArgs a, const DenseItem *items)
 {
     const DenseItem d = items[blockIdx.x];
     FewItem it = {};
@@ -31,22 +32,18 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_cross_few(FewArgs a, const D
     few_rows<D, kIn, false>(a, it);
 }
 
-// Rows of split ranges from their partial results: D / 4 threads to a row.
-template <int D, int kIn>
-__global__ __launch_bounds__(256) void k_cross_merge(CrossMergeArgs a)
+// Rows of split ranges from their partial results.
+template <int D, int kIn, bool kSplit>
+__global__ __launch_bounds__(256) void k_cross_join(CrossMergeArgs a)
 {
-    constexpr int kPer = 256 / (D / 4);
+    constexpr int kPer = kSplit ? 1 : 256 / (D / 4);
     const int rec = (int)blockIdx.x / a.blocks;
     const DenseMerge g = a.merges[rec];
-    const int r = ((int)blockIdx.x - rec * a.blocks) * kPer + (int)threadIdx.x / (D / 4);
-    const int c = threadIdx.x % (D / 4) * 4;
-    if (threadIdx.x >= kPer * (D / 4) || r >= g.rows) return;
-    float m = -INFINITY, l = 0.f;
-    f4 o = f4{0.f, 0.f, 0.f, 0.f};
-    merge_pieces<D>(a.part_o, a.part_ml, (int64_t)g.part + r, g.stride, g.count, c, m, l, o);
-    const int64_t out = query_row(a.q, g.head, (int64_t)g.row + r);
-    store4<kIn>(a.O, out * D + c, o * (l == 0.f ? 0.f : 1.f / l));
-    if (c == 0) a.lse[out] = natural_lse(m, l);
+    const int r = ((int)blockIdx.x - rec * a.blocks) * kPer +
+                  (kSplit ? 0 : (int)threadIdx.x / (D / 4));
+    if (r >= g.rows || (!kSplit && (int)threadIdx.x >= kPer * (D / 4))) return;
+    join_row<D, kIn, kSplit>(a.part_o, a.part_ml, {(int64_t)g.part + r, g.stride, g.count},
+                             {0, 0, 0}, query_row(a.q, g.head, (int64_t)g.row + r), a.O, a.lse);
 }
 
 template <int D, int kIn>
@@ -60,9 +57,14 @@ template <int D, int kIn>
 hipError_t launch_cross_merge_d(const f3s_cross_plan_s &p, CrossMergeArgs a, hipStream_t s)
 {
     constexpr int kPer = 256 / (D / 4);
-    a.blocks = (p.fwd_merge_rows + kPer - 1) / kPer;
-    if (p.n_fwd_merge)
-        k_cross_merge<D, kIn><<<(unsigned)(p.n_fwd_merge * a.blocks), 256, 0, s>>>(a);
+    if (!p.n_fwd_merge) return hipSuccess;
+    const bool split = (int64_t)p.n_fwd_merge * p.fwd_merge_rows <= kSplitJoins;
+    a.blocks = split ? p.fwd_merge_rows : (p.fwd_merge_rows + kPer - 1) / kPer;
+    const unsigned grid = (unsigned)(p.n_fwd_merge * a.blocks);
+    if (split)
+        k_cross_join<D, kIn, true><<<grid, 256, 0, s>>>(a);
+    else
+        k_cross_join<D, kIn, false><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 

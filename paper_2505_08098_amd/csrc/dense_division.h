@@ -43,7 +43,15 @@ struct Division {
             longest = one > longest ? one : longest;
         }
         const double rounds = (double)ceil_div((int64_t)n, slots);
-        return longest * n <= 1.25 * total ? rounds * longest : total / slots + longest / 2;
+        const double t = longest * n <= 1.25 * total ? rounds * longest
+                                                     : total / slots + longest / 2;
+        return t + (split(ranges, unit, per) ? kLaunch : 0.0);
+    }
+    static bool split(const std::vector<Range> &ranges, int64_t unit, int64_t per)
+    {
+        for (const Range &r : ranges)
+            if (ceil_div(r.others, unit) > per) return true;
+        return false;
     }
     static int64_t pieces(int64_t units, int64_t per)
     {
@@ -51,6 +59,8 @@ struct Division {
     }
     static constexpr double kOver = 2;  // an item's beginning and end, in units
     static constexpr double kJoin = 1;  // a piece's partial results
+    // The launch that joins them, 5 us, where a unit takes 1.1 (f16, d = 64).
+    static constexpr double kLaunch = 5;
     static constexpr int64_t kMostPieces = 16;
 
     // `slots`: workgroups that run at once; pieces have `least` rows or more.
@@ -74,7 +84,6 @@ struct Division {
             }
             if (k > kMostPieces && k * heads > 4 * slots) break;
         }
-        if (getenv("F3S_PIECES")) per = ceil_div(top, atoi(getenv("F3S_PIECES")));
         // The tiles of a sequence, head and piece walk the same rows: they come
         // one behind the other and run side by side, in step, so that a row is
         // fetched once for many of them.  (Shares cut wherever they are equal,

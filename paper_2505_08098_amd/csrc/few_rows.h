@@ -28,6 +28,13 @@ constexpr int kFewRows = 16;
 constexpr int kFewKeys = 32;
 constexpr int kFewWaves = 4;
 
+// Waves per SIMD, as many as the registers hold without spills: loads of more
+// waves are in flight.
+constexpr int few_waves(int d, bool cache)
+{
+    return cache ? (d <= 64 ? 4 : d <= 160 ? 3 : 2) : (d <= 32 ? 4 : d <= 64 ? 3 : d <= 128 ? 2 : 1);
+}
+
 // What a workgroup does.
 struct FewItem {
     int64_t row;         // first query row of the key head
@@ -169,28 +176,51 @@ __device__ __forceinline__ float natural_lse(float m, float l)
     return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// One thread's four columns (from c) of a row whose partial results are rows
-// first, first + stride, ... (n of them): their states combined in order, added
-// to (m, l, o).  Eight pieces' loads are in flight together.
-template <int D>
-__device__ __forceinline__ void merge_pieces(const float *part_o, const float *part_ml,
-                                             int64_t first, int64_t stride, int n, int c,
-                                             float &m, float &l, f4 &o)
+// The partial results of a row: n of them at rows first, first + stride, ...
+struct PartRows {
+    int64_t first, stride;
+    int n;
+};
+
+// Joins a row's partial results (those of x, then those of y) and stores it at
+// row `out` of O and lse.  kSplit: the whole workgroup of 256 threads does it,
+// each group of D / 4 threads (four columns each) every G-th piece, the groups'
+// states meeting in LDS; else one group of D / 4 threads does it alone, `c` its
+// thread's first column.  Four pieces' loads are in flight together.  With few
+// rows the pieces' loads one behind the other are what a join waits for: 64 rows
+// of 64 pieces of 128 took @@ us with one group, @@ with eight; with many rows
+// the second form launches fewer workgroups (@@ rows: @@ us against @@).
+template <int D, int kIn, bool kSplit>
+__device__ __forceinline__ void join_row(const float *part_o, const float *part_ml,
+                                         const PartRows &x, const PartRows &y, int64_t out,
+                                         void *O, float *lse)
 {
-    constexpr int kAhead = 8;
-    for (int p = 0; p < n; p += kAhead) {
+    constexpr int kGroup = D / 4, kAhead = 4;
+    constexpr int kGroups = kSplit ? 256 / kGroup : 1;
+    __shared__ float s_ml[kGroups][2];
+    __shared__ __attribute__((aligned(16))) float s_o[kSplit ? kGroups : 1][kSplit ? D : 4];
+    const int group = kSplit ? (int)threadIdx.x / kGroup : 0;
+    const int c = (int)threadIdx.x % kGroup * 4;
+    const int n = x.n + y.n;
+    float m = -INFINITY, l = 0.f;
+    f4 o = f4{0.f, 0.f, 0.f, 0.f};
+    for (int p = group; p < n && group < kGroups; p += kGroups * kAhead) {
         f4 po[kAhead];
         float pm[kAhead], pl[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const int64_t row = first + stride * min(p + k, n - 1);
-            pm[k] = p + k < n ? part_ml[2 * row] : -INFINITY;
+            const int at = min(p + k * kGroups, n - 1);
+            const int64_t row = at < x.n ? x.first + x.stride * at : y.first + y.stride * (at - x.n);
+            pm[k] = part_ml[2 * row];
             pl[k] = part_ml[2 * row + 1];
             po[k] = *reinterpret_cast<const f4 *>(part_o + row * D + c);
         }
         float top = m;
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) top = fmaxf(top, pm[k]);
+        for (int k = 0; k < kAhead; ++k) {
+            if (p + k * kGroups >= n) pm[k] = -INFINITY;
+            top = fmaxf(top, pm[k]);
+        }
         const float ref = top == -INFINITY ? 0.f : top;
         const float f = __builtin_amdgcn_exp2f(m - ref);
         m = top;
@@ -203,7 +233,36 @@ __device__ __forceinline__ void merge_pieces(const float *part_o, const float *p
             o += w * po[k];
         }
     }
+    if constexpr (kSplit) {
+        if (group < kGroups) {
+            if (c == 0) {
+                s_ml[group][0] = m;
+                s_ml[group][1] = l;
+            }
+            *reinterpret_cast<f4 *>(&s_o[group][c]) = o;
+        }
+        __syncthreads();
+        if (threadIdx.x >= kGroup) return;
+        float top = s_ml[0][0];
+#pragma unroll
+        for (int k = 1; k < kGroups; ++k) top = fmaxf(top, s_ml[k][0]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        m = top;
+        l = 0.f;
+        o = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+            const float w = __builtin_amdgcn_exp2f(s_ml[k][0] - ref);
+            l += w * s_ml[k][1];
+            o += w * *reinterpret_cast<const f4 *>(&s_o[k][c]);
+        }
+    }
+    store4<kIn>(O, out * D + c, o * (l == 0.f ? 0.f : 1.f / l));
+    if (c == 0) lse[out] = natural_lse(m, l);
 }
+
+// Rows up to which a workgroup joins one.
+constexpr int64_t kSplitJoins = 8192;
 
 template <int D, int kIn, bool kCache>
 __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)

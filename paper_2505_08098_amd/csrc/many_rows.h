@@ -285,14 +285,17 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
         for (int e = 1; e < 16 * kBlocks; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
         mx = max_xor32(mx) * a.sl2;
         const float m_new = fmaxf(m_run, mx);
-        const float m_ref = m_new == -INFINITY ? 0.f : m_new;
-        if (__ballot(m_new > m_run)) {
-            const float alpha = __builtin_amdgcn_exp2f(m_run - m_ref);
+        // (a maximum that has grown by less than 2^6 is not worth the products: the
+        // probabilities may as well be up to 64, with the same bits)
+        if (__ballot(m_new > m_run + 6.f)) {
+            const float alpha =
+                __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
             l_run *= alpha;
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) o[d] *= alpha;
             m_run = m_new;
         }
+        const float m_ref = m_run == -INFINITY ? 0.f : m_run;
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 16 * kBlocks; ++e) {

@@ -12,17 +12,18 @@ include/f3s_cache.h).  Argument marshalling only, like ``binding``.
 """
 import contextlib
 import ctypes
+import functools
 import math
 
 import torch
 
-from .binding import (_DTYPE_CODE, F3S_OK, F3SError, _BuildOn, _check_device_tensor,
-                      load_library)
-from . import binding as _binding
+from .binding import (_DTYPE_CODE, _TENSORS, F3S_OK, F3SError, _BuildOn,
+                      _check_device_tensor, _raw_stream, load_library)
 
 _LIB = None
 _vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
 _HALF = (torch.float16, torch.bfloat16)
+_READ_TYPES = _HALF + (torch.float32,)
 
 
 class _CacheStruct(ctypes.Structure):
@@ -65,18 +66,32 @@ def _switch(device, stream):
             yield
 
 
-_NOTHING = contextlib.nullcontext()
+# The current device (torch's own accessor where it has one: 0.1 us instead of 0.5).
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _on(device, stream):
-    """The device and stream of a call made current, so that results and
-    workspaces are the stream's own memory (torch hands a stream's freed memory
-    to that stream's later work only)."""
-    if stream is not None and stream.device != device:
+def _elsewhere(device, stream):
+    """None where a call runs as it is; else what makes its device and stream
+    current, so that results and workspaces are the stream's own memory (torch
+    hands a stream's freed memory to that stream's later work only)."""
+    if stream is None:
+        return None if _current_device() == device.index else _switch(device, None)
+    if stream.device != device:
         raise ValueError(f"the stream is on {stream.device}, the operands on {device}")
-    if stream is None and torch.cuda.current_device() == device.index:
-        return _NOTHING
     return _switch(device, stream)
+
+
+def _on_its_device(fn):
+    """The call with its device and stream current; fn takes a plan or a cache
+    first and no stream."""
+    @functools.wraps(fn)
+    def call(handle, *args, stream=None, **kwargs):
+        switch = _elsewhere(handle.device, stream)
+        if switch is None:
+            return fn(handle, *args, **kwargs)
+        with switch:
+            return fn(handle, *args, **kwargs)
+    return call
 
 
 def _call(name, *args):
@@ -86,6 +101,9 @@ def _call(name, *args):
 
 
 def _check(t, name, dtype, device, shape):
+    if (type(t) in _TENSORS and t.dtype is dtype and t.shape == shape and t.device == device
+            and t.is_contiguous()):
+        return
     _check_device_tensor(t, name, dtype, device)
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
@@ -160,6 +178,7 @@ class CrossPlan:
         self.heads, self.kv_heads, self.d = int(heads), int(kv_heads), int(d)
         self.q_shape = (int(q[-1]), self.heads, self.d)
         self.k_shape = (int(k[-1]), self.kv_heads, self.d)
+        self.scale = 1.0 / math.sqrt(self.d)
         self._forward_bytes = L.f3s_cross_forward_workspace_bytes(h)
         self._backward_bytes = L.f3s_cross_backward_workspace_bytes(h)
 
@@ -195,41 +214,42 @@ def _cross_operands(plan, Q, K, V):
     return dtype
 
 
-def cross_forward(plan, Q, K, V, scale=None, out=None, lse=None, stream=None):
+@_on_its_device
+def cross_forward(plan, Q, K, V, scale=None, out=None, lse=None):
     """f3s_cross_forward: O = softmax(scale Q K^T) V within each sequence of
-    the plan.  Q [rows, heads, d], K and V [rows, kv_heads, d], fp16 or bf16.
-    Returns (O, lse): O like Q, lse fp32 [rows, heads]."""
+    the plan.  Q [rows, heads, d], K and V [rows, kv_heads, d], fp16 or bf16;
+    ``stream=`` (default: torch's current one).  Returns (O, lse): O like Q,
+    lse fp32 [rows, heads]."""
     dtype = _cross_operands(plan, Q, K, V)
-    if scale is None:
-        scale = 1.0 / math.sqrt(plan.d)
-    with _on(plan.device, stream):
-        out = _result(out, "out", plan.q_shape, dtype, plan.device)
-        lse = _result(lse, "lse", plan.q_shape[:2], torch.float32, plan.device)
-        ws = _workspace(plan._forward_bytes, plan.device)
-        _call("f3s_cross_forward", plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(),
-              _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(), float(scale), _ptr(ws),
-              plan._forward_bytes, _binding._raw_stream(plan.device.index))
+    device = plan.device
+    out = _result(out, "out", plan.q_shape, dtype, device)
+    lse = _result(lse, "lse", plan.q_shape[:2], torch.float32, device)
+    nbytes = plan._forward_bytes
+    ws = _workspace(nbytes, device)
+    _call("f3s_cross_forward", plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+          _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
+          plan.scale if scale is None else float(scale), _ptr(ws), nbytes,
+          _raw_stream(device.index))
     return out, lse
 
 
-def cross_backward(plan, Q, K, V, O, dO, lse, scale=None, stream=None):
+@_on_its_device
+def cross_backward(plan, Q, K, V, O, dO, lse, scale=None):
     """f3s_cross_backward: (dQ, dK, dV), of the operands' shapes and type, for
-    dO = dL/dO and the forward's O and lse."""
+    dO = dL/dO and the forward's O and lse; ``stream=`` as cross_forward."""
     dtype = _cross_operands(plan, Q, K, V)
-    _check(O, "O", dtype, plan.device, plan.q_shape)
-    _check(dO, "dO", dtype, plan.device, plan.q_shape)
-    _check(lse, "lse", torch.float32, plan.device, plan.q_shape[:2])
-    if scale is None:
-        scale = 1.0 / math.sqrt(plan.d)
-    with _on(plan.device, stream):
-        dQ = torch.empty(plan.q_shape, dtype=dtype, device=plan.device)
-        dK, dV = (torch.empty(plan.k_shape, dtype=dtype, device=plan.device)
-                  for _ in range(2))
-        ws = _workspace(plan._backward_bytes, plan.device)
-        _call("f3s_cross_backward", plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(),
-              _DTYPE_CODE[dtype], O.data_ptr(), dO.data_ptr(), lse.data_ptr(), dQ.data_ptr(),
-              dK.data_ptr(), dV.data_ptr(), float(scale), _ptr(ws), plan._backward_bytes,
-              _binding._raw_stream(plan.device.index))
+    device = plan.device
+    _check(O, "O", dtype, device, plan.q_shape)
+    _check(dO, "dO", dtype, device, plan.q_shape)
+    _check(lse, "lse", torch.float32, device, plan.q_shape[:2])
+    dQ = torch.empty(plan.q_shape, dtype=dtype, device=device)
+    dK, dV = (torch.empty(plan.k_shape, dtype=dtype, device=device) for _ in range(2))
+    nbytes = plan._backward_bytes
+    ws = _workspace(nbytes, device)
+    _call("f3s_cross_backward", plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+          _DTYPE_CODE[dtype], O.data_ptr(), dO.data_ptr(), lse.data_ptr(), dQ.data_ptr(),
+          dK.data_ptr(), dV.data_ptr(), plan.scale if scale is None else float(scale),
+          _ptr(ws), nbytes, _raw_stream(device.index))
     return dQ, dK, dV
 
 
@@ -260,6 +280,8 @@ class Cache:
                                     v_exp.data_ptr(), self.n_pages, self.kv_heads,
                                     self.page_size, self.d)
         self._ref = ctypes.byref(self._struct)
+        self.scale = 1.0 / math.sqrt(self.d) if self.d else 1.0
+        self._bytes = {}  # workspace of an attend call, by its sizes
 
     @classmethod
     def empty(cls, n_pages, page_size, kv_heads, d, device="cuda"):
@@ -273,76 +295,86 @@ class Cache:
 
 def _sequences(cache, table, lens):
     """(number of sequences, pages of a table row), checked."""
-    _check_device_tensor(table, "table", torch.int32, cache.device)
-    _check_device_tensor(lens, "lens", torch.int32, cache.device)
+    device = cache.device
+    for t, n in ((table, "table"), (lens, "lens")):
+        if not (type(t) in _TENSORS and t.dtype is torch.int32 and t.device == device
+                and t.is_contiguous()):
+            _check_device_tensor(t, n, torch.int32, device)
     if table.dim() != 2 or lens.dim() != 1 or table.shape[0] != lens.shape[0]:
         raise ValueError("table must be [sequences, pages], lens [sequences]")
     return table.shape
 
 
-def cache_write(cache, K, V, table, lens, stream=None):
+@_on_its_device
+def cache_write(cache, K, V, table, lens):
     """f3s_cache_write: the newest rows of every sequence, K and V [sequences,
     n, kv_heads, d] in fp16 or bf16, quantised into the pages of ``table``
     (int32 [sequences, pages]).  ``lens`` (int32) are the sequences' lengths
-    with these rows; row t goes to position lens[b] - n + t."""
+    with these rows; row t goes to position lens[b] - n + t.  ``stream=``
+    (default: torch's current one)."""
     B, pages = _sequences(cache, table, lens)
     dtype = _dtype_of(K, "K")
     if K.dim() != 4:
         raise ValueError("K must be [sequences, n, kv_heads, d]")
     n = K.shape[1]
-    for t, name in ((K, "K"), (V, "V")):
-        _check(t, name, dtype, cache.device, (B, n, cache.kv_heads, cache.d))
-    with _on(cache.device, stream):
-        _call("f3s_cache_write", cache._ref, K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
-              table.data_ptr(), pages, lens.data_ptr(), B, n,
-              _binding._raw_stream(cache.device.index))
+    shape = (B, n, cache.kv_heads, cache.d)
+    _check(K, "K", dtype, cache.device, shape)
+    _check(V, "V", dtype, cache.device, shape)
+    _call("f3s_cache_write", cache._ref, K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
+          table.data_ptr(), pages, lens.data_ptr(), B, n, _raw_stream(cache.device.index))
 
 
-def cache_read(cache, table, lens, n, dtype=torch.float16, stream=None):
+@_on_its_device
+def cache_read(cache, table, lens, n, dtype=torch.float16):
     """f3s_cache_read: the ``n`` newest rows of every sequence, (K, V) of
-    ``dtype`` (float16, bfloat16 or float32), [sequences, n, kv_heads, d]."""
+    ``dtype`` (float16, bfloat16 or float32), [sequences, n, kv_heads, d];
+    ``stream=`` as cache_write."""
     B, pages = _sequences(cache, table, lens)
-    if dtype not in _HALF + (torch.float32,):
+    if dtype not in _READ_TYPES:
         raise TypeError("dtype must be float16, bfloat16 or float32")
-    shape = (B, int(n), cache.kv_heads, cache.d)
-    with _on(cache.device, stream):
-        K, V = (torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
-        _call("f3s_cache_read", cache._ref, K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
-              table.data_ptr(), pages, lens.data_ptr(), B, int(n),
-              _binding._raw_stream(cache.device.index))
+    n = int(n)
+    shape = (B, n, cache.kv_heads, cache.d)
+    K = torch.empty(shape, dtype=dtype, device=cache.device)
+    V = torch.empty_like(K)
+    _call("f3s_cache_read", cache._ref, K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
+          table.data_ptr(), pages, lens.data_ptr(), B, n, _raw_stream(cache.device.index))
     return K, V
 
 
+@_on_its_device
 def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, out=None,
-                 lse=None, stream=None):
+                 lse=None):
     """f3s_cache_attend: the newest tokens of every sequence, Q [sequences, n,
     heads, d] in fp16 or bf16, attend to the first ``prefix_len`` tokens of the
     pages ``prefix`` (int32, shared by all sequences) and to their own cached
-    keys up to themselves.  Returns (O, lse): O like Q, lse fp32 [sequences, n,
-    heads]."""
+    keys up to themselves; ``stream=`` as cache_write.  Returns (O, lse): O
+    like Q, lse fp32 [sequences, n, heads]."""
     B, pages = _sequences(cache, table, lens)
     dtype = _dtype_of(Q, "Q")
     if Q.dim() != 4 or Q.shape[2] < 1 or Q.shape[2] % cache.kv_heads:
         raise ValueError("Q must be [sequences, n, heads, d], heads a multiple of kv_heads")
     n, heads = Q.shape[1:3]
-    _check(Q, "Q", dtype, cache.device, (B, n, heads, cache.d))
+    device = cache.device
+    _check(Q, "Q", dtype, device, (B, n, heads, cache.d))
     prefix_len = int(prefix_len)
     if prefix_len < 0 or (prefix is None) != (prefix_len == 0):
         raise ValueError("prefix and a positive prefix_len come together")
     if prefix is not None:
-        _check_device_tensor(prefix, "prefix", torch.int32, cache.device)
+        _check_device_tensor(prefix, "prefix", torch.int32, device)
         if prefix.dim() != 1 or prefix.numel() * cache.page_size < prefix_len:
             raise ValueError("prefix must name enough pages for prefix_len tokens")
-    if scale is None:
-        scale = 1.0 / math.sqrt(cache.d)
-    sizes = (pages, B, n, heads)
-    with _on(cache.device, stream):
-        out = _result(out, "out", Q.shape, dtype, cache.device)
-        lse = _result(lse, "lse", Q.shape[:3], torch.float32, cache.device)
-        nbytes = _lib().f3s_cache_attend_workspace_bytes(cache._ref, *sizes, prefix_len)
-        ws = _workspace(nbytes, cache.device)
-        _call("f3s_cache_attend", cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype],
-              out.data_ptr(), lse.data_ptr(), table.data_ptr(), pages, lens.data_ptr(), B, n,
-              heads, _ptr(prefix), prefix_len, float(scale), _ptr(ws), nbytes,
-              _binding._raw_stream(cache.device.index))
+    sizes = (pages, B, n, heads, prefix_len)
+    nbytes = cache._bytes.get(sizes)
+    if nbytes is None:
+        if len(cache._bytes) >= 64:  # (a prefix that grows)
+            cache._bytes.clear()
+        nbytes = _lib().f3s_cache_attend_workspace_bytes(cache._ref, *sizes)
+        cache._bytes[sizes] = nbytes
+    out = _result(out, "out", Q.shape, dtype, device)
+    lse = _result(lse, "lse", Q.shape[:3], torch.float32, device)
+    ws = _workspace(nbytes, device)
+    _call("f3s_cache_attend", cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(),
+          lse.data_ptr(), table.data_ptr(), pages, lens.data_ptr(), B, n, heads,
+          _ptr(prefix), prefix_len, cache.scale if scale is None else float(scale), _ptr(ws),
+          nbytes, _raw_stream(device.index))
     return out, lse

@@ -201,3 +201,20 @@ def _compare(cache, Q, table, lens, prefix, prefix_len, scale, O, lse):
 ])
 def test_attend(gpu, dtype, d, page, kv, g, lens, n, prefix):
     _attend_case(gpu, dtype, d, page, kv, g, lens, n, prefix)
+
+
+@pytest.mark.parametrize("rows", ["16", "128"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d,page,kv,g,B,n,prefix", [
+    (64, 16, 2, 4, 20, 1, 130),            # 80 rows
+    (128, 64, 1, 8, 33, 1, 1000),          # 264 rows, a tile that is not full
+    (128, 32, 2, 4, 5, 5, 321),
+    (96, 16, 1, 5, 14, 1, 64), (32, 32, 1, 1, 129, 1, 63),
+    (256, 128, 1, 2, 40, 1, 300), (160, 16, 1, 3, 30, 1, 65),
+    (64, 16, 1, 1, 70, 1, 4500),           # more keys than one workgroup walks
+])
+def test_attend_shared_prefix(gpu, monkeypatch, rows, dtype, d, page, kv, g, B, n, prefix):
+    """The prefix by the kernel of 16 query rows and by that of 128."""
+    monkeypatch.setenv("F3S_PREFIX_ROWS", rows)
+    lens = [(7 * b) % 50 for b in range(B)]
+    _attend_case(gpu, dtype, d, page, kv, g, lens, n, prefix)

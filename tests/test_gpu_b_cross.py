@@ -83,10 +83,13 @@ CASES = [
 ]
 
 
+@pytest.mark.parametrize("rows", ["16", "128"])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("padded", [False, True])
 @pytest.mark.parametrize("d,kv,g,q,k", CASES)
-def test_forward(gpu, dtype, padded, d, kv, g, q, k):
+def test_forward(gpu, monkeypatch, rows, dtype, padded, d, kv, g, q, k):
+    """By the kernel of 16 query rows and by that of 128."""
+    monkeypatch.setenv("F3S_CROSS_ROWS", rows)
     _case(gpu, dtype, d, kv, g, q, k, padded=padded, grad=False)
 
 
