@@ -43,8 +43,9 @@ struct Division {
             longest = one > longest ? one : longest;
         }
         const double rounds = (double)ceil_div((int64_t)n, slots);
-        const double t = longest * n <= 1.25 * total ? rounds * longest
-                                                     : total / slots + longest / 2;
+        const double t = rounds <= 1                  ? longest
+                         : longest * n <= 1.25 * total ? rounds * longest
+                                                       : total / slots + longest / 2;
         return t + (split(ranges, unit, per) ? kLaunch : 0.0);
     }
     static bool split(const std::vector<Range> &ranges, int64_t unit, int64_t per)

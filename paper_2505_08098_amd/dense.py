@@ -17,8 +17,8 @@ import math
 
 import torch
 
-from .binding import (_DTYPE_CODE, _TENSORS, F3S_OK, F3SError, _BuildOn,
-                      _check_device_tensor, _raw_stream, load_library)
+from .binding import (_DTYPE_CODE, _TENSORS, F3SError, _BuildOn, _check_device_tensor,
+                      _empty_like, _raw_stream, load_library)
 
 _LIB = None
 _vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
@@ -94,12 +94,6 @@ def _on_its_device(fn):
     return call
 
 
-def _call(name, *args):
-    rc = getattr(_lib(), name)(*args)
-    if rc != F3S_OK:
-        raise F3SError(rc, name)
-
-
 def _check(t, name, dtype, device, shape):
     if (type(t) in _TENSORS and t.dtype is dtype and t.shape == shape and t.device == device
             and t.is_contiguous()):
@@ -115,20 +109,8 @@ def _dtype_of(t, name):
     return t.dtype
 
 
-def _result(t, name, shape, dtype, device):
-    """The caller's tensor for a result, or a new one."""
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    _check(t, name, dtype, device, shape)
-    return t
-
-
-def _workspace(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-
-
-def _ptr(t):
-    return t.data_ptr() if t is not None else None
+def _fail(rc, name):
+    raise F3SError(rc, name)
 
 
 def _host_ints(x, name):
@@ -178,6 +160,7 @@ class CrossPlan:
         self.heads, self.kv_heads, self.d = int(heads), int(kv_heads), int(d)
         self.q_shape = (int(q[-1]), self.heads, self.d)
         self.k_shape = (int(k[-1]), self.kv_heads, self.d)
+        self.lse_shape = self.q_shape[:2]
         self.scale = 1.0 / math.sqrt(self.d)
         self._forward_bytes = L.f3s_cross_forward_workspace_bytes(h)
         self._backward_bytes = L.f3s_cross_backward_workspace_bytes(h)
@@ -222,14 +205,22 @@ def cross_forward(plan, Q, K, V, scale=None, out=None, lse=None):
     lse fp32 [rows, heads]."""
     dtype = _cross_operands(plan, Q, K, V)
     device = plan.device
-    out = _result(out, "out", plan.q_shape, dtype, device)
-    lse = _result(lse, "lse", plan.q_shape[:2], torch.float32, device)
+    if out is None:
+        out = _empty_like(Q, dtype)
+    else:
+        _check(out, "out", dtype, device, plan.q_shape)
+    if lse is None:
+        lse = torch.empty(plan.lse_shape, dtype=torch.float32, device=device)
+    else:
+        _check(lse, "lse", torch.float32, device, plan.lse_shape)
     nbytes = plan._forward_bytes
-    ws = _workspace(nbytes, device)
-    _call("f3s_cross_forward", plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(),
-          _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
-          plan.scale if scale is None else float(scale), _ptr(ws), nbytes,
-          _raw_stream(device.index))
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    rc = _lib().f3s_cross_forward(
+        plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
+        out.data_ptr(), lse.data_ptr(), plan.scale if scale is None else float(scale),
+        ws.data_ptr() if nbytes else None, nbytes, _raw_stream(device.index))
+    if rc:
+        _fail(rc, "f3s_cross_forward")
     return out, lse
 
 
@@ -241,15 +232,17 @@ def cross_backward(plan, Q, K, V, O, dO, lse, scale=None):
     device = plan.device
     _check(O, "O", dtype, device, plan.q_shape)
     _check(dO, "dO", dtype, device, plan.q_shape)
-    _check(lse, "lse", torch.float32, device, plan.q_shape[:2])
-    dQ = torch.empty(plan.q_shape, dtype=dtype, device=device)
-    dK, dV = (torch.empty(plan.k_shape, dtype=dtype, device=device) for _ in range(2))
+    _check(lse, "lse", torch.float32, device, plan.lse_shape)
+    dQ, dK, dV = _empty_like(Q, dtype), _empty_like(K, dtype), _empty_like(V, dtype)
     nbytes = plan._backward_bytes
-    ws = _workspace(nbytes, device)
-    _call("f3s_cross_backward", plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(),
-          _DTYPE_CODE[dtype], O.data_ptr(), dO.data_ptr(), lse.data_ptr(), dQ.data_ptr(),
-          dK.data_ptr(), dV.data_ptr(), plan.scale if scale is None else float(scale),
-          _ptr(ws), nbytes, _raw_stream(device.index))
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    rc = _lib().f3s_cross_backward(
+        plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
+        O.data_ptr(), dO.data_ptr(), lse.data_ptr(), dQ.data_ptr(), dK.data_ptr(),
+        dV.data_ptr(), plan.scale if scale is None else float(scale),
+        ws.data_ptr() if nbytes else None, nbytes, _raw_stream(device.index))
+    if rc:
+        _fail(rc, "f3s_cross_backward")
     return dQ, dK, dV
 
 
@@ -320,8 +313,11 @@ def cache_write(cache, K, V, table, lens):
     shape = (B, n, cache.kv_heads, cache.d)
     _check(K, "K", dtype, cache.device, shape)
     _check(V, "V", dtype, cache.device, shape)
-    _call("f3s_cache_write", cache._ref, K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
-          table.data_ptr(), pages, lens.data_ptr(), B, n, _raw_stream(cache.device.index))
+    rc = _lib().f3s_cache_write(
+        cache._ref, K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype], table.data_ptr(), pages,
+        lens.data_ptr(), B, n, _raw_stream(cache.device.index))
+    if rc:
+        _fail(rc, "f3s_cache_write")
 
 
 @_on_its_device
@@ -336,8 +332,11 @@ def cache_read(cache, table, lens, n, dtype=torch.float16):
     shape = (B, n, cache.kv_heads, cache.d)
     K = torch.empty(shape, dtype=dtype, device=cache.device)
     V = torch.empty_like(K)
-    _call("f3s_cache_read", cache._ref, K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
-          table.data_ptr(), pages, lens.data_ptr(), B, n, _raw_stream(cache.device.index))
+    rc = _lib().f3s_cache_read(
+        cache._ref, K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype], table.data_ptr(), pages,
+        lens.data_ptr(), B, n, _raw_stream(cache.device.index))
+    if rc:
+        _fail(rc, "f3s_cache_read")
     return K, V
 
 
@@ -353,14 +352,17 @@ def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, o
     dtype = _dtype_of(Q, "Q")
     if Q.dim() != 4 or Q.shape[2] < 1 or Q.shape[2] % cache.kv_heads:
         raise ValueError("Q must be [sequences, n, heads, d], heads a multiple of kv_heads")
-    n, heads = Q.shape[1:3]
+    _, n, heads, _ = shape = Q.shape
     device = cache.device
     _check(Q, "Q", dtype, device, (B, n, heads, cache.d))
-    prefix_len = int(prefix_len)
-    if prefix_len < 0 or (prefix is None) != (prefix_len == 0):
-        raise ValueError("prefix and a positive prefix_len come together")
-    if prefix is not None:
+    if prefix is None:
+        if prefix_len != 0:
+            raise ValueError("prefix and a positive prefix_len come together")
+    else:
+        prefix_len = int(prefix_len)
         _check_device_tensor(prefix, "prefix", torch.int32, device)
+        if prefix_len < 1:
+            raise ValueError("prefix and a positive prefix_len come together")
         if prefix.dim() != 1 or prefix.numel() * cache.page_size < prefix_len:
             raise ValueError("prefix must name enough pages for prefix_len tokens")
     sizes = (pages, B, n, heads, prefix_len)
@@ -370,11 +372,21 @@ def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, o
             cache._bytes.clear()
         nbytes = _lib().f3s_cache_attend_workspace_bytes(cache._ref, *sizes)
         cache._bytes[sizes] = nbytes
-    out = _result(out, "out", Q.shape, dtype, device)
-    lse = _result(lse, "lse", Q.shape[:3], torch.float32, device)
-    ws = _workspace(nbytes, device)
-    _call("f3s_cache_attend", cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(),
-          lse.data_ptr(), table.data_ptr(), pages, lens.data_ptr(), B, n, heads,
-          _ptr(prefix), prefix_len, cache.scale if scale is None else float(scale), _ptr(ws),
-          nbytes, _raw_stream(device.index))
+    if out is None:
+        out = _empty_like(Q, dtype)
+    else:
+        _check(out, "out", dtype, device, shape)
+    if lse is None:
+        lse = torch.empty((B, n, heads), dtype=torch.float32, device=device)
+    else:
+        _check(lse, "lse", torch.float32, device, (B, n, heads))
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    rc = _lib().f3s_cache_attend(
+        cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
+        table.data_ptr(), pages, lens.data_ptr(), B, n, heads,
+        None if prefix is None else prefix.data_ptr(), prefix_len,
+        cache.scale if scale is None else float(scale), ws.data_ptr() if nbytes else None,
+        nbytes, _raw_stream(device.index))
+    if rc:
+        _fail(rc, "f3s_cache_attend")
     return out, lse

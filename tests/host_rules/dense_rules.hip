@@ -123,6 +123,10 @@ static void divisions()
     d.make({{0, 4001, 0, 4095}, {4001, 4099, 4095, 4001}}, 4, 128, 64, 256, 512);
     const double n = (double)d.merges.front().count;
     CHECK(std::ceil(260 * n / 512) / n < 0.7);
+    // a few long tiles of different lengths: divided, however short the others are
+    Division f;
+    f.make({{0, 59, 0, 1016}, {59, 40, 1016, 760}, {99, 20, 1776, 512}}, 2, 128, 64, 256, 512);
+    CHECK(f.items.size() > 15 && f.merges.size() == 6);
 }
 
 static void own_keys()
