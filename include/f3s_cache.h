@@ -51,7 +51,8 @@ typedef struct {
  *   table      device int32 [n_seqs, max_pages]
  *   lens       device int32 [n_seqs], the lengths after this call
  * Two rows of one call must not lie at the same place (a page named twice):
- * what such a place then holds is not defined.  Asynchronous on `stream`; no
+ * what such a place then holds is not defined.  K and V must not overlap the
+ * cache.  Asynchronous on `stream`; no
  * allocation, no synchronisation.
  */
 f3s_status_t f3s_cache_write(const f3s_cache_t *cache, const void *K, const void *V,
@@ -62,7 +63,8 @@ f3s_status_t f3s_cache_write(const f3s_cache_t *cache, const void *K, const void
 /*
  * Read the n_new newest rows of every sequence back: K, V (laid out as for
  * f3s_cache_write) receive the values rounded to dtype (F16, BF16 or F32) to
- * nearest even, zeros where a row has no place.  K or V may be NULL.
+ * nearest even, zeros where a row has no place.  K or V may be NULL; they must
+ * not overlap each other or anything that is read.
  */
 f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtype_t dtype,
                             const int32_t *table, int32_t max_pages, const int32_t *lens,

@@ -192,6 +192,7 @@ f3s_status_t f3s_cache_attend(const f3s_cache_t *cache, const void *Q, f3s_dtype
               {cache->v_exp, cb},
               {table, (size_t)n_seqs * max_pages * 4},
               {lens, (size_t)n_seqs * 4},
+              {prefix, ((size_t)prefix_len + cache->page_size - 1) / cache->page_size * 4},
               {workspace, w.bytes}};
     for (const auto &x : in)
         if (overlaps(O, qb, x.p, x.n) || overlaps(lse, lb, x.p, x.n))

@@ -185,6 +185,26 @@ struct Read {
 
 bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
+// Whether n bytes at p share any with the cache or, where they are written
+// (`out`), with what is read beside it.
+bool meets(const void *p, size_t n, const RowArgs &a, bool out)
+{
+    const size_t places = (size_t)a.c.n_pages * a.c.n_kv_heads * a.c.page_size;
+    const size_t seqs = a.rows / ((size_t)a.n_new * a.c.n_kv_heads);
+    const struct {
+        const void *p;
+        size_t n;
+    } with[] = {{a.c.k, places * a.c.d}, {a.c.v, places * a.c.d}, {a.c.k_exp, places},
+                {a.c.v_exp, places}, {a.table, out ? seqs * a.max_pages * 4 : 0},
+                {a.lens, out ? seqs * 4 : 0}};
+    const uintptr_t x = (uintptr_t)p;
+    for (const auto &w : with) {
+        const uintptr_t y = (uintptr_t)w.p;
+        if (p && w.n && x < y + w.n && y < x + n) return true;
+    }
+    return false;
+}
+
 }  // namespace
 
 f3s_status_t check_cache(const f3s_cache_t *c)
@@ -235,7 +255,9 @@ f3s_status_t f3s_cache_write(const f3s_cache_t *cache, const void *K, const void
     if (dtype != F3S_DTYPE_F16 && dtype != F3S_DTYPE_BF16)
         return f3s::set_status(F3S_ERR_UNSUPPORTED);
     if (a.rows == 0) return F3S_OK;
-    if (!K || !V || !f3s::aligned(K, 16) || !f3s::aligned(V, 16))
+    const size_t bytes = (size_t)a.rows * cache->d * 2;
+    if (!K || !V || !f3s::aligned(K, 16) || !f3s::aligned(V, 16) ||
+        f3s::meets(K, bytes, a, false) || f3s::meets(V, bytes, a, false))
         return f3s::set_status(F3S_ERR_INVALID_VALUE);
     return f3s::set_status(f3s::status_of(
         f3s::with_d<f3s::Write>(cache->d, a, K, V, dtype == F3S_DTYPE_BF16, stream)));
@@ -251,7 +273,10 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
     if (dtype != F3S_DTYPE_F16 && dtype != F3S_DTYPE_BF16 && dtype != F3S_DTYPE_F32)
         return f3s::set_status(F3S_ERR_UNSUPPORTED);
     if (a.rows == 0 || (!K && !V)) return F3S_OK;
-    if (!f3s::aligned(K, 16) || !f3s::aligned(V, 16))
+    const size_t bytes = (size_t)a.rows * cache->d * (dtype == F3S_DTYPE_F32 ? 4 : 2);
+    const uintptr_t k = (uintptr_t)K, v = (uintptr_t)V;
+    if (!f3s::aligned(K, 16) || !f3s::aligned(V, 16) || f3s::meets(K, bytes, a, true) ||
+        f3s::meets(V, bytes, a, true) || (K && V && k < v + bytes && v < k + bytes))
         return f3s::set_status(F3S_ERR_INVALID_VALUE);
     return f3s::set_status(
         f3s::status_of(f3s::with_d<f3s::Read>(cache->d, a, K, V, dtype, stream)));
