@@ -3,10 +3,15 @@
 //
 // The kernel of many_rows.h with another way into LDS: a tile's codes wait in
 // registers and are widened as they are stored, once for the 128 rows of the
-// workgroup, K to the queries' type and V to f16 (every code is exact in both).
-// A key's power of two multiplies its scores, a value's its probabilities,
-// relative to the tile's largest power and that to the largest so far, so that
-// P V runs in f16 whatever the values' size.
+// workgroup, K to the queries' type and V to f16.  The vector unit is what bounds
+// it (each exponential, maximum and sum costs the cycles that 1/2 product does),
+// so the powers of two ride on that conversion: a key's relative to the tile's
+// largest, which multiplies the scores within the exponential's own fused
+// operation, a value's relative to the largest that the workgroup has met, which
+// the sums are multiples of.  A code has four bits, so the widened value is exact
+// unless its row is 2^15 times smaller than that largest one (f16; 2^117 in
+// bf16); then it is off by at most 2^-25 of the largest power, which is less than
+// the probabilities' own rounding leaves.
 #pragma once
 
 #include "attend.h"
@@ -27,24 +32,32 @@ template <int D>
 struct CodeTile {
     using T = ManyTile<D, code_keys(D)>;
     __attribute__((aligned(16))) uint8_t k[T::kBytes], v[T::kBytes];
-    __attribute__((aligned(16))) float ck[T::kRows];  // power of a key, times |scale| log2 e
-    __attribute__((aligned(16))) float fv[T::kRows];  // power of a value / the tile's largest
-    uint32_t there[2];  // keys that are there, a bit each
-    int32_t top;        // the tile's largest power
 };
 
-// Largest of a wave's numbers, by lane moves of the vector unit (through LDS they
-// would hold up the wave that every other one waits for).
-__device__ __forceinline__ int wave_max(int v)
+// Largest of the lower and of the upper halves of a wave's numbers, by lane moves
+// of the vector unit (through LDS they would hold up the wave that every other
+// one waits for).
+__device__ __forceinline__ uint32_t wave_max2(uint32_t v)
 {
-    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x121, 0xF, 0xF, false));  // row_ror:1
-    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x122, 0xF, 0xF, false));
-    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x124, 0xF, 0xF, false));
-    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x128, 0xF, 0xF, false));
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    auto larger = [](uint32_t x, uint32_t y) {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(
+            __builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
+    };
+    v = larger(v, __builtin_amdgcn_mov_dpp(v, 0x121, 0xF, 0xF, true));  // row_ror:1
+    v = larger(v, __builtin_amdgcn_mov_dpp(v, 0x122, 0xF, 0xF, true));
+    v = larger(v, __builtin_amdgcn_mov_dpp(v, 0x124, 0xF, 0xF, true));
+    v = larger(v, __builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, true));
     auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    v = max((int)r[0], (int)r[1]);
+    v = larger(r[0], r[1]);
     r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    return max((int)r[0], (int)r[1]);
+    return __builtin_amdgcn_readfirstlane(larger(r[0], r[1]));
+}
+
+// 2^e for e <= 0, at least 2^-126.
+__device__ __forceinline__ float power_of(int e)
+{
+    return __builtin_bit_cast(float, (max(e, -126) + 127) << 23);
 }
 
 template <int D, int kIn>
@@ -70,35 +83,36 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
     const bool there = mine < rows;
     const bool busy = 32 * wave < rows;
 
+    h8 q[D / 16];
+    load_rows32<D>(q, a.few.Q,
+                   query_row(a.few.q, head, (int64_t)tile * kManyRows + (there ? mine : 0)),
+                   there, a.few.flip, lane);
     const int page0 = begin >> shift;
     for (int i = threadIdx.x; i < ((end - 1) >> shift) - page0 + 1; i += kManyThreads)
         s_pages[i] = a.prefix[page0 + i];
     __syncthreads();
 
-    h8 q[D / 16];
-    load_rows32<D>(q, a.few.Q,
-                   query_row(a.few.q, head, (int64_t)tile * kManyRows + (there ? mine : 0)),
-                   there, a.few.flip, lane);
     f16v o[D / 32];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) o[d] = zero16();
     float m_run = -INFINITY, l_run = 0.f;
     int ref = 0;  // o holds multiples of 2^(ref - 127)
 
-    // Two tiles are on their way at a time: one would have to come within the time
-    // that another is worked on (@@ us instead of @@ for 16,384 keys and 512
-    // rows of 128 per key head, 8 key heads).
     constexpr int kSets = code_sets(D);
     u4 kr[kSets][kLoads], vr[kSets][kLoads];
-    int ke[2] = {0, 0}, ve[2] = {0, 0};
-    bool ok[2] = {false, false};   // of the key that this thread looks after
-    uint32_t missing[2] = {0, 0};  // of its pieces
-    // Row of the cache of a key of the range, or -1.
-    auto place = [&](int key) -> int64_t {
-        if (key >= end) return -1;
-        const int page = s_pages[(key >> shift) - page0];
-        if (page < 0 || page >= a.few.n_pages) return -1;
-        return (((int64_t)page * a.few.n_kv + head) << shift) + (key & ((1 << shift) - 1));
+    bool ok[kSets];  // whether the key that this lane looks after is there
+    uint32_t ke[kSets], ve[kSets];
+    // Of the tiles in LDS: the keys that are there, a bit each, what their scores
+    // are multiplied by, and the power that their values are relative to.
+    uint64_t keys[2];
+    float times[2];
+    int top[2], most = 0;
+    // Row of the cache of a key of the range; of one that is not there any row.
+    auto place = [&](int key, bool *there) -> int64_t {
+        const int page = s_pages[(min(key, end - 1) >> shift) - page0];
+        *there = key < end && (unsigned)page < (unsigned)a.few.n_pages;
+        return (((int64_t)(*there ? page : 0) * a.few.n_kv + head) << shift) +
+               (key & ((1 << shift) - 1));
     };
     auto fetch = [&](int t, auto b) {
         constexpr int w = kSets > 1 ? decltype(b)::kIndex : 0;
@@ -107,48 +121,43 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
         for (int j = 0; j < kLoads; ++j) {
             const int f = (int)threadIdx.x + kManyThreads * j;
             const int row = kEven ? f / kCodes : min(f / kCodes, kKeys - 1);
-            // (a key that is not there reads the cache's first row, and is left out)
-            const int64_t r = place(first + row);
-            const int64_t at = (r < 0 ? 0 : r) * D + f % kCodes * 16;
+            bool there;
+            const int64_t at = place(first + row, &there) * D + f % kCodes * 16;
             kr[w][j] = *reinterpret_cast<const u4 *>(a.few.k + at);
             vr[w][j] = *reinterpret_cast<const u4 *>(a.few.v + at);
-            missing[w] = (j ? missing[w] : 0u) | (r < 0 ? 1u << j : 0u);
         }
-        const int64_t r = place(first + (int)threadIdx.x % kKeys);
-        ok[w] = r >= 0;
-        ke[w] = a.few.k_exp[r < 0 ? 0 : r];
-        ve[w] = a.few.v_exp[r < 0 ? 0 : r];
+        const int64_t r = place(first + (int)threadIdx.x % kKeys, &ok[w]);
+        ke[w] = a.few.k_exp[r];
+        ve[w] = a.few.v_exp[r];
     };
     auto put = [&](auto b) {
         constexpr int w = kSets > 1 ? decltype(b)::kIndex : 0;
-        CodeTile<D> &to = b.kIndex ? s1 : s0;
+        constexpr int at = b.kIndex;
+        CodeTile<D> &to = at ? s1 : s0;
+        const int mine = ok[w] ? (int)(ke[w] | ve[w] << 16) : -1;  // its powers, or -1
+        keys[at] = __ballot(mine >= 0);  // (of 32 keys: each twice)
+        const uint32_t tops = wave_max2(mine < 0 ? 0 : mine);
+        const int key_top = tops & 255;
+        most = max(most, (int)(tops >> 16));
+        top[at] = most;
+        times[at] = fminf(__builtin_ldexpf(a.few.sl2, key_top - 127), 0x1.fffffep127f);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int f = (int)threadIdx.x + kManyThreads * j, row = f / kCodes;
+            const int its = __builtin_amdgcn_ds_bpermute(4 * row, mine);
             if (!kEven && row >= kKeys) continue;
             const int c = f % kCodes, sw = T::swizzle(row & 31);
             // (a value that is left out has to be finite: 0 times it is added)
-            if (missing[w] >> j & 1) vr[w][j] = u4{0, 0, 0, 0};
+            if (its < 0) vr[w][j] = u4{0, 0, 0, 0};
+            const float kp = power_of(its < 0 ? 0 : (its & 255) - key_top);
+            const float vp = power_of(its < 0 ? 0 : (its >> 16) - most);
             const u2 klo = {kr[w][j][0], kr[w][j][1]}, khi = {kr[w][j][2], kr[w][j][3]};
             const u2 vlo = {vr[w][j][0], vr[w][j][1]}, vhi = {vr[w][j][2], vr[w][j][3]};
             uint8_t *pk = to.k + row * T::kStride, *pv = to.v + row * T::kStride;
-            *reinterpret_cast<h8 *>(pk + ((2 * c) ^ sw) * 16) = codes_to<kIn>(klo);
-            *reinterpret_cast<h8 *>(pk + ((2 * c + 1) ^ sw) * 16) = codes_to<kIn>(khi);
-            *reinterpret_cast<h8 *>(pv + ((2 * c) ^ sw) * 16) = codes_to<kInF16>(vlo);
-            *reinterpret_cast<h8 *>(pv + ((2 * c + 1) ^ sw) * 16) = codes_to<kInF16>(vhi);
-        }
-        if (threadIdx.x < 64) {  // (of 32 keys: twice the same)
-            const int power = ok[w] ? ve[w] : 0, top = wave_max(power);
-            const uint64_t mask = __ballot(ok[w]);
-            if ((int)threadIdx.x < kKeys) {
-                to.ck[threadIdx.x] = fminf(__builtin_ldexpf(a.few.sl2, ke[w] - 127), 0x1.fffffep127f);
-                to.fv[threadIdx.x] = __builtin_ldexpf(1.f, power - top);
-            }
-            if (threadIdx.x == 0) {
-                to.there[0] = (uint32_t)mask;
-                to.there[1] = (uint32_t)(mask >> 32);
-                to.top = top;
-            }
+            *reinterpret_cast<h8 *>(pk + ((2 * c) ^ sw) * 16) = codes_to<kIn>(klo, kp);
+            *reinterpret_cast<h8 *>(pk + ((2 * c + 1) ^ sw) * 16) = codes_to<kIn>(khi, kp);
+            *reinterpret_cast<h8 *>(pv + ((2 * c) ^ sw) * 16) = codes_to<kInF16>(vlo, vp);
+            *reinterpret_cast<h8 *>(pv + ((2 * c + 1) ^ sw) * 16) = codes_to<kInF16>(vhi, vp);
         }
     };
     auto work = [&](auto b) {
@@ -163,54 +172,43 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
             for (int h = 0; h < kBlocks; ++h)
                 s[h] = mfma32<kIn>(T::rows32(from.k, 32 * h, c, lane), q[c], s[h]);
         }
-#pragma unroll
-        for (int r = 0; r < 4 * kBlocks; ++r) {
-            const f4 c = *reinterpret_cast<const f4 *>(&from.ck[8 * r + 4 * (lane >> 5)]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[r >> 2][4 * (r & 3) + e] *= c[e];
-        }
-        const uint32_t all_there = from.there[0] & (kBlocks > 1 ? from.there[1] : ~0u);
-        if (__builtin_amdgcn_readfirstlane(all_there) != ~0u) {
+        float by = times[b.kIndex];
+        const uint64_t all = keys[b.kIndex];
+        if (kBlocks > 1 ? ~all : ~(uint32_t)all) {
 #pragma unroll
             for (int h = 0; h < kBlocks; ++h) {
-                const uint32_t mask = from.there[h] >> (4 * (lane >> 5));
+                const uint32_t mask = (uint32_t)(all >> 32 * h) >> (4 * (lane >> 5));
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (!(mask >> (8 * (e >> 2) + (e & 3)) & 1)) s[h][e] = -INFINITY;
+                    s[h][e] = mask >> (8 * (e >> 2) + (e & 3)) & 1 ? s[h][e] * by : -INFINITY;
             }
+            by = 1.f;  // (0 times infinity would be NaN)
         }
         float mx = s[0][0];
 #pragma unroll
         for (int e = 1; e < 16 * kBlocks; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
-        mx = max_xor32(mx);
+        mx = max_xor32(mx) * by;
         const float m_new = fmaxf(m_run, mx);
-        const int top = __builtin_amdgcn_readfirstlane(from.top);
         // (a maximum that has grown by less than 2^6 is not worth the products: the
         // probabilities may as well be up to 64, in f16 with the same 11 bits)
-        if (__ballot(m_new > m_run + 6.f) || top > ref) {
+        if (__ballot(m_new > m_run + 6.f) || top[b.kIndex] > ref) {
             float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
             l_run *= alpha;
-            alpha = __builtin_ldexpf(alpha, ref - max(top, ref));
-            ref = max(top, ref);
+            alpha = __builtin_ldexpf(alpha, ref - top[b.kIndex]);
+            ref = top[b.kIndex];
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) o[d] *= alpha;
             m_run = m_new;
         }
         const float m_ref = m_run == -INFINITY ? 0.f : m_run;
-        const float less = __builtin_ldexpf(1.f, top - ref);
         float sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < 4 * kBlocks; ++r) {
-            f4 f = *reinterpret_cast<const f4 *>(&from.fv[8 * r + 4 * (lane >> 5)]);
-            if (top < ref) f *= less;
+        for (int h = 0; h < kBlocks; ++h)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = 4 * (r & 3) + e;
-                const float p = __builtin_amdgcn_exp2f(s[r >> 2][i] - m_ref);
-                sum += p;
-                s[r >> 2][i] = p * f[e];
+            for (int e = 0; e < 16; ++e) {
+                s[h][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][e], by, -m_ref));
+                sum += s[h][e];
             }
-        }
         l_run += sum;
 #pragma unroll
         for (int c = 0; c < 2 * kBlocks; ++c) {

@@ -81,21 +81,22 @@ struct FewTile {
     static_assert(kFewKeys * kPieces % 64 == 0, "");
 };
 
+// Eight codes times `power`, a power of two.
 template <int kIn>
-__device__ __forceinline__ h8 codes_to(u2 c)
+__device__ __forceinline__ h8 codes_to(u2 c, float power = 1.f)
 {
     h8 out;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         if constexpr (kIn == kInBF16) {
             typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-            const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[k], 1.0f, false);
-            const b2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[k], 1.0f, true);
+            const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[k], power, false);
+            const b2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[k], power, true);
             const h2 x = __builtin_bit_cast(h2, a), y = __builtin_bit_cast(h2, b);
             out[4 * k] = x[0], out[4 * k + 1] = x[1], out[4 * k + 2] = y[0], out[4 * k + 3] = y[1];
         } else {
-            const h2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[k], 1.0f, false);
-            const h2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[k], 1.0f, true);
+            const h2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[k], power, false);
+            const h2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[k], power, true);
             out[4 * k] = a[0], out[4 * k + 1] = a[1], out[4 * k + 2] = b[0], out[4 * k + 3] = b[1];
         }
     }
