@@ -82,14 +82,19 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
  *              row-major, 16-byte aligned; O must not overlap an input
  *   lse        device fp32 [n_seqs, n_new, n_heads]: log of the sum of the
  *              exponentials (-inf, and O = 0, for a token that sees no key)
- *   table, lens  as above; keys behind the table do not take part
+ *   table, lens  as above; keys behind the table do not take part, and it has
+ *              room for 2^30 tokens at most
  *   prefix     device int32 [ceil(prefix_len / page_size)]: the pages of the
- *              prefix (its last one may end inside); NULL if prefix_len is 0
+ *              prefix (its last one may end inside); NULL if prefix_len is 0;
+ *              prefix_len <= 2^30
  *   scale      finite
  *   workspace  device, at least f3s_cache_attend_workspace_bytes(...) bytes,
  *              256-byte aligned; needs no initialisation, and calls that
  *              overlap in time need one each.  NULL if that is 0
- * Inputs must be finite.  The work is divided on the device, by the lengths
+ * Inputs must be finite.  Scores, sums and statistics are fp32; the products
+ * with V are f16, relative to the largest power of two among the values so far:
+ * beside 2^-11 of its probability a key adds an error of up to 2^-25 of the
+ * largest |value|.  The work is divided on the device, by the lengths
  * that it finds there: a captured call stays right when they change.  A prefix
  * is read once for many sequences: for 16 query rows of a key head at a time,
  * or, with many rows and much work, for 128 (environment F3S_PREFIX_ROWS=16 or

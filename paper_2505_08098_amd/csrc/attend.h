@@ -10,6 +10,8 @@ namespace f3s {
 // Keys are handed out in units of 64, at least kLeastUnits to a workgroup.
 constexpr int kUnit = 64;
 constexpr int kLeastUnits = 4;
+// Tokens of a sequence's table, or of the prefix.
+constexpr int32_t kMostTokens = 1 << 30;
 
 struct AttendArgs {
     FewArgs few;

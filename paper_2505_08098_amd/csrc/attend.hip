@@ -42,12 +42,14 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_new,
             int32_t n_heads, int32_t prefix_len, int prefix_rows, AttendArgs *a, Layout *w)
 {
+    // (a key's number and a piece's length add up to less than 2^31)
+    if ((double)n_new * n_heads * n_seqs > 0x7FFFFFFF || prefix_len > f3s::kMostTokens ||
+        (double)max_pages * c.page_size > f3s::kMostTokens ||
+        (double)max_pages * c.page_size / f3s::kUnit * n_seqs + n_seqs > 1e9)
+        return false;
     const int64_t g = n_heads / c.n_kv_heads;
     const int64_t rows = n_new * g, all = rows * n_seqs;
     const int64_t cap = (int64_t)max_pages * c.page_size;
-    if (all * c.n_kv_heads > 0x7FFFFFFF || cap > 0x7FFFFFFF ||
-        (double)cap / f3s::kUnit * n_seqs + n_seqs > 1e9)
-        return false;
     a->n_seqs = n_seqs;
     a->n_new = n_new;
     a->max_pages = max_pages;

@@ -64,7 +64,8 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
         if (ql * g > longest) longest = ql * g;
     }
     *st = F3S_ERR_TOO_LARGE;
-    if (q_ptr[n] * g > 0x7FFFFFFF || (double)q_ptr[n] * n_heads / 16 + n_heads > 2147483647.0)
+    // (a row's number and a tile add up to less than 2^31)
+    if (q_ptr[n] * g > 0x7FFFF000 || k_ptr[n] > 0x7FFFF000 || (double)q_ptr[n] * n_heads / 16 + n_heads > 2147483647.0)
         return nullptr;
     Division f, dq, dkv;
     const char *rows_env = getenv("F3S_CROSS_ROWS");

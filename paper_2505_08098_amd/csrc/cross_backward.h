@@ -159,9 +159,10 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
                                 lane);
 }
 
-// d = 96 and 128: the sums of dK and dV leave no room for both K and V beside
-// them if two waves are to share a SIMD, which is worth more (d = 128, 16 heads
-// over 4, 2 x 4,050 x 4,050: @@ us against @@ with one); V's rows stay in LDS.
+// d = 64 to 128: the sums of dK and dV leave no room for both K and V beside
+// them if two waves (three of d = 64) are to share a SIMD, which is worth more
+// (d = 128, 16 heads over 4, 2 x 4,050 x 4,050: 1,007 us against 1,424 with one
+// wave, the rest of the kernel as it then was); V's rows stay in LDS.
 constexpr bool dkv_v_in_lds(int d) { return d > 32 && d <= 128; }
 
 template <int D>

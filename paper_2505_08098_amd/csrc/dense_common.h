@@ -125,20 +125,4 @@ f3s_status_t set_status(f3s_status_t s);
 f3s_status_t status_of(hipError_t e);
 hipError_t limited_malloc(void **p, size_t bytes);
 
-// Makes a device current for a scope (a plan's, or the stream's).
-struct OnDevice {
-    int prev = -1;
-    bool ok = false;
-    explicit OnDevice(int device)
-    {
-        if (hipGetDevice(&prev) != hipSuccess) return;
-        ok = prev == device || hipSetDevice(device) == hipSuccess;
-        if (prev == device) prev = -1;
-    }
-    ~OnDevice()
-    {
-        if (prev >= 0) (void)hipSetDevice(prev);
-    }
-};
-
 }  // namespace f3s

@@ -63,18 +63,26 @@ struct Division {
     // The launch that joins them, 5 us, where a unit takes 1.1 (f16, d = 64).
     static constexpr double kLaunch = 5;
     static constexpr int64_t kMostPieces = 16;
+    // Items of a pass (32 bytes each); a batch of more is refused.
+    static constexpr double kMostItems = 1 << 26;
 
     // `slots`: workgroups that run at once; pieces have `least` rows or more.
     void make(std::vector<Range> ranges, int32_t heads, int64_t tile, int64_t unit,
               int64_t least, int64_t slots)
     {
+        double tiles = 0;
+        for (const Range &r : ranges) tiles += (double)ceil_div(r.rows, tile) * heads;
+        if (tiles > kMostItems) {
+            parts = INT64_MAX;
+            return;
+        }
         // the longest first: what is left for the end are short ones
         std::stable_sort(ranges.begin(), ranges.end(),
                          [](const Range &a, const Range &b) { return a.others > b.others; });
         const int64_t top = ranges.empty() ? 1 : ceil_div(ranges[0].others, unit);
         int64_t per = top < 1 ? 1 : top;
         double best = time(ranges, heads, tile, unit, slots, per);
-        for (int64_t k = 2; k <= top; ++k) {
+        for (int64_t k = 2; k <= top; k += k > kMostPieces ? k / kMostPieces : 1) {
             // (as many pieces as it takes to fill the GPU, and then some)
             const int64_t p = ceil_div(top, k);
             if (p * unit < least) break;

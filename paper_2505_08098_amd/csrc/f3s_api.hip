@@ -39,9 +39,9 @@ size_t alloc_limit()
     return e && *e ? (size_t)strtoull(e, nullptr, 10) : ~(size_t)0;
 }
 
-// (for the library's other entry points)
 }  // namespace
 
+// For the entry points in the other files.
 namespace f3s {
 f3s_status_t set_status(f3s_status_t s) { return s == F3S_OK ? s : fail(s); }
 f3s_status_t status_of(hipError_t e) { return from_hip(e); }

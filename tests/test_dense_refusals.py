@@ -2,6 +2,7 @@
 every refusal comes before any device work."""
 import ctypes
 import math
+import time
 
 import numpy as np
 import pytest
@@ -45,7 +46,7 @@ def _plan(lib, q, k, ql=None, kl=None, n=None, heads=4, kv=2, d=64):
     (dict(q=[0, 9, 3]), INVALID), (dict(k=[0, 9, 3]), INVALID),
     (dict(ql=[3, 7]), INVALID), (dict(ql=[-1, 3]), INVALID),
     (dict(kl=[5, 5]), INVALID), (dict(kl=[0, -4]), INVALID),
-    (dict(q=[0, 3, 2147483647]), TOO_LARGE),
+    (dict(q=[0, 3, 2147483647]), TOO_LARGE), (dict(k=[0, 3, 2147483647]), TOO_LARGE),
     (dict(), HIP),
 ])
 def test_cross_plan(lib, change, status):
@@ -151,6 +152,8 @@ def test_write_takes_no_null_rows_and_no_fp32(lib):
     (dict(lse=17 * A), INVALID), (dict(O=32 * A), INVALID),
     (dict(ws=None), INVALID), (dict(ws=32 * A + 16), INVALID), (dict(nbytes=4096), INVALID),
     (dict(B=1 << 20, n=1 << 11), TOO_LARGE), (dict(pages=1 << 28), TOO_LARGE),
+    (dict(prefix=9 * A, P=(1 << 30) + 1), TOO_LARGE),
+    (dict(B=(1 << 31) - 1, n=(1 << 31) - 1, heads=1 << 30), TOO_LARGE),
     (dict(B=0), OK), (dict(n=0), OK),
     (dict(), HIP), (dict(prefix=9 * A, P=5), HIP),
     (dict(pages=16, ws=None, nbytes=0), HIP),        # short tables need no workspace
@@ -198,3 +201,25 @@ def test_cache_arguments():
         dense.Cache(e, e, e, e)
     with pytest.raises(ValueError):
         dense.Cache([1], t, e, e)
+
+
+@pytest.mark.parametrize("q_ptr, k_ptr, heads, kv", [
+    ([0, 1], [0, 2**31 - 1], 65535, 65535),        # 2^37 keys of all heads
+    ([0, 2**31 - 1], [0, 1], 1000, 1000),          # 2^31 rows of many heads
+    (range(40001), range(40001), 8000, 8000),      # a tile for each of 3.2e8 rows
+])
+def test_plans_of_too_many_tiles_are_refused_at_once(lib, q_ptr, k_ptr, heads, kv):
+    """Before lists of them are made, which memory would not hold."""
+    start = time.monotonic()
+    assert _plan(lib, q_ptr, k_ptr, heads=heads, kv=kv, d=32) == TOO_LARGE
+    assert time.monotonic() - start < 10
+
+
+def test_a_plan_of_many_sequences_is_divided_soon(lib):
+    """200,000 sequences, one with a million keys: without a GPU the plan then
+    fails, for want of one."""
+    n = 200000
+    k = [0] + [10**6 + 100 * b for b in range(n)]
+    start = time.monotonic()
+    assert _plan(lib, range(n + 1), k, heads=4, kv=1) == HIP
+    assert time.monotonic() - start < 10
