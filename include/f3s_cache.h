@@ -52,8 +52,8 @@ typedef struct {
  *   lens       device int32 [n_seqs], the lengths after this call
  * Two rows of one call must not lie at the same place (a page named twice):
  * what such a place then holds is not defined.  K and V must not overlap the
- * cache.  Asynchronous on `stream`; no
- * allocation, no synchronisation.
+ * cache.  F3S_ERR_TOO_LARGE beyond 2^27 rows (sequences, tokens, key heads).
+ * Asynchronous on `stream`; no allocation, no synchronisation.
  */
 f3s_status_t f3s_cache_write(const f3s_cache_t *cache, const void *K, const void *V,
                              f3s_dtype_t dtype, const int32_t *table, int32_t max_pages,

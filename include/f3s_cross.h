@@ -36,8 +36,8 @@ typedef struct f3s_cross_plan_s *f3s_cross_plan_t;
  * F3S_CROSS_ROWS=16 or 128, read here, forces one).
  * The plan copies what it needs.  Synchronous on the current device's null
  * stream.  NULL on error (f3s_last_error); F3S_ERR_TOO_LARGE if the batch has
- * more than 2^31 - 2^12 rows of K, or query rows per key head, or more than 2^26
- * tiles of rows.
+ * more than 2^31 - 2^12 rows of K, or query rows per key head, or more than 2^23
+ * tiles of rows (or pieces of them).
  */
 f3s_cross_plan_t f3s_cross_plan(const int32_t *q_ptr, const int32_t *k_ptr,
                                 const int32_t *q_len, const int32_t *k_len, int32_t n_seqs,

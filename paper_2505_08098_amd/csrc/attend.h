@@ -145,7 +145,8 @@ __global__ __launch_bounds__(64 * kFewWaves, few_waves(D, true)) void k_attend(A
         it.end = min(o.keys, item_unit(o.units, k + 1, o.items) * kUnit);
         it.causal = a.n_new > 1;
         it.first = rb * kFewRows;
-        it.limit = (int)cache_position(a.lens[o.seq], a.n_new, 0) + 1;
+        // (behind the keys that there are, any limit does)
+        it.limit = (int)min(cache_position(a.lens[o.seq], a.n_new, 0) + 1, (int64_t)o.keys);
         it.part = a.direct ? -1
                            : ((int64_t)i * a.few.n_kv + it.head) * a.rows + rb * kFewRows;
     }

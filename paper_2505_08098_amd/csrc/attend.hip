@@ -107,8 +107,10 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     w->prefix_rows = (int64_t)a->prefix_splits * c.n_kv_heads * all;
     a->prefix_part = w->own_rows;
     const int64_t n = w->own_rows + w->prefix_rows;
-    if (items * a->row_blocks +
-            (int64_t)a->prefix_splits * c.n_kv_heads * a->prefix_blocks > 0x7FFFFFFF)
+    // (a join has four rows or more to a workgroup where there are many)
+    if (items * a->row_blocks + (int64_t)a->prefix_splits * c.n_kv_heads * a->prefix_blocks >
+            f3s::kMostGrid ||
+        all * c.n_kv_heads / 4 >= f3s::kMostGrid)
         return false;
     w->ml = round256((size_t)n * c.d * 4);
     w->desc = w->ml + round256((size_t)n * 8);

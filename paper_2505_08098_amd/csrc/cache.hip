@@ -234,7 +234,9 @@ f3s_status_t row_args(const f3s_cache_t *c, const int32_t *table, int32_t max_pa
     if (n_seqs == 0 || n_new == 0) return F3S_OK;
     if (!lens || !f3s::aligned(lens, 4) || (max_pages && !table) || !f3s::aligned(table, 4))
         return F3S_ERR_INVALID_VALUE;
-    if ((double)n_seqs * n_new * c->n_kv_heads > 2147483647.0) return F3S_ERR_TOO_LARGE;
+    if ((double)n_seqs * n_new * c->n_kv_heads >
+        (double)f3s::kMostGrid * (f3s::kThreads / f3s::lanes_of(c->d)))
+        return F3S_ERR_TOO_LARGE;
     *a = f3s::RowArgs{*c, table, lens, max_pages, __builtin_ctz(c->page_size), n_new,
                       (uint32_t)n_seqs * (uint32_t)n_new * (uint32_t)c->n_kv_heads};
     return F3S_OK;

@@ -14,6 +14,9 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef int i2v __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i2v lds_i2;
 
+// Workgroups of 256 threads that one launch takes (fewer than 2^32 threads).
+constexpr int64_t kMostGrid = 0xFFFFFFFF / 256;
+
 // The query rows of one key head: row r (over all tokens) is token r / g,
 // query head kh * g + r % g, so the g rows of a token lie one behind the other.
 struct QueryRows {

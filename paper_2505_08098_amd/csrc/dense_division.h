@@ -63,8 +63,8 @@ struct Division {
     // The launch that joins them, 5 us, where a unit takes 1.1 (f16, d = 64).
     static constexpr double kLaunch = 5;
     static constexpr int64_t kMostPieces = 16;
-    // Items of a pass (32 bytes each); a batch of more is refused.
-    static constexpr double kMostItems = 1 << 26;
+    // Tiles of a pass; a batch of more is refused.
+    static constexpr double kMostTiles = 1 << 23;
 
     // `slots`: workgroups that run at once; pieces have `least` rows or more.
     void make(std::vector<Range> ranges, int32_t heads, int64_t tile, int64_t unit,
@@ -72,7 +72,7 @@ struct Division {
     {
         double tiles = 0;
         for (const Range &r : ranges) tiles += (double)ceil_div(r.rows, tile) * heads;
-        if (tiles > kMostItems) {
+        if (tiles > kMostTiles) {
             parts = INT64_MAX;
             return;
         }
@@ -129,8 +129,9 @@ struct Division {
 
     bool fits() const
     {
-        return parts <= 0x7FFFFFFF && items.size() <= 0x7FFFFFFF &&
-               (int64_t)merges.size() * merge_rows <= 0x7FFFFFFF;
+        // (two workgroups to an item, one to four rows of a merge at most)
+        return parts <= 0x7FFFFFFF && 2 * (int64_t)items.size() <= kMostGrid &&
+               (int64_t)merges.size() * (merge_rows / 4 + 1) <= kMostGrid;
     }
 };
 

@@ -117,7 +117,7 @@ def test_caches(lib, change, status):
     (dict(table=7 * A + 1), INVALID), (dict(dtype=FP8), UNSUPPORTED), (dict(dtype=9), UNSUPPORTED),
     (dict(K=5 * A + 8), INVALID), (dict(V=6 * A + 2), INVALID),
     (dict(K=A), INVALID), (dict(V=4 * A), INVALID), (dict(K=2 * A - 16), INVALID),  # the cache
-    (dict(B=1 << 20, n=1 << 11), TOO_LARGE),
+    (dict(B=1 << 20, n=1 << 11), TOO_LARGE), (dict(B=1 << 19, n=1 << 10), TOO_LARGE),
     (dict(B=0), OK), (dict(n=0), OK), (dict(B=0, lens=None, table=None), OK),
     (dict(), HIP),
 ])
@@ -152,6 +152,7 @@ def test_write_takes_no_null_rows_and_no_fp32(lib):
     (dict(lse=17 * A), INVALID), (dict(O=32 * A), INVALID),
     (dict(ws=None), INVALID), (dict(ws=32 * A + 16), INVALID), (dict(nbytes=4096), INVALID),
     (dict(B=1 << 20, n=1 << 11), TOO_LARGE), (dict(pages=1 << 28), TOO_LARGE),
+    (dict(B=1 << 17, n=1 << 8), TOO_LARGE),
     (dict(prefix=9 * A, P=(1 << 30) + 1), TOO_LARGE),
     (dict(B=(1 << 31) - 1, n=(1 << 31) - 1, heads=1 << 30), TOO_LARGE),
     (dict(B=0), OK), (dict(n=0), OK),
