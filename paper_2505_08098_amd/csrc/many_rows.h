@@ -120,8 +120,8 @@ struct ManyTile {
     static __device__ __forceinline__ h8 rows32(const uint8_t *tile, int row, int c, int lane)
     {
         const int i = lane & 31;
-        return *reinterpret_cast<const h8 *>(tile + row * kStride + i * kStride +
-                                             ((2 * c + (lane >> 5)) ^ swizzle(i)) * 16);
+        const int at = (row + i) * kStride + ((2 * c + (lane >> 5)) ^ swizzle(i)) * 16;
+        return *reinterpret_cast<const h8 *>(tile + at);
     }
     // Operand with elements d .. d + 31 as rows and the tile's rows row .. + 15 as
     // reduction slots (d a multiple of 32, row of 16), in the order in which a lane
@@ -131,11 +131,13 @@ struct ManyTile {
     {
         const int s = lane & 15, i = 4 * (lane >> 5) + (s >> 2);
         const int piece = d / 8 + 2 * (lane >> 4 & 1) + (s >> 1 & 1);
-        const uint8_t *p = tile + row * kStride + 8 * (s & 1);
-        const uint8_t *lo = p + i * kStride + (piece ^ swizzle(row % 32 + i)) * 16;
-        const uint8_t *hi = p + (i + 8) * kStride + (piece ^ swizzle(row % 32 + i + 8)) * 16;
-        return cat44(lds_read_tr(reinterpret_cast<const _Float16 *>(lo)),
-                     lds_read_tr(reinterpret_cast<const _Float16 *>(hi)));
+        // (one sum each, not a chain: behind five steps from a variable the compiler
+        // no longer tells it from the other buffer, and waits for the loads into that)
+        const int lo = (row + i) * kStride + (piece ^ swizzle(row % 32 + i)) * 16 + 8 * (s & 1);
+        const int hi =
+            (row + i + 8) * kStride + (piece ^ swizzle(row % 32 + i + 8)) * 16 + 8 * (s & 1);
+        return cat44(lds_read_tr(reinterpret_cast<const _Float16 *>(tile + lo)),
+                     lds_read_tr(reinterpret_cast<const _Float16 *>(tile + hi)));
     }
 };
 
