@@ -63,22 +63,16 @@ struct Division {
     // The launch that joins them, 5 us, where a unit takes 1.1 (f16, d = 64).
     static constexpr double kLaunch = 5;
     static constexpr int64_t kMostPieces = 16;
+    // Times that a division by a second rule has to beat the first's (they are
+    // estimates).
+    static constexpr double kWorth = 0.95;
     // Tiles of a pass; a batch of more is refused.
     static constexpr double kMostTiles = 1 << 23;
 
-    // `slots`: workgroups that run at once; pieces have `least` rows or more.
-    void make(std::vector<Range> ranges, int32_t heads, int64_t tile, int64_t unit,
-              int64_t least, int64_t slots)
+    // Units of a piece, where all are divided alike, that take the least time.
+    static int64_t best_pieces(const std::vector<Range> &ranges, int32_t heads, int64_t tile,
+                               int64_t unit, int64_t least, int64_t slots, double *takes)
     {
-        double tiles = 0;
-        for (const Range &r : ranges) tiles += (double)ceil_div(r.rows, tile) * heads;
-        if (tiles > kMostTiles) {
-            parts = INT64_MAX;
-            return;
-        }
-        // the longest first: what is left for the end are short ones
-        std::stable_sort(ranges.begin(), ranges.end(),
-                         [](const Range &a, const Range &b) { return a.others > b.others; });
         const int64_t top = ranges.empty() ? 1 : ceil_div(ranges[0].others, unit);
         int64_t per = top < 1 ? 1 : top;
         double best = time(ranges, heads, tile, unit, slots, per);
@@ -93,14 +87,61 @@ struct Division {
             }
             if (k > kMostPieces && k * heads > 4 * slots) break;
         }
+        *takes = best;
+        return per;
+    }
+
+    // `slots`: workgroups that run at once; pieces have `least` rows or more.
+    void make(std::vector<Range> ranges, int32_t heads, int64_t tile, int64_t unit,
+              int64_t least, int64_t slots)
+    {
+        double tiles = 0;
+        for (const Range &r : ranges) tiles += (double)ceil_div(r.rows, tile) * heads;
+        if (tiles > kMostTiles) {
+            parts = INT64_MAX;
+            return;
+        }
+        // the longest first: what is left for the end are short ones
+        std::stable_sort(ranges.begin(), ranges.end(),
+                         [](const Range &a, const Range &b) { return a.others > b.others; });
+        double best = 0;
+        int64_t per = best_pieces(ranges, heads, tile, unit, least, slots, &best);
+        std::vector<int64_t> most(ranges.size(), per);  // units of a range's pieces
+        // A few tiles too many cost a round.  What is left of the ranges behind
+        // their whole tiles is then better cut small and run behind the others:
+        // 260 tiles of 253 units on 512 places as 512 halves and 4 x 64 pieces
+        // instead of 260 x 11 pieces (dK and dV of 2 x 4,050 x 4,050, 16 heads of
+        // 128 over 4: 558 us and 22 for their sums instead of 616 and 46).
+        std::vector<Range> whole, rest;
+        for (const Range &r : ranges) {
+            const int64_t n = r.rows / tile * tile;
+            if (n) whole.push_back({r.row, n, r.other, r.others});
+            if (n < r.rows) rest.push_back({r.row + n, r.rows - n, r.other, r.others});
+        }
+        if (!whole.empty() && !rest.empty()) {
+            const int64_t small = ceil_div(least, unit);
+            double t = 0, n = 0;
+            per = best_pieces(whole, heads, tile, unit, least, slots, &t);
+            for (const Range &r : rest)
+                n += (double)pieces(ceil_div(r.others, unit), small) * heads;
+            t += (double)ceil_div((int64_t)n, slots) * (small + kOver + kJoin) +
+                 (split(whole, unit, per) ? 0 : kLaunch);
+            if (t < kWorth * best) {
+                most.assign(whole.size(), per);
+                most.resize(whole.size() + rest.size(), small);
+                ranges.swap(whole);
+                ranges.insert(ranges.end(), rest.begin(), rest.end());
+            }
+        }
         // The tiles of a sequence, head and piece walk the same rows: they come
         // one behind the other and run side by side, in step, so that a row is
         // fetched once for many of them.  (Shares cut wherever they are equal,
         // which are out of step, took 1.5 times as long; one consecutive range
         // of the items for each XCD instead of every eighth 10% longer: forward,
         // 2 x 4,050 tokens, 32 heads of 128 over 8, 8,100 keys.)
-        for (const Range &r : ranges) {
-            const int64_t units = ceil_div(r.others, unit), n = pieces(units, per);
+        for (size_t i = 0; i < ranges.size(); ++i) {
+            const Range &r = ranges[i];
+            const int64_t units = ceil_div(r.others, unit), n = pieces(units, most[i]);
             for (int32_t h = 0; h < heads; ++h) {
                 const int64_t part = parts;
                 for (int64_t k = 0; k < n; ++k) {

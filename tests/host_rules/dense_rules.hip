@@ -117,12 +117,21 @@ static void divisions()
         for (const DenseItem &i : e.items)
             if (i.part >= 0) CHECK(i.others >= 64);
     }
-    // 260 tiles on 512 places: not 520 halves (two rounds), but pieces that fill
-    // their rounds
+    // 260 tiles on 512 places: not 520 halves (two rounds), but 512, and the four
+    // behind them in short pieces
     Division d;
     d.make({{0, 4001, 0, 4095}, {4001, 4099, 4095, 4001}}, 4, 128, 64, 256, 512);
-    const double n = (double)d.merges.front().count;
-    CHECK(std::ceil(260 * n / 512) / n < 0.7);
+    int64_t longest = 0, whole = 0;
+    for (const DenseItem &i : d.items) {
+        if (i.others > longest) longest = i.others;
+        whole += i.rows == 128;
+    }
+    check_division(d, {{0, 4001, 0, 4095}, {4001, 4099, 4095, 4001}}, 4, 128, 64);
+    CHECK(whole <= 512 || longest <= 1600);
+    // where all rounds are full but for a few, nothing is gained
+    Division g;
+    g.make({{0, 128 * 100 + 5, 0, 4096}}, 8, 128, 64, 256, 512);
+    check_division(g, {{0, 128 * 100 + 5, 0, 4096}}, 8, 128, 64);
     // a few long tiles of different lengths: divided, however short the others are
     Division f;
     f.make({{0, 59, 0, 1016}, {59, 40, 1016, 760}, {99, 20, 1776, 512}}, 2, 128, 64, 256, 512);
