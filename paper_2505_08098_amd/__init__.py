@@ -4,6 +4,10 @@
     plan = f3s.Plan(row_ptr, col_idx, N)          # device int32 CSR
     O = f3s.run(plan, Q, K, V, scale=1/d**0.5)    # fp16 in, fp32 out
 
+and dense attention for decoders (see ``dense``): ``CrossPlan``, ``cross_forward``,
+``cross_backward`` over an encoder's states; ``Cache``, ``cache_write``, ``cache_read``,
+``cache_attend`` over an 8-bit key/value cache.
+
 The compute path is the HIP library only (see ``binding``); ``workloads``
 holds the seeded synthetic inputs.
 """
