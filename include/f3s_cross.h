@@ -79,7 +79,10 @@ f3s_status_t f3s_cross_forward(f3s_cross_plan_t plan, const void *Q, const void 
  * dK and dV summed over the query heads of a key head.  dO, dQ as Q; dK, dV
  * as K; every element is written.  P and dS enter the products in dtype (fp16
  * gradients need the usual scaling of the loss: a dS below 2^-14 loses bits);
- * sums in fp32, gradients rounded once.  Otherwise as the forward.
+ * sums in fp32, gradients rounded once.  delta comes from the rounded O: where
+ * one key has nearly all of a row's probability, dS is what is left of two equal
+ * numbers and keeps that rounding (2^-9 of |dO . O| in bf16).  Otherwise as the
+ * forward.
  */
 f3s_status_t f3s_cross_backward(f3s_cross_plan_t plan, const void *Q, const void *K,
                                 const void *V, f3s_dtype_t dtype, const void *O,

@@ -18,11 +18,13 @@ constexpr int64_t kUnits = 256;  // compute units
 constexpr int64_t kWorkgroups = 8 * kUnits;
 // The prefix takes the kernel of many rows from more than this many query rows
 // of a key head on (below, its tiles would be half empty), and from so many
-// operations that its higher rate pays for a launch of its own (whole calls,
-// 8 key heads of 128: 128 rows and 16,384 keys, 8.6 G, 44.5 us instead of 53.4;
-// 256 rows and 4,096 keys, 4.3 G, 38.5 instead of 37.0).
+// scores (rows x keys) that its higher rate pays for a launch of its own.  Calls
+// on short own keys, us with 16 rows and with 128:
+//   8 key heads of 128, 128 rows: 4.2 M scores 24.4 and 25.4, 8.4 M 36.2 and 30.5
+//   8 key heads of  64, 128 rows: 4.2 M scores 18.5 and 19.4, 8.4 M 25.0 and 21.9
+//   4 key heads of 256, 256 rows: 4.2 M scores 38.0 and 44.8, 8.4 M 59.4 and 54.7
 constexpr int64_t kFewPrefixRows = 64;
-constexpr double kManyWork = 6e9;
+constexpr int64_t kManyScores = 6000000;
 // What a piece of the prefix costs beside its keys (queries, partial results),
 // in units of 64 keys.
 constexpr int64_t kPieceCost = 3;
@@ -70,7 +72,7 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
         a->prefix_many = prefix_rows == f3s::kManyRows;
     else
         a->prefix_many = all > kFewPrefixRows &&
-                         4.0 * (double)all * prefix_len * c.d * c.n_kv_heads > kManyWork;
+                         (double)all * prefix_len * c.n_kv_heads > kManyScores;
     a->prefix_many = a->prefix_many && prefix_len;
     a->prefix_blocks =
         (int32_t)ceil_div(all, a->prefix_many ? f3s::kManyRows : f3s::kFewRows);

@@ -12,9 +12,11 @@
 // P comes from lse, so nothing of the size of the scores is stored: 7 products
 // instead of 5.  As in the forward, the accumulator of the first products is
 // the operand of the second in place, each wave has 32 rows of its own side in
-// registers, and tiles of 64 rows of the other side pass through LDS for all
-// four waves in two buffers.  The matrix units and LDS reads (one operand of
-// every product) are the bound.
+// registers, and tiles of 32 rows of the other side (d = 32: 64) pass through LDS
+// for all four waves in two buffers.  As in the forward power is the bound, and in
+// k_cross_dkv LDS reads (one operand of every product, and V): 2 x 4,050 x 4,050,
+// 16 heads of 128 over 4, bf16, takes 413 us for dQ and 558 for dK and dV, 970
+// TFLOP/s of the 7 products.
 #pragma once
 
 #include "many_rows.h"

@@ -18,6 +18,10 @@
 // that of a value its probability, taken relative to the largest power so far
 // (both exactly), so that P V runs in f16 with 11 bits of P whatever the
 // values' size.
+//
+// One token of 64 sequences of 1,500 to 4,097 keys, 8 key heads of 128 in bf16: 135
+// us, 5.5 TB/s; of 500 to 8,192 cached keys: 116 us, 4.9 TB/s (a copy of 2 GiB
+// moves 4.8).
 #pragma once
 
 #include "dense_common.h"

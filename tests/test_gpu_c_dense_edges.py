@@ -492,6 +492,37 @@ def test_many_new_tokens_and_many_sequences(gpu, B, n, lens):
     _attend_case(gpu, torch.float16, 32, 32, 1, 2, lens, n, 21)
 
 
+def test_thousands_of_sequences(gpu):
+    """More sequences than a wave looks at in one go: every one as if alone."""
+    gen = torch.Generator().manual_seed(31)
+    kv, d, page, B = 2, 64, 16, 5000
+    table7, n_pages = _table(gen, 7, 4)
+    cache = _cache(gpu, n_pages, page, kv, d)
+    x = [_rows(gen, (7, 64, kv, d), torch.float16).to(DEV) for _ in "KV"]
+    gpu.cache_write(cache, *x, table7.to(DEV), _int32([64] * 7))
+    lens7 = [0, 1, 63, 64, 17, 40, 33]
+    Q7 = torch.randn((7, 1, 4, d), generator=gen).half()
+    pick = torch.randint(0, 7, (B,), generator=gen)
+    lens = torch.tensor(lens7)[pick]
+    O, lse = gpu.cache_attend(cache, Q7[pick].to(DEV), table7[pick].to(DEV),
+                              lens.to(torch.int32).to(DEV))
+    first = [int((pick == k).nonzero()[0]) for k in range(7)]
+    _compare(cache, Q7, table7, lens7, None, 0, 0.125, O[first], lse[first])
+    # (a sequence this short is one piece wherever it stands)
+    at = torch.tensor(first)[pick].to(DEV)
+    assert torch.equal(O, O[at]) and torch.equal(lse, lse[at])
+    # the same keys as one plan's: sequences of one token over 0 .. 64 rows
+    plan = gpu.CrossPlan(range(B + 1), _sums(lens.tolist()), 4, kv, d)
+    K, V = (torch.cat([x[w][int(k), :lens7[int(k)]] for k in pick]) for w in range(2))
+    C, clse = gpu.cross_forward(plan, Q7[pick].to(DEV).view(B, 4, d), K, V)
+    assert torch.equal(C, C[at]) and torch.equal(clse, clse[at])
+    G = torch.randn((7, 4, d), generator=gen).half()[pick].to(DEV)
+    grads = gpu.cross_backward(plan, Q7[pick].to(DEV).view(B, 4, d), K, V, C, G, clse)
+    assert torch.equal(grads[0], grads[0][at])
+    for got in grads[1:]:
+        assert bool(torch.isfinite(got).all())
+
+
 # ---- all of it together -------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", TYPES)
