@@ -252,8 +252,8 @@ class Cache:
     """Pages of keys and values in 8 bits: codes ``k`` and ``v``
     (float8_e4m3fn, [pages, kv_heads, page_size, d]) and a power of two for
     each row, ``k_exp`` and ``v_exp`` (uint8, [pages, kv_heads, page_size]:
-    value = code * 2^(exp - 127)).  The tensors are the caller's and may be
-    moved or copied like any others."""
+    value = code * 2^(exp - 127)).  The tensors are the caller's and stay where
+    they are: another place for them is another Cache."""
 
     def __init__(self, k, v, k_exp, v_exp):
         if not isinstance(k, torch.Tensor) or k.dim() != 4:
@@ -264,7 +264,7 @@ class Cache:
             _check_device_tensor(t, n, torch.uint8, k.device)
         if v.shape != k.shape or k_exp.shape != k.shape[:3] or v_exp.shape != k.shape[:3]:
             raise ValueError("k and v must share one shape, k_exp and v_exp its first three")
-        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self._tensors = (k, v, k_exp, v_exp)
         self.device = k.device
         self.n_pages, self.kv_heads, self.page_size, self.d = k.shape
         if self.n_pages > 2**31 - 1:
@@ -275,6 +275,12 @@ class Cache:
         self._ref = ctypes.byref(self._struct)
         self.scale = 1.0 / math.sqrt(self.d) if self.d else 1.0
         self._bytes = {}  # workspace of an attend call, by its sizes
+
+    # (read-only: the struct holds their addresses)
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    k_exp = property(lambda self: self._tensors[2])
+    v_exp = property(lambda self: self._tensors[3])
 
     @classmethod
     def empty(cls, n_pages, page_size, kv_heads, d, device="cuda"):

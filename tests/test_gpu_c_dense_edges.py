@@ -272,6 +272,8 @@ def test_binding_refusals(gpu):
         gpu.Cache(codes.transpose(1, 2), cache.v, cache.k_exp, cache.v_exp)
     with pytest.raises(TypeError):
         gpu.Cache(codes.view(torch.uint8), cache.v, cache.k_exp, cache.v_exp)
+    with pytest.raises(AttributeError):
+        cache.k = cache.v                # (calls would go on reading the old place)
     odd = gpu.Cache.empty(2, 24, 1, 64)
     with pytest.raises(gpu.F3SError):
         gpu.cache_write(odd, K[:, :, :1].contiguous(), K[:, :, :1].contiguous(), table, lens)
@@ -565,3 +567,14 @@ def test_a_decoder_generates(gpu, dtype):
                               EV[j, h // g].double().cpu(), 0.125, u)
                 close(C[b: b + 1, h], f["O"], f["O_tol"], ("cross", t, b, h))
                 close(clse[b: b + 1, h], f["lse"], f["lse_tol"], ("lse", t, b, h))
+
+
+# ---- failures ------------------------------------------------------------------------------
+
+def test_a_plan_out_of_memory(gpu, monkeypatch):
+    """No room for a plan's lists is an error that the next plan does not feel."""
+    monkeypatch.setenv("F3S_ALLOC_LIMIT_BYTES", "64")
+    with pytest.raises(gpu.F3SError, match="OUT_OF_MEMORY"):
+        gpu.CrossPlan([0, 300], [0, 300], 4, 2, 64)
+    monkeypatch.delenv("F3S_ALLOC_LIMIT_BYTES")
+    _case(gpu, torch.float16, 64, 2, 2, [30, 3], [70, 33])
