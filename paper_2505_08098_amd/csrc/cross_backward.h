@@ -47,22 +47,15 @@ __device__ __forceinline__ f4 quad(const f16v &x, int k)
     return f4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
 }
 
-// An O^T-like accumulator's row, scaled and rounded, or as it is into partial sums.
-template <int D, int kIn, int D0, int D1>
-__device__ __forceinline__ void store_row(const f16v (&x)[(D1 - D0) / 32], float scale, void *to,
-                                          int64_t at, float *part, int lane)
+// An O^T-like accumulator's row, as it is, into partial sums.
+template <int kCols>
+__device__ __forceinline__ void store_part(const f16v (&x)[kCols / 32], float *part, int lane)
 {
-    const int col = D0 + 4 * (lane >> 5);
 #pragma unroll
-    for (int d = 0; d < (D1 - D0) / 32; ++d)
+    for (int d = 0; d < kCols / 32; ++d)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const f4 v = quad(x[d], k);
-            if (part)
-                *reinterpret_cast<f4 *>(part + 32 * d + 8 * k + col) = v;
-            else
-                store4<kIn>(to, at * D + 32 * d + 8 * k + col, v * scale);
-        }
+        for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<f4 *>(part + 32 * d + 8 * k + 4 * (lane >> 5)) = quad(x[d], k);
 }
 
 constexpr int dq_waves(int d) { return d <= 32 ? 4 : d <= 64 ? 3 : d <= 128 ? 2 : 1; }
@@ -154,11 +147,15 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
         products_done();
     };
     walk_tiles<T::kDirect>((it.others + kTile - 1) / kTile, fetch, put, work);
-    if (there)
-        store_row<D, kIn, 0, D>(dq, a.scale, a.dQ, at,
-                                it.part >= 0 ? a.part_dq + ((int64_t)it.part + mine) * D
-                                             : nullptr,
-                                lane);
+    if (it.part >= 0) {
+        if (there) store_part<D>(dq, a.part_dq + ((int64_t)it.part + mine) * D, lane);
+        return;
+    }
+    __syncthreads();  // nobody reads the tiles
+    store_rows32<D, kIn, D>(
+        wave == 0 ? s_k0 : wave == 1 ? s_k1 : wave == 2 ? s_v0 : s_v1, dq, a.scale, a.dQ,
+        [&](int r) { return query_row(a.q, it.head, (int64_t)it.row + 32 * wave + r); },
+        it.rows - 32 * wave, 0, lane);
 }
 
 // d = 64 to 128: the sums of dK and dV leave no room for both K and V beside
@@ -283,10 +280,19 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
         products_done();
     };
     walk_tiles<T::kDirect>((it.others + kTile - 1) / kTile, fetch, put, work);
-    if (!there) return;
-    float *part = it.part >= 0 ? a.part_dkv + ((int64_t)it.part + mine) * (2 * D) : nullptr;
-    store_row<D, kIn, D0, D1>(dk, a.scale, a.dK, at, part, lane);
-    store_row<D, kIn, D0, D1>(dv, 1.f, a.dV, at, part ? part + D : nullptr, lane);
+    if (it.part >= 0) {
+        if (!there) return;
+        float *part = a.part_dkv + ((int64_t)it.part + mine) * (2 * D) + D0;
+        store_part<D1 - D0>(dk, part, lane);
+        store_part<D1 - D0>(dv, part + D, lane);
+        return;
+    }
+    __syncthreads();  // nobody reads the tiles
+    static_assert(2 * 64 * (D1 - D0) <= sizeof(DkvBuffer<D>), "two waves to a buffer");
+    uint8_t *const lds = reinterpret_cast<uint8_t *>(wave & 2 ? &s1 : &s0) + (wave & 1) * 64 * (D1 - D0);
+    auto row = [&](int r) { return ((int64_t)it.row + 32 * wave + r) * a.n_kv + it.head; };
+    store_rows32<D, kIn, D1 - D0>(lds, dk, a.scale, a.dK, row, it.rows - 32 * wave, D0, lane);
+    store_rows32<D, kIn, D1 - D0>(lds, dv, 1.f, a.dV, row, it.rows - 32 * wave, D0, lane);
 }
 
 template <int D, int kIn>

@@ -223,6 +223,43 @@ __device__ __forceinline__ float sum_xor32(float v)
     return __builtin_bit_cast(float, (int)r[0]) + __builtin_bit_cast(float, (int)r[1]);
 }
 
+// Stores a wave's 32 result rows of kCols columns from an O^T-like accumulator,
+// scaled and rounded: `rows` of them, row r as row at(r) of `to` from column
+// `col` on.  A lane holds 8 bytes here and there of one row; through 64 kCols
+// bytes of LDS (the wave's own, nothing else in it in use) they become whole
+// rows of 16-byte pieces (dK and dV of 56 sequences of 11 to 22 tokens over 964 to
+// 2,891, 16 heads of 128 over 4: 131 us instead of 175).
+template <int D, int kIn, int kCols, typename At>
+__device__ __forceinline__ void store_rows32(uint8_t *lds, const f16v (&x)[kCols / 32],
+                                             float scale, void *to, At at, int rows, int col,
+                                             int lane)
+{
+    constexpr int kPieces = kCols / 8, kMask = kPieces % 8 ? 3 : 7;
+    asm("" : "+v"(lane));  // (what follows from it is not kept in registers until here)
+    const int i = lane & 31;
+#pragma unroll
+    for (int d = 0; d < kCols / 32; ++d)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            h4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = to16<kIn>(x[d][4 * k + e] * scale);
+            *reinterpret_cast<h4 *>(lds + i * (2 * kCols) + ((4 * d + k) ^ (i & kMask)) * 16 +
+                                    8 * (lane >> 5)) = v;
+        }
+    tile_fence<kFewWaves>();
+#pragma unroll
+    for (int j = 0; j < kPieces / 2; ++j) {
+        const int f = lane + 64 * j, row = f / kPieces, piece = f % kPieces;
+        if (row < rows)
+            *reinterpret_cast<u4 *>(reinterpret_cast<uint8_t *>(to) +
+                                    (at(row) * D + col) * 2 + piece * 16) =
+                *reinterpret_cast<const u4 *>(lds + row * (2 * kCols) +
+                                              (piece ^ (row & kMask)) * 16);
+    }
+    tile_fence<kFewWaves>();
+}
+
 // Waves per SIMD that the registers leave room for.
 constexpr int many_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
 
@@ -322,9 +359,9 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
     };
     walk_tiles<T::kDirect>((it.others + kKeys - 1) / kKeys, fetch, put, work);
     const float l = sum_xor32(l_run);
-    if (!there) return;
     const int col = 4 * (lane >> 5);
     if (it.part >= 0) {
+        if (!there) return;
         float *to = a.part_o + ((int64_t)it.part + mine) * D + col;
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
@@ -338,15 +375,11 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
         }
         return;
     }
-    const int64_t at = query_row(a.q, it.head, (int64_t)it.row + mine);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            store4<kIn>(a.O, at * D + 32 * d + 8 * k + col,
-                        f4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * inv);
-    if (col == 0) a.lse[at] = natural_lse(m_run, l);
+    auto at = [&](int r) { return query_row(a.q, it.head, (int64_t)it.row + 32 * wave + r); };
+    __syncthreads();  // nobody reads the tiles
+    store_rows32<D, kIn, D>(wave == 0 ? s_k0 : wave == 1 ? s_k1 : wave == 2 ? s_v0 : s_v1, o,
+                            l == 0.f ? 0.f : 1.f / l, a.O, at, it.rows - 32 * wave, 0, lane);
+    if (there && col == 0) a.lse[at(lane & 31)] = natural_lse(m_run, l);
 }
 
 template <int D, int kIn>
