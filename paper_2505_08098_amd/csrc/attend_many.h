@@ -13,7 +13,7 @@
 // bf16); then it is off by at most 2^-25 of the largest power, which is less than
 // the probabilities' own rounding leaves.
 //
-// 512 rows of a key head, 16,384 keys, 8 key heads of 128: 57 us, 600 TFLOP/s; a
+// 512 rows of a key head, 16,384 keys, 8 key heads of 128: 54 us, 635 TFLOP/s; a
 // tile of 64 keys takes 2.7 us, the beginning and the partial results 14.
 #pragma once
 
@@ -241,21 +241,16 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
     }
 
     const float l = sum_xor32(l_run);
-    if (!there) return;
     const int64_t part = a.prefix_part + ((int64_t)split * a.few.n_kv + head) * all +
-                         (int64_t)tile * kManyRows + mine;
-    const int col = 4 * (lane >> 5);
-    float *to = a.few.part_o + part * D + col;
-    const float power = __builtin_ldexpf(1.f, ref - 127);
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            *reinterpret_cast<f4 *>(to + 32 * d + 8 * k) =
-                f4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * power;
-    if (col == 0) {
-        a.few.part_ml[2 * part] = m_run;
-        a.few.part_ml[2 * part + 1] = l;
+                         (int64_t)tile * kManyRows + 32 * wave;
+    uint8_t *const lds = wave == 0 ? s0.k : wave == 1 ? s0.v : wave == 2 ? s1.k : s1.v;
+    __syncthreads();  // nobody reads the tiles
+    store_part32<D, T::kBytes / 128 / 32 * 32>(lds, o, __builtin_ldexpf(1.f, ref - 127),
+                                               a.few.part_o + part * D, D, rows - 32 * wave,
+                                               lane);
+    if (there && lane < 32) {
+        a.few.part_ml[2 * (part + lane)] = m_run;
+        a.few.part_ml[2 * (part + lane) + 1] = l;
     }
 }
 

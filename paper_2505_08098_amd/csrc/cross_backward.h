@@ -41,23 +41,6 @@ struct CrossBwdArgs {
 constexpr int bwd_tile(int d) { return d <= 32 ? 64 : 32; }
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Four columns of a result row from an accumulator.
-__device__ __forceinline__ f4 quad(const f16v &x, int k)
-{
-    return f4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
-}
-
-// An O^T-like accumulator's row, as it is, into partial sums.
-template <int kCols>
-__device__ __forceinline__ void store_part(const f16v (&x)[kCols / 32], float *part, int lane)
-{
-#pragma unroll
-    for (int d = 0; d < kCols / 32; ++d)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            *reinterpret_cast<f4 *>(part + 32 * d + 8 * k + 4 * (lane >> 5)) = quad(x[d], k);
-}
-
 constexpr int dq_waves(int d) { return d <= 32 ? 4 : d <= 64 ? 3 : d <= 128 ? 2 : 1; }
 constexpr int dkv_halves(int d) { return d <= 128 ? 1 : 2; }
 constexpr int dkv_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
@@ -147,15 +130,17 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
         products_done();
     };
     walk_tiles<T::kDirect>((it.others + kTile - 1) / kTile, fetch, put, work);
-    if (it.part >= 0) {
-        if (there) store_part<D>(dq, a.part_dq + ((int64_t)it.part + mine) * D, lane);
-        return;
-    }
+    uint8_t *const lds = wave == 0 ? s_k0 : wave == 1 ? s_k1 : wave == 2 ? s_v0 : s_v1;
+    const int rows = it.rows - 32 * wave;
     __syncthreads();  // nobody reads the tiles
-    store_rows32<D, kIn, D>(
-        wave == 0 ? s_k0 : wave == 1 ? s_k1 : wave == 2 ? s_v0 : s_v1, dq, a.scale, a.dQ,
-        [&](int r) { return query_row(a.q, it.head, (int64_t)it.row + 32 * wave + r); },
-        it.rows - 32 * wave, 0, lane);
+    if (it.part >= 0)
+        store_part32<D, T::kBytes / 128 / 32 * 32>(
+            lds, dq, 1.f, a.part_dq + ((int64_t)it.part + 32 * wave) * D, D, rows, lane);
+    else
+        store_rows32<D, kIn, D>(
+            lds, dq, a.scale, a.dQ,
+            [&](int r) { return query_row(a.q, it.head, (int64_t)it.row + 32 * wave + r); }, rows,
+            0, lane);
 }
 
 // d = 64 to 128: the sums of dK and dV leave no room for both K and V beside
@@ -183,7 +168,7 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
     using T = DkvTile<D>;
     using TV = ManyTile<D, kManyRows>;
     constexpr bool kVInLds = dkv_v_in_lds(D);
-    constexpr int kTile = T::kRows;
+    constexpr int kTile = T::kRows, kWidth = D1 - D0;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int mine = 32 * wave + (lane & 31);
@@ -234,7 +219,7 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
     } else {
         load_rows32<D>(v, a.V, at, there, 0u, lane);
     }
-    constexpr int kCols = (D1 - D0) / 32;
+    constexpr int kCols = kWidth / 32;
     f16v dk[kCols], dv[kCols];
 #pragma unroll
     for (int d = 0; d < kCols; ++d) dk[d] = dv[d] = zero16();
@@ -280,19 +265,21 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
         products_done();
     };
     walk_tiles<T::kDirect>((it.others + kTile - 1) / kTile, fetch, put, work);
+    // (two waves to a buffer)
+    constexpr int kOwn = sizeof(DkvBuffer<D>) / 2 / 16 * 16, kChunk = kOwn / 128 / 32 * 32;
+    static_assert(kOwn >= 64 * kWidth && kChunk >= 32, "room for a wave's rows");
+    uint8_t *const lds = reinterpret_cast<uint8_t *>(wave & 2 ? &s1 : &s0) + (wave & 1) * kOwn;
+    const int rows = it.rows - 32 * wave;
+    __syncthreads();  // nobody reads the tiles
     if (it.part >= 0) {
-        if (!there) return;
-        float *part = a.part_dkv + ((int64_t)it.part + mine) * (2 * D) + D0;
-        store_part<D1 - D0>(dk, part, lane);
-        store_part<D1 - D0>(dv, part + D, lane);
+        float *part = a.part_dkv + ((int64_t)it.part + 32 * wave) * (2 * D) + D0;
+        store_part32<kWidth, kChunk>(lds, dk, 1.f, part, 2 * D, rows, lane);
+        store_part32<kWidth, kChunk>(lds, dv, 1.f, part + D, 2 * D, rows, lane);
         return;
     }
-    __syncthreads();  // nobody reads the tiles
-    static_assert(2 * 64 * (D1 - D0) <= sizeof(DkvBuffer<D>), "two waves to a buffer");
-    uint8_t *const lds = reinterpret_cast<uint8_t *>(wave & 2 ? &s1 : &s0) + (wave & 1) * 64 * (D1 - D0);
     auto row = [&](int r) { return ((int64_t)it.row + 32 * wave + r) * a.n_kv + it.head; };
-    store_rows32<D, kIn, D1 - D0>(lds, dk, a.scale, a.dK, row, it.rows - 32 * wave, D0, lane);
-    store_rows32<D, kIn, D1 - D0>(lds, dv, 1.f, a.dV, row, it.rows - 32 * wave, D0, lane);
+    store_rows32<D, kIn, kWidth>(lds, dk, a.scale, a.dK, row, rows, D0, lane);
+    store_rows32<D, kIn, kWidth>(lds, dv, 1.f, a.dV, row, rows, D0, lane);
 }
 
 template <int D, int kIn>
