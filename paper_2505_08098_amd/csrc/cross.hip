@@ -22,6 +22,11 @@ using f3s::set_status;
 constexpr int64_t kUnits = 256;  // compute units
 // Workgroups that the kernel of few rows aims at.
 constexpr int64_t kFewWorkgroups = 4 * kUnits;
+// What a launch that joins pieces costs there, in units of 64 keys, of which one
+// takes 0.4 us (d = 64) to 0.6 us (128).  One token of 4 sequences over 500 to 1,000
+// keys, 8 key heads, whole and in pieces: 8.0 and 6.7 us on the GPU and 9.2 and
+// 13.5 us from one call to the next (d = 64), 12.0 and 7.9, 12.1 and 13.4 (128).
+constexpr double kFewLaunch = 10;
 // Query rows of a key head up to which the forward takes the kernel of few rows:
 // one sequence's row over 100 keys takes 2.7 us with it and 3.8 with the other, 4
 // over 8,192 keys 8.6 and 10.8; 16 rows of 16 sequences over 2,048 keys 28.9 and
@@ -72,7 +77,7 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
     const bool few = rows_env && *rows_env ? atoi(rows_env) == f3s::kFewRows
                                            : longest <= kFewLongest;
     if (few)
-        f.make(fwd, n_kv, f3s::kFewRows, 64, 256, kFewWorkgroups);
+        f.make(fwd, n_kv, f3s::kFewRows, 64, 256, kFewWorkgroups, kFewLaunch);
     else
         f.make(fwd, n_kv, f3s::kManyRows, 64, 256, kUnits * f3s::many_waves(d));
     dq.make(fwd, n_kv, f3s::kManyRows, 64, 256, kUnits * f3s::dq_waves(d));

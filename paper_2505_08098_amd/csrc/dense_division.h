@@ -31,7 +31,7 @@ struct Division {
     // one size run in rounds (520 on 512 places take as long as 1,024); of
     // different sizes, the longest first, they end about one piece apart.
     static double time(const std::vector<Range> &ranges, int32_t heads, int64_t tile,
-                       int64_t unit, int64_t slots, int64_t per)
+                       int64_t unit, int64_t slots, int64_t per, double launch)
     {
         double total = 0, n = 0, longest = 0;
         for (const Range &r : ranges) {
@@ -46,7 +46,7 @@ struct Division {
         const double t = rounds <= 1                  ? longest
                          : longest * n <= 1.25 * total ? rounds * longest
                                                        : total / slots + longest / 2;
-        return t + (split(ranges, unit, per) ? kLaunch : 0.0);
+        return t + (split(ranges, unit, per) ? launch : 0.0);
     }
     static bool split(const std::vector<Range> &ranges, int64_t unit, int64_t per)
     {
@@ -71,16 +71,17 @@ struct Division {
 
     // Units of a piece, where all are divided alike, that take the least time.
     static int64_t best_pieces(const std::vector<Range> &ranges, int32_t heads, int64_t tile,
-                               int64_t unit, int64_t least, int64_t slots, double *takes)
+                               int64_t unit, int64_t least, int64_t slots, double launch,
+                               double *takes)
     {
         const int64_t top = ranges.empty() ? 1 : ceil_div(ranges[0].others, unit);
         int64_t per = top < 1 ? 1 : top;
-        double best = time(ranges, heads, tile, unit, slots, per);
+        double best = time(ranges, heads, tile, unit, slots, per, launch);
         for (int64_t k = 2; k <= top; k += k > kMostPieces ? k / kMostPieces : 1) {
             // (as many pieces as it takes to fill the GPU, and then some)
             const int64_t p = ceil_div(top, k);
             if (p * unit < least) break;
-            const double t = time(ranges, heads, tile, unit, slots, p);
+            const double t = time(ranges, heads, tile, unit, slots, p, launch);
             if (t < best) {
                 best = t;
                 per = p;
@@ -93,7 +94,7 @@ struct Division {
 
     // `slots`: workgroups that run at once; pieces have `least` rows or more.
     void make(std::vector<Range> ranges, int32_t heads, int64_t tile, int64_t unit,
-              int64_t least, int64_t slots)
+              int64_t least, int64_t slots, double launch = kLaunch)
     {
         double tiles = 0;
         for (const Range &r : ranges) tiles += (double)ceil_div(r.rows, tile) * heads;
@@ -105,7 +106,7 @@ struct Division {
         std::stable_sort(ranges.begin(), ranges.end(),
                          [](const Range &a, const Range &b) { return a.others > b.others; });
         double best = 0;
-        int64_t per = best_pieces(ranges, heads, tile, unit, least, slots, &best);
+        int64_t per = best_pieces(ranges, heads, tile, unit, least, slots, launch, &best);
         std::vector<int64_t> most(ranges.size(), per);  // units of a range's pieces
         // A few tiles too many cost a round.  What is left of the ranges behind
         // their whole tiles is then better cut small and run behind the others:
@@ -121,11 +122,11 @@ struct Division {
         if (!whole.empty() && !rest.empty()) {
             const int64_t small = ceil_div(least, unit);
             double t = 0, n = 0;
-            per = best_pieces(whole, heads, tile, unit, least, slots, &t);
+            per = best_pieces(whole, heads, tile, unit, least, slots, launch, &t);
             for (const Range &r : rest)
                 n += (double)pieces(ceil_div(r.others, unit), small) * heads;
             t += (double)ceil_div((int64_t)n, slots) * (small + kOver + kJoin) +
-                 (split(whole, unit, per) ? 0 : kLaunch);
+                 (split(whole, unit, per) ? 0 : launch);
             if (t < kWorth * best) {
                 most.assign(whole.size(), per);
                 most.resize(whole.size() + rest.size(), small);
