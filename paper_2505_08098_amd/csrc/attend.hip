@@ -25,6 +25,13 @@ constexpr int64_t kWorkgroups = 8 * kUnits;
 //   4 key heads of 256, 256 rows: 4.2 M scores 38.0 and 44.8, 8.4 M 59.4 and 54.7
 constexpr int64_t kFewPrefixRows = 64;
 constexpr int64_t kManyScores = 6000000;
+// Units that a table has room for up to which no sequence is divided (so that one
+// launch does).  Calls over 250 to 500 and 445 to 890 own keys, 8 key heads of 128,
+// us on the GPU and from one call to the next, whole and in pieces:
+//    4 sequences:  9.5, 11.3 and 10.0, 14.3;   13.0, 13.3 and 10.3, 14.3
+//   64 sequences: 15.4, 15.2 and 21.3, 21.2;   21.5, 21.3 and 28.4, 28.0
+// (16 of 750 to 1,500: 21.3, 21.2 and 16.2, 16.1).
+constexpr int64_t kDirectUnits = 14;
 // What a piece of the prefix costs beside its keys (queries, partial results),
 // in units of 64 keys.
 constexpr int64_t kPieceCost = 3;
@@ -59,12 +66,12 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     a->rows = (int32_t)rows;
     a->row_blocks = (int32_t)ceil_div(rows, f3s::kFewRows);
     const int64_t cap_units = ceil_div(cap, f3s::kUnit);
-    a->direct = prefix_len == 0 && cap_units <= f3s::kLeastUnits;
+    a->direct = prefix_len == 0 && cap_units <= kDirectUnits;
     int64_t share = ceil_div(kWorkgroups, (int64_t)c.n_kv_heads * a->row_blocks);
     // (no more than the table has places for)
     const int64_t most = ceil_div(cap_units * n_seqs, f3s::kLeastUnits);
     if (share > most) share = most;
-    if (share < 1) share = 1;
+    if (share < 1 || a->direct) share = 1;  // (a sequence is one piece)
     a->share = (int32_t)share;
     a->own_items = a->direct || cap_units <= f3s::kLeastUnits ? n_seqs
                                                               : (int32_t)(share + n_seqs);

@@ -166,8 +166,8 @@ def test_attend(lib, change, status):
 def test_attend_workspace(lib):
     c = _cache()
     size = lambda *a: lib.f3s_cache_attend_workspace_bytes(ctypes.byref(c), *a)
-    assert size(16, 3, 1, 4, 0) == 0            # 256 keys: one workgroup has them all
-    assert size(17, 3, 1, 4, 0) > 0
+    assert size(56, 3, 1, 4, 0) == 0            # 896 keys: one workgroup has them all
+    assert size(57, 3, 1, 4, 0) > 0
     assert size(16, 3, 1, 4, 1) > 0
     assert size(400, 3, 2, 4, 100) <= size(400, 3, 2, 4, 100000)
     assert size(400, 3, 2, 3, 0) == 0 and size(-1, 3, 2, 4, 0) == 0

@@ -122,11 +122,11 @@ def test_every_16_bit_value(gpu):
         assert torch.equal(got, e.view(-1))
 
 
-def _attend_case(gpu, dtype, d, page, kv, g, lens, n, prefix_len, scale=None, seed=0):
+def _attend_case(gpu, dtype, d, page, kv, g, lens, n, prefix_len, scale=None, seed=0, room=0):
     gen = torch.Generator().manual_seed(seed + d + page + n)
     B = len(lens)
     shared = -(-prefix_len // page)
-    table, n_pages = _table(gen, B, max(1, -(-max(lens) // page)), first=shared)
+    table, n_pages = _table(gen, B, max(1, -(-max(max(lens), room) // page)), first=shared)
     cache = _cache(gpu, n_pages, page, kv, d)
     lens_d = torch.tensor(lens, dtype=torch.int32, device=DEV)
     prefix = None
@@ -201,6 +201,21 @@ def _compare(cache, Q, table, lens, prefix, prefix_len, scale, O, lse):
 ])
 def test_attend(gpu, dtype, d, page, kv, g, lens, n, prefix):
     _attend_case(gpu, dtype, d, page, kv, g, lens, n, prefix)
+
+
+@pytest.mark.parametrize("d,page,kv,g,lens,n", [
+    (64, 16, 2, 1, [1, 0, 5, 33, 16, 17], 1), (64, 16, 1, 4, [300, 1, 64, 65], 1),
+    (128, 64, 2, 4, [1000, 3, 517], 1), (32, 16, 3, 1, [40, 41], 5),
+    (96, 16, 1, 2, [290], 3), (256, 256, 1, 3, [600, 20], 2),
+    (64, 16, 1, 40, [570, 200], 1), (64, 16, 1, 3, [0, 0], 2), (160, 128, 1, 1, [1500], 9),
+    (64, 32, 2, 8, [4000, 70, 1], 2)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attend_in_pieces(gpu, dtype, d, page, kv, g, lens, n):
+    """Tables with room for more than one workgroup walks: pieces, whatever the
+    lengths are, and none of it where there is room for 896 keys."""
+    _attend_case(gpu, dtype, d, page, kv, g, lens, n, 0, room=3000)
+    short = [min(m, 896) for m in lens]
+    _attend_case(gpu, dtype, d, page, kv, g, short, n, 0, room=896)
 
 
 @pytest.mark.parametrize("rows", ["16", "128"])

@@ -498,7 +498,7 @@ def test_thousands_of_sequences(gpu):
     """More sequences than a wave looks at in one go: every one as if alone."""
     gen = torch.Generator().manual_seed(31)
     kv, d, page, B = 2, 64, 16, 5000
-    table7, n_pages = _table(gen, 7, 4)
+    table7, n_pages = _table(gen, 7, 60)         # (room for more: found on the device)
     cache = _cache(gpu, n_pages, page, kv, d)
     x = [_rows(gen, (7, 64, kv, d), torch.float16).to(DEV) for _ in "KV"]
     gpu.cache_write(cache, *x, table7.to(DEV), _int32([64] * 7))
