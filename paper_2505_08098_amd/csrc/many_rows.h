@@ -15,9 +15,9 @@
 // sums stay in the lane until the end.
 //
 // 2 x 4,050 tokens, 32 heads of 128 over 8, 8,100 keys, bf16: 1,076 us, 1,000
-// TFLOP/s, where a library's product of 8,192^3 reaches 1,200.  Power bounds both:
-// the clock falls to 1.9 GHz, the matrix units are busy 47% of the time and the
-// vector unit as long again.
+// TFLOP/s, where a library's product of 8,192^3 reaches 1,200.  The clock falls to
+// 1.9 GHz, the matrix units are busy 47% of its cycles and the vector unit as long
+// again, and more waves or earlier reads gain nothing: power seems to be the bound.
 #pragma once
 
 #include "few_rows.h"
