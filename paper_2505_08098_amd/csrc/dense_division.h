@@ -92,7 +92,10 @@ struct Division {
         return per;
     }
 
-    // `slots`: workgroups that run at once; pieces have `least` rows or more.
+    // `slots`: workgroups that run at once.  A range is divided into pieces of at
+    // most as many units for as many as `least` rows or more; what does not come out
+    // even is spread over them, so that the shortest has half as many rows (128 of
+    // 256: 320 rows as 128 and 192).
     void make(std::vector<Range> ranges, int32_t heads, int64_t tile, int64_t unit,
               int64_t least, int64_t slots, double launch = kLaunch)
     {
