@@ -152,6 +152,18 @@ constexpr bool dkv_v_in_lds(int d) { return d > 32 && d <= 128; }
 template <int D>
 using DkvTile = ManyTile<D, bwd_tile(D)>;
 
+// P enters dV's product times 2^12 in f16, whose least normal number is 2^-14: a
+// row's probabilities sum to 1, so those of a few ten thousand keys would lose bits
+// (1.3% of each at a million keys, the same way for all), and no scaling of dO helps,
+// since P has none of it.  They keep 11 bits down to 2^-26, and 2^12 leaves 16 times
+// of room above 1 for what lse is off by.  The factor costs nothing: it is added to
+// the exponent with lse, dS takes it out within the subtraction of delta (exactly),
+// and dV as it is stored.  bf16 has fp32's exponents.
+template <int kIn>
+constexpr float kPUp = kIn == kInF16 ? 0x1p12f : 1.f;
+template <int kIn>
+constexpr float kPUpLog2 = kIn == kInF16 ? 12.f : 0.f;
+
 // A tile of query rows and what belongs to it.
 template <int D>
 struct DkvBuffer {
@@ -169,6 +181,7 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
     using TV = ManyTile<D, kManyRows>;
     constexpr bool kVInLds = dkv_v_in_lds(D);
     constexpr int kTile = T::kRows, kWidth = D1 - D0;
+    constexpr float kPDown = 1.f / kPUp<kIn>;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int mine = 32 * wave + (lane & 31);
@@ -201,8 +214,9 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
         tg.put(to.g);
         if (threadIdx.x < kTile) {
             to.lse[threadIdx.x] =
-                kTile * t + (int)threadIdx.x < it.others ? sr.x : INFINITY;  // (P = 0)
-            to.delta[threadIdx.x] = sr.y;
+                kTile * t + (int)threadIdx.x < it.others ? sr.x - kPUpLog2<kIn>
+                                                         : INFINITY;  // (P = 0)
+            to.delta[threadIdx.x] = sr.y * kPDown;
         }
     };
     h8 k[D / 16], v[kVInLds ? 1 : D / 16];
@@ -248,7 +262,7 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
                     const float y =
                         __builtin_amdgcn_exp2f(fmaf(x[4 * r + e], a.sl2, -l[e]));
                     p[4 * r + e] = y;
-                    x[4 * r + e] = y * (dp[4 * r + e] - w[e]);
+                    x[4 * r + e] = y * fmaf(dp[4 * r + e], kPDown, -w[e]);
                 }
             }
 #pragma unroll
@@ -274,12 +288,12 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
     if (it.part >= 0) {
         float *part = a.part_dkv + ((int64_t)it.part + 32 * wave) * (2 * D) + D0;
         store_part32<kWidth, kChunk>(lds, dk, 1.f, part, 2 * D, rows, lane);
-        store_part32<kWidth, kChunk>(lds, dv, 1.f, part + D, 2 * D, rows, lane);
+        store_part32<kWidth, kChunk>(lds, dv, kPDown, part + D, 2 * D, rows, lane);
         return;
     }
     auto row = [&](int r) { return ((int64_t)it.row + 32 * wave + r) * a.n_kv + it.head; };
     store_rows32<D, kIn, kWidth>(lds, dk, a.scale, a.dK, row, rows, D0, lane);
-    store_rows32<D, kIn, kWidth>(lds, dv, 1.f, a.dV, row, rows, D0, lane);
+    store_rows32<D, kIn, kWidth>(lds, dv, kPDown, a.dV, row, rows, D0, lane);
 }
 
 template <int D, int kIn>

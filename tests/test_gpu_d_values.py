@@ -1,11 +1,12 @@
 """Values of the dense operators where 16 bits of a product's operands could lose
-them: tokens before one whose values are far larger."""
+them: tokens before one whose values are far larger, probabilities of very many
+keys."""
 import math
 
 import pytest
 import torch
 
-from _dense import attention, close, half_step
+from _dense import F32, attention, close, half_step
 from test_gpu_b_cache import TYPES, _cache, _rows, _table, _values
 
 pytestmark = pytest.mark.gpu
@@ -74,3 +75,43 @@ def test_later_tokens_with_large_values(gpu, dtype, d, page, kv, g, lens, n, P, 
                 # probabilities are relative to its own largest power)
                 close(O[b, t: t + 1, h], f["O"], f["O_tol"], (b, t, h))
                 close(lse[b, t: t + 1, h], f["lse"], f["lse_tol"], ("lse", b, t, h))
+
+
+# ---- probabilities of very many keys ---------------------------------------------------
+
+@pytest.mark.parametrize("d,kv,g,q_len,k_len", [
+    (32, 1, 1, [1, 3], [360000, 30000]), (64, 1, 2, [1], [130500]), (160, 1, 1, [2], [200100]),
+    (128, 2, 2, [2], [50123]), (32, 1, 1, [400], [40001]),       # (divided: many query rows)
+])
+def test_value_gradients_of_many_keys(gpu, d, kv, g, q_len, k_len):
+    """dV in fp16 where every probability is far below 2^-14, fp16's least normal
+    number: each keeps its 11 bits all the same.  (dO is as large as a scaled loss
+    makes it, so that dV itself is a normal number.)"""
+    gen = torch.Generator().manual_seed(d + kv + g)
+    dtype, u, H, scale = torch.float16, 2.0 ** -11, kv * g, 1 / math.sqrt(d)
+    q_ptr, k_ptr = ([sum(x[:b]) for b in range(len(x) + 1)] for x in (q_len, k_len))
+    Q = (torch.randn((q_ptr[-1], H, d), generator=gen) / 1024).to(dtype).to(DEV)
+    G = (torch.randn((q_ptr[-1], H, d), generator=gen) * 512).to(dtype).to(DEV)
+    K, V = (torch.randn((k_ptr[-1], kv, d), generator=gen).to(dtype).to(DEV) for _ in "KV")
+    plan = gpu.CrossPlan(q_ptr, k_ptr, H, kv, d, device=DEV)
+    O, lse = gpu.cross_forward(plan, Q, K, V)
+    got = gpu.cross_backward(plan, Q, K, V, O, G, lse)[2]
+    want = torch.zeros(V.shape, dtype=torch.float64, device=DEV)
+    tol = torch.zeros_like(want)
+    for b in range(len(q_len)):
+        i, j = slice(q_ptr[b], q_ptr[b + 1]), slice(k_ptr[b], k_ptr[b + 1])
+        for h in range(H):
+            q, k, w = Q[i, h].double(), K[j, h // g].double(), G[i, h].double()
+            x = q @ k.T * scale
+            lse64 = torch.logsumexp(x, 1, keepdim=True)
+            P = torch.exp(x - lse64)
+            want[j, h // g] += P.T @ w
+            # P's rounding; the score's 32-bit sum and the exponential (4 ulp); lse: its
+            # sum of a lane's keys / 64 and of the pieces, and its own rounding; 32-bit
+            # sums over the query rows
+            off = u + (d + 8) * F32 * scale * float((q.abs() @ k.abs().T).max()) + 8 * F32 + \
+                (k_len[b] / 64 + 64 + 4 * float(lse64.abs().max())) * F32 + \
+                (g * q_len[b] / 16 + 64) * F32
+            tol[j, h // g] += off * (P.T @ w.abs())
+    # dV itself is rounded once (2^-25: below 2^-14)
+    close(got, want.cpu(), (tol + u * want.abs() + 2.0 ** -25).cpu(), "dV")
