@@ -89,8 +89,9 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
  *              prefix_len <= 2^30
  *   scale      finite
  *   workspace  device, at least f3s_cache_attend_workspace_bytes(...) bytes,
- *              256-byte aligned; needs no initialisation, and calls that
- *              overlap in time need one each.  NULL if that is 0
+ *              256-byte aligned; needs no initialisation, must not overlap
+ *              anything else of the call, and calls that overlap in time need
+ *              one each.  NULL if that is 0
  * Inputs must be finite.  Scores, sums and statistics are fp32; the products
  * with V are f16, relative to the largest power of two among the values that the
  * token has seen so far: beside 2^-11 of its probability a key adds an error of up

@@ -61,8 +61,8 @@ size_t f3s_cross_backward_workspace_bytes(f3s_cross_plan_t plan);
  *              256-byte aligned; needs no initialisation; NULL if that is 0
  *   scale      finite
  *   stream     of the plan's device (else F3S_ERR_INVALID_VALUE)
- * Inputs must be finite where they are not padding.  Outputs must not overlap
- * each other or an input.  Scores, softmax and sums in fp32; the
+ * Inputs must be finite where they are not padding.  Outputs and workspace must
+ * not overlap each other or an input.  Scores, softmax and sums in fp32; the
  * probabilities enter the value product in dtype, O is rounded once.
  * Asynchronous on `stream`; no allocation, no synchronisation; deterministic.
  * Calls on one plan may overlap in time, each with a workspace of its own.

@@ -205,12 +205,16 @@ f3s_status_t f3s_cache_attend(const f3s_cache_t *cache, const void *Q, f3s_dtype
               {cache->v_exp, cb},
               {table, (size_t)n_seqs * max_pages * 4},
               {lens, (size_t)n_seqs * 4},
-              {prefix, ((size_t)prefix_len + cache->page_size - 1) / cache->page_size * 4},
-              {workspace, w.bytes}};
+              {prefix, ((size_t)prefix_len + cache->page_size - 1) / cache->page_size * 4}};
+    // (partial results over lengths or pages that others still read would lead
+    // anywhere)
     for (const auto &x : in)
-        if (overlaps(O, qb, x.p, x.n) || overlaps(lse, lb, x.p, x.n))
+        if (overlaps(O, qb, x.p, x.n) || overlaps(lse, lb, x.p, x.n) ||
+            overlaps(workspace, w.bytes, x.p, x.n))
             return set_status(F3S_ERR_INVALID_VALUE);
-    if (overlaps(O, qb, lse, lb)) return set_status(F3S_ERR_INVALID_VALUE);
+    if (overlaps(O, qb, lse, lb) || overlaps(O, qb, workspace, w.bytes) ||
+        overlaps(lse, lb, workspace, w.bytes))
+        return set_status(F3S_ERR_INVALID_VALUE);
     a.table = table;
     a.lens = lens;
     a.prefix = prefix;

@@ -219,11 +219,14 @@ f3s_status_t f3s_cross_forward(f3s_cross_plan_t p, const void *Q, const void *K,
     const struct {
         const void *p;
         size_t n;
-    } in[] = {{Q, qb}, {K, kb}, {V, kb}, {workspace, need}};
+    } in[] = {{Q, qb}, {K, kb}, {V, kb}};
     for (const auto &x : in)
-        if (overlaps(O, qb, x.p, x.n) || overlaps(lse, lb, x.p, x.n))
+        if (overlaps(O, qb, x.p, x.n) || overlaps(lse, lb, x.p, x.n) ||
+            overlaps(workspace, need, x.p, x.n))
             return set_status(F3S_ERR_INVALID_VALUE);
-    if (overlaps(O, qb, lse, lb)) return set_status(F3S_ERR_INVALID_VALUE);
+    if (overlaps(O, qb, lse, lb) || overlaps(O, qb, workspace, need) ||
+        overlaps(lse, lb, workspace, need))
+        return set_status(F3S_ERR_INVALID_VALUE);
     f3s::FewArgs a = {};
     a.Q = Q;
     a.K = K;
@@ -279,8 +282,10 @@ f3s_status_t f3s_cross_backward(f3s_cross_plan_t p, const void *Q, const void *K
     const Span in[] = {{Q, qb}, {K, kb}, {V, kb}, {O, qb}, {dO, qb}, {lse, lb},
                        {workspace, need}};
     const Span out[] = {{dQ, qb}, {dK, kb}, {dV, kb}};
+    const Span &stats = in[5], &room = in[6];
     for (const Span &x : in)
-        if ((x.n && !x.p) || !aligned(x.p, x.p == lse ? 4 : 16))
+        if ((x.n && !x.p) || !aligned(x.p, &x == &stats ? 4 : 16) ||
+            (&x != &room && overlaps(room.p, room.n, x.p, x.n)))
             return set_status(F3S_ERR_INVALID_VALUE);
     for (const Span &x : out) {
         if ((x.n && !x.p) || !aligned(x.p, 16)) return set_status(F3S_ERR_INVALID_VALUE);
