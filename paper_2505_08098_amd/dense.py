@@ -24,6 +24,7 @@ _LIB = None
 _vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
 _HALF = (torch.float16, torch.bfloat16)
 _READ_TYPES = _HALF + (torch.float32,)
+_MOST = 2**31 - 1
 
 
 class _CacheStruct(ctypes.Structure):
@@ -118,9 +119,17 @@ def _host_ints(x, name):
     a = np.asarray(x)
     if a.ndim != 1 or (a.size and a.dtype.kind not in "iu"):
         raise ValueError(f"{name} must be a host sequence of whole numbers")
-    if a.size and (a.min() < 0 or a.max() > 2**31 - 1):
+    if a.size and (a.min() < 0 or a.max() > _MOST):
         raise ValueError(f"{name} must lie in [0, 2^31)")
     return np.ascontiguousarray(a, dtype=np.int32)
+
+
+def _size(x, name):
+    """x as an int that 32 bits hold (ctypes would take it modulo 2^32)."""
+    x = int(x)
+    if not -_MOST <= x <= _MOST:
+        raise ValueError(f"{name} must be a 32-bit number, got {x}")
+    return x
 
 
 # ---- cross attention ----------------------------------------------------------
@@ -143,21 +152,22 @@ class CrossPlan:
                 for x, n in ((q_len, "q_len"), (k_len, "k_len"))]
         if any(x is not None and x.size != q.size - 1 for x in lens):
             raise ValueError("q_len and k_len must hold one entry per sequence")
+        heads, d = _size(heads, "heads"), _size(d, "d")
+        kv_heads = heads if kv_heads is None else _size(kv_heads, "kv_heads")
         device = torch.device(device)
         if device.type != "cuda":
             raise ValueError("the plan's device must be a GPU")
         if device.index is None:
             device = torch.device("cuda", torch.cuda.current_device())
         ptr = lambda a: None if a is None else a.ctypes.data_as(_vp)
-        kv_heads = heads if kv_heads is None else kv_heads
         with _BuildOn(device):
             h = L.f3s_cross_plan(ptr(q), ptr(k), ptr(lens[0]), ptr(lens[1]), q.size - 1,
-                                 int(heads), int(kv_heads), int(d))
+                                 heads, kv_heads, d)
         if not h:
             raise F3SError(L.f3s_last_error(), "f3s_cross_plan")
         self._h = h
         self.device = device
-        self.heads, self.kv_heads, self.d = int(heads), int(kv_heads), int(d)
+        self.heads, self.kv_heads, self.d = heads, kv_heads, d
         self.q_shape = (int(q[-1]), self.heads, self.d)
         self.k_shape = (int(k[-1]), self.kv_heads, self.d)
         self.lse_shape = self.q_shape[:2]
@@ -267,8 +277,8 @@ class Cache:
         self._tensors = (k, v, k_exp, v_exp)
         self.device = k.device
         self.n_pages, self.kv_heads, self.page_size, self.d = k.shape
-        if self.n_pages > 2**31 - 1:
-            raise ValueError("more than 2^31 - 1 pages")
+        if max(k.shape) > _MOST:
+            raise ValueError("more than 2^31 - 1 pages, heads, tokens or values")
         self._struct = _CacheStruct(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(),
                                     v_exp.data_ptr(), self.n_pages, self.kv_heads,
                                     self.page_size, self.d)
@@ -301,6 +311,8 @@ def _sequences(cache, table, lens):
             _check_device_tensor(t, n, torch.int32, device)
     if table.dim() != 2 or lens.dim() != 1 or table.shape[0] != lens.shape[0]:
         raise ValueError("table must be [sequences, pages], lens [sequences]")
+    if table.shape[1] > _MOST or table.shape[0] > _MOST:
+        raise ValueError("more than 2^31 - 1 sequences, or pages of one")
     return table.shape
 
 
@@ -315,7 +327,7 @@ def cache_write(cache, K, V, table, lens):
     dtype = _dtype_of(K, "K")
     if K.dim() != 4:
         raise ValueError("K must be [sequences, n, kv_heads, d]")
-    n = K.shape[1]
+    n = _size(K.shape[1], "n")
     shape = (B, n, cache.kv_heads, cache.d)
     _check(K, "K", dtype, cache.device, shape)
     _check(V, "V", dtype, cache.device, shape)
@@ -334,7 +346,7 @@ def cache_read(cache, table, lens, n, dtype=torch.float16):
     B, pages = _sequences(cache, table, lens)
     if dtype not in _READ_TYPES:
         raise TypeError("dtype must be float16, bfloat16 or float32")
-    n = int(n)
+    n = _size(n, "n")
     shape = (B, n, cache.kv_heads, cache.d)
     K = torch.empty(shape, dtype=dtype, device=cache.device)
     V = torch.empty_like(K)
@@ -365,7 +377,7 @@ def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, o
         if prefix_len != 0:
             raise ValueError("prefix and a positive prefix_len come together")
     else:
-        prefix_len = int(prefix_len)
+        prefix_len = _size(prefix_len, "prefix_len")
         _check_device_tensor(prefix, "prefix", torch.int32, device)
         if prefix_len < 1:
             raise ValueError("prefix and a positive prefix_len come together")
@@ -374,6 +386,8 @@ def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, o
     sizes = (pages, B, n, heads, prefix_len)
     nbytes = cache._bytes.get(sizes)
     if nbytes is None:
+        if max(sizes) > _MOST:
+            raise ValueError("more than 2^31 - 1 tokens or heads")
         if len(cache._bytes) >= 64:  # (a prefix that grows)
             cache._bytes.clear()
         nbytes = _lib().f3s_cache_attend_workspace_bytes(cache._ref, *sizes)
