@@ -92,15 +92,16 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
  *              256-byte aligned; needs no initialisation, must not overlap
  *              anything else of the call, and calls that overlap in time need
  *              one each.  NULL if that is 0
- * Inputs must be finite.  Scores, sums and statistics are fp32; the products
- * with V are f16, relative to the largest power of two among the values that the
- * token has seen so far: beside 2^-11 of its probability a key adds an error of up
- * to 2^-25 of the largest |value| that the token sees.  The work is divided on the
- * device, by the lengths that it finds there: a captured call stays right when they
- * change.  A prefix is read once for many sequences: for 16 query rows of a key
- * head at a time, or, with many rows and much work, for 128 (environment
- * F3S_PREFIX_ROWS=16 or 128 forces one).  Deterministic.  Asynchronous on `stream`;
- * no allocation, no synchronisation.
+ * Inputs must be finite.  Scores, sums and statistics are fp32 (products of Q with
+ * codes, before and after scaling, and |V| times the number of keys have to stay
+ * below 2^127); the products with V are f16, relative to the largest power of two
+ * among the values that the token has seen so far: beside 2^-11 of its probability
+ * a key adds an error of up to 2^-25 of the largest |value| that the token sees.
+ * The work is divided on the device, by the lengths that it finds there: a captured
+ * call stays right when they change.  A prefix is read once for many sequences: for
+ * 16 query rows of a key head at a time, or, with many rows and much work, for 128
+ * (environment F3S_PREFIX_ROWS=16 or 128 forces one).  Deterministic.
+ * Asynchronous on `stream`; no allocation, no synchronisation.
  */
 f3s_status_t f3s_cache_attend(const f3s_cache_t *cache, const void *Q, f3s_dtype_t dtype,
                               void *O, float *lse, const int32_t *table, int32_t max_pages,

@@ -223,7 +223,7 @@ f3s_status_t f3s_cache_attend(const f3s_cache_t *cache, const void *Q, f3s_dtype
     a.few.lse = lse;
     a.few.q = f3s::query_rows(n_heads, n_heads / cache->n_kv_heads);
     a.few.n_kv = cache->n_kv_heads;
-    a.few.sl2 = (float)(fabs((double)scale) * 1.4426950408889634);
+    a.few.sl2 = f3s::scale_log2e(scale);
     a.few.flip = signbit(scale) ? 0x80008000u : 0u;
     a.few.k = (const uint8_t *)cache->k;
     a.few.v = (const uint8_t *)cache->v;

@@ -157,7 +157,7 @@ size_t parts_bytes(int64_t rows, int32_t d, int32_t record)
 // of an f16 or bf16 product below 2^100 into 0 as well.
 float base2_scale(float scale)
 {
-    const float s = (float)(fabs((double)scale) * 1.4426950408889634);
+    const float s = f3s::scale_log2e(scale);
     return s < 0x1p-120f ? 0x1p-120f : s;
 }
 

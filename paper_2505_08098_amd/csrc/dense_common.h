@@ -43,6 +43,14 @@ __device__ __forceinline__ int64_t query_row(const QueryRows &q, int kh, int64_t
     return (int64_t)t * (uint32_t)(q.n_heads - q.g) + (uint32_t)r + (uint32_t)(kh * q.g);
 }
 
+// |scale| log2 e in 32 bits, the largest number of theirs where it is larger (a
+// score of 0 times infinity would be NaN).
+inline float scale_log2e(float scale)
+{
+    const double s = (scale < 0 ? -(double)scale : (double)scale) * 1.4426950408889634;
+    return s < 0x1.fffffep127 ? (float)s : 0x1.fffffep127f;
+}
+
 // One workgroup's share of a forward or backward pass over a ragged batch.
 // Rows are those of the pass's own side (packed query rows of the key head,
 // or key rows); others are the rows of the other side that it walks.

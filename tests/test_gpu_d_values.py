@@ -115,3 +115,44 @@ def test_value_gradients_of_many_keys(gpu, d, kv, g, q_len, k_len):
             tol[j, h // g] += off * (P.T @ w.abs())
     # dV itself is rounded once (2^-25: below 2^-14)
     close(got, want.cpu(), (tol + u * want.abs() + 2.0 ** -25).cpu(), "dV")
+
+
+# ---- the largest scales ------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows", ["16", "128"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [3.4e38, -3e38])
+def test_largest_scales(gpu, monkeypatch, rows, dtype, scale):
+    """Every finite scale is taken, also where scale log2 e is not finite in 32 bits:
+    scores of 0 stay 0."""
+    monkeypatch.setenv("F3S_CROSS_ROWS", rows)
+    monkeypatch.setenv("F3S_PREFIX_ROWS", rows)
+    gen = torch.Generator().manual_seed(2)
+    u, n, kv, d = half_step(dtype), 77, 2, 64
+    V = torch.randn((n, kv, d), generator=gen).to(dtype).to(DEV)
+    zero = torch.zeros((3, 4, d), dtype=dtype, device=DEV)
+    plan = gpu.CrossPlan([0, 3], [0, n], 4, kv, d, device=DEV)
+    G = torch.ones_like(zero)
+    mean = V.double().mean(0).repeat_interleave(2, 0).expand(3, 4, d).cpu()
+    size = V.double().abs().mean(0).repeat_interleave(2, 0).expand(3, 4, d).cpu()
+    O, lse = gpu.cross_forward(plan, zero, V, V, scale=scale)
+    # (1 / n is rounded to 16 bits, in the cache to 11)
+    close(O, mean, (u + 256 * F32) * size + u * mean.abs() + 2.0 ** -25, "O")
+    close(lse, torch.full((3, 4), math.log(n)).double(), torch.full((3, 4), 16 * F32).double(),
+          "lse")
+    dV = gpu.cross_backward(plan, zero, V, V, O, G, lse, scale=scale)[2]
+    want = torch.full(V.shape, 6 / n, dtype=torch.float64)
+    close(dV, want, (2 * u + 256 * F32) * want, "dV")
+    cache = _cache(gpu, 10, 16, kv, d)
+    table, lens = torch.arange(5, 10, dtype=torch.int32, device=DEV).view(1, -1), _int32([n])
+    pages = torch.arange(5, dtype=torch.int32, device=DEV)
+    for t in (table, pages.view(1, -1)):
+        gpu.cache_write(cache, V[None], V[None], t, lens)
+    back = gpu.cache_read(cache, table, lens, n, torch.float32)[1][0].double()
+    mean = back.mean(0).repeat_interleave(2, 0)[None].cpu()
+    size = back.abs().mean(0).repeat_interleave(2, 0)[None].cpu()
+    for k, more in ((n, {}), (2 * n, dict(prefix=pages, prefix_len=n))):
+        O, lse = gpu.cache_attend(cache, zero[None, :1], table, lens, scale=scale, **more)
+        close(O[0], mean, (2.0 ** -11 + 256 * F32) * size + u * mean.abs() + 2.0 ** -24 * 4, "O")
+        close(lse[0], torch.full((1, 4), math.log(k)).double(),
+              torch.full((1, 4), 16 * F32).double(), "lse")
