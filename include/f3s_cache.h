@@ -96,7 +96,7 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
  * codes, before and after scaling, and |V| times the number of keys have to stay
  * below 2^127); the products with V are f16, relative to the largest power of two
  * among the values that the token has seen so far: beside 2^-11 of its probability
- * a key adds an error of up to 2^-25 of the largest |value| that the token sees.
+ * a key adds an error of up to 2^-33 of the largest |value| that the token sees.
  * The work is divided on the device, by the lengths that it finds there: a captured
  * call stays right when they change.  A prefix is read once for many sequences: for
  * 16 query rows of a key head at a time, or, with many rows and much work, for 128

@@ -64,7 +64,8 @@ size_t f3s_cross_backward_workspace_bytes(f3s_cross_plan_t plan);
  * Inputs must be finite where they are not padding.  Outputs and workspace must
  * not overlap each other or an input.  Scores, softmax and sums in fp32 (scaled
  * scores and |V| times the number of keys have to stay below 2^127); the
- * probabilities enter the value product in dtype, O is rounded once.
+ * probabilities enter the value product in dtype (fp16: relative to the row's
+ * largest, one below 2^-23 keeps multiples of 2^-33), O is rounded once.
  * Asynchronous on `stream`; no allocation, no synchronisation; deterministic.
  * Calls on one plan may overlap in time, each with a workspace of its own.
  */

@@ -170,7 +170,8 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a)
     const PartRows own = {((int64_t)d.x * a.few.n_kv + kh) * a.rows + (r - (int64_t)b * a.rows),
                           (int64_t)a.few.n_kv * a.rows, d.y};
     const PartRows prefix = {a.prefix_part + kh * all + r, a.few.n_kv * all, a.prefix_splits};
-    join_row<D, kIn, kSplit>(a.few.part_o, a.few.part_ml, own, prefix, out, a.few.O, a.few.lse);
+    join_row<D, kIn, kInF16, kSplit>(a.few.part_o, a.few.part_ml, own, prefix, out, a.few.O,
+                                     a.few.lse);
 }
 
 template <int D, int kIn>

@@ -10,8 +10,8 @@
 // operation, a value's relative to the largest that the workgroup has met, which
 // the sums are multiples of.  A code has four bits, so the widened value is exact
 // unless its row is 2^15 times smaller than that largest one (f16; 2^117 in
-// bf16); then it is off by at most 2^-25 of the largest power, which is less than
-// the probabilities' own rounding leaves.
+// bf16); then it is off by at most 2^-25 of the largest power, which is no more
+// than the probabilities' own rounding leaves.
 //
 // 512 rows of a key head, 16,384 keys, 8 key heads of 128: 54 us, 635 TFLOP/s; a
 // tile of 64 keys takes 2.7 us, the beginning and the partial results 14.
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
     f16v o[D / 32];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) o[d] = zero16();
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;  // maximum, lowered by kRaise
     int ref = 0;  // o holds multiples of 2^(ref - 127)
 
     constexpr int kSets = code_sets(D);
@@ -190,10 +190,10 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
         float mx = s[0][0];
 #pragma unroll
         for (int e = 1; e < 16 * kBlocks; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
-        mx = max_xor32(mx) * by;
+        mx = max_xor32(mx) * by - kRaise<kInF16>;
         const float m_new = fmaxf(m_run, mx);
         // (a maximum that has grown by less than 2^6 is not worth the products: the
-        // probabilities may as well be up to 64, in f16 with the same 11 bits)
+        // probabilities may as well be 64 times larger, with the same 11 bits)
         if (__ballot(m_new > m_run + 6.f) || top[b.kIndex] > ref) {
             float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
             l_run *= alpha;
@@ -240,14 +240,14 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
         if (t + 1 < n) step(t + 1, Buffer<1>(), Buffer<0>());
     }
 
-    const float l = sum_xor32(l_run);
+    const float l = __builtin_ldexpf(sum_xor32(l_run), -kRaise<kInF16>);
     const int64_t part = a.prefix_part + ((int64_t)split * a.few.n_kv + head) * all +
                          (int64_t)tile * kManyRows + 32 * wave;
     uint8_t *const lds = wave == 0 ? s0.k : wave == 1 ? s0.v : wave == 2 ? s1.k : s1.v;
     __syncthreads();  // nobody reads the tiles
-    store_part32<D, T::kBytes / 128 / 32 * 32>(lds, o, __builtin_ldexpf(1.f, ref - 127),
-                                               a.few.part_o + part * D, D, rows - 32 * wave,
-                                               lane);
+    store_part32<D, T::kBytes / 128 / 32 * 32>(
+        lds, o, __builtin_ldexpf(1.f, ref - 127 - kRaise<kInF16>), a.few.part_o + part * D, D,
+        rows - 32 * wave, lane);
     if (there && lane < 32) {
         a.few.part_ml[2 * (part + lane)] = m_run;
         a.few.part_ml[2 * (part + lane) + 1] = l;

@@ -42,7 +42,7 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossMergeArgs a)
     const int r = ((int)blockIdx.x - rec * a.blocks) * kPer +
                   (kSplit ? 0 : (int)threadIdx.x / (D / 4));
     if (r >= g.rows || (!kSplit && (int)threadIdx.x >= kPer * (D / 4))) return;
-    join_row<D, kIn, kSplit>(a.part_o, a.part_ml, {(int64_t)g.part + r, g.stride, g.count},
+    join_row<D, kIn, kIn, kSplit>(a.part_o, a.part_ml, {(int64_t)g.part + r, g.stride, g.count},
                              {0, 0, 0}, query_row(a.q, g.head, (int64_t)g.row + r), a.O, a.lse);
 }
 

@@ -148,6 +148,15 @@ __device__ __forceinline__ float from16(_Float16 x)
         return (float)x;
 }
 
+// Probabilities enter an f16 product times 2^kRaise.  Relative to the row's largest,
+// one below 2^-14 would be no normal number of f16 and lose bits, and where many
+// keys are alike all of them are off the same way (by 2.4% at 2^-19.6).  With 2^9,
+// and the 2^6 by which a maximum may lag behind (many_rows.h), all of f16 is used:
+// 11 bits down to 2^-23.  The running maximum is kept that much lower, which costs a
+// subtraction a tile.  bf16 has fp32's exponents.
+template <int kPV>
+constexpr int kRaise = kPV == kInF16 ? 9 : 0;
+
 __device__ __forceinline__ float sum_xor16_32(float v)
 {
     int b = __builtin_bit_cast(int, v);
@@ -175,13 +184,14 @@ __device__ __forceinline__ void store4(void *O, int64_t at, f4 v)
     *reinterpret_cast<h4 *>(reinterpret_cast<_Float16 *>(O) + at) = x;
 }
 
-// Natural log-sum-exp of a row with maximum m (base 2) and sum l.
+// Natural log-sum-exp of a row with sum l relative to 2^m.
 __device__ __forceinline__ float natural_lse(float m, float l)
 {
     return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// The partial results of a row: n of them at rows first, first + stride, ...
+// The partial results of a row: n of them at rows first, first + stride, ...  Each
+// is an output and a sum l relative to 2^(m + kRaise), m its (lowered) maximum.
 struct PartRows {
     int64_t first, stride;
     int n;
@@ -196,7 +206,7 @@ struct PartRows {
 // many the workgroups and what they read: of 128 values, 1,024 rows of 17 pieces
 // took 8.8 us split and 14.6 by one group, 2,048 rows 8.4 and 9.2, 4,096 rows 9.2
 // and 8.4, 8,192 rows of 9 pieces 14.5 and 10.1.
-template <int D, int kIn, bool kSplit>
+template <int D, int kIn, int kPV, bool kSplit>
 __device__ __forceinline__ void join_row(const float *part_o, const float *part_ml,
                                          const PartRows &x, const PartRows &y, int64_t out,
                                          void *O, float *lse)
@@ -264,7 +274,7 @@ __device__ __forceinline__ void join_row(const float *part_o, const float *part_
         }
     }
     store4<kIn>(O, out * D + c, o * (l == 0.f ? 0.f : 1.f / l));
-    if (c == 0) lse[out] = natural_lse(m, l);
+    if (c == 0) lse[out] = natural_lse(m + kRaise<kPV>, l);
 }
 
 // Rows up to which a workgroup joins one.
@@ -304,7 +314,7 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
     f4 o[D / 16];
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) o[t] = f4{0.f, 0.f, 0.f, 0.f};
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;  // maximum, lowered by kRaise
     int ref = 0;  // cache: this row's o holds multiples of 2^(ref - 127)
 
     u4 kr[T::kLoads], vr[T::kLoads];
@@ -407,7 +417,7 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
 #pragma unroll
         for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
         mx = max_xor32(max_xor16(mx));
-        const float m_new = fmaxf(m_run, mx);
+        const float m_new = fmaxf(m_run, mx - kRaise<kPV>);
         const float m_ref = m_new == -INFINITY ? 0.f : m_new;  // (no key yet)
         float alpha = __builtin_amdgcn_exp2f(m_run - m_ref);
         bool rescale = m_new > m_run;
@@ -463,14 +473,19 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
     }
 
     // the four waves' states meet: scaled to the common maximum and summed
-    float l_all = sum_xor16_32(l_run);
+    constexpr float kLower = 1.f / (1 << kRaise<kPV>);
+    const float l_all = sum_xor16_32(l_run) * kLower;
     float *const mine = reinterpret_cast<float *>(s_tile[wave]);
     tile_fence<kFewWaves>();
-    if (kCache) {
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d)
+    for (int d = 0; d < D / 16; ++d) {
+        if (kCache) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) o[d][k] = __builtin_ldexpf(o[d][k], ref - 127);
+            for (int k = 0; k < 4; ++k)
+                o[d][k] = __builtin_ldexpf(o[d][k], ref - 127 - kRaise<kPV>);
+        } else {
+            o[d] *= kLower;
+        }
     }
 #pragma unroll
     for (int d = 0; d < D / 16; ++d)
@@ -505,7 +520,7 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
         } else {
             const int64_t at = query_row(a.q, it.head, it.row + r);
             store4<kIn>(a.O, at * D + c, sum * (l == 0.f ? 0.f : 1.f / l));
-            if (c == 0) a.lse[at] = natural_lse(m, l);
+            if (c == 0) a.lse[at] = natural_lse(m + kRaise<kPV>, l);
         }
     }
 }

@@ -319,7 +319,7 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
     f16v o[D / 32];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) o[d] = zero16();
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;  // maximum, lowered by kRaise
 
     T tk, tv;
     const uint32_t row_bytes = (uint32_t)a.n_kv * (2 * D);
@@ -362,10 +362,10 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
         float mx = s[0][0];
 #pragma unroll
         for (int e = 1; e < 16 * kBlocks; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
-        mx = max_xor32(mx) * a.sl2;
+        mx = max_xor32(mx) * a.sl2 - kRaise<kIn>;
         const float m_new = fmaxf(m_run, mx);
         // (a maximum that has grown by less than 2^6 is not worth the products: the
-        // probabilities may as well be up to 64, with the same bits)
+        // probabilities may as well be 64 times larger, with the same bits)
         if (__ballot(m_new > m_run + 6.f)) {
             const float alpha =
                 __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
@@ -393,13 +393,14 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
         products_done();
     };
     walk_tiles<T::kDirect>((it.others + kKeys - 1) / kKeys, fetch, put, work);
-    const float l = sum_xor32(l_run);
+    constexpr float kLower = 1.f / (1 << kRaise<kIn>);
+    const float l = sum_xor32(l_run) * kLower;
     const int col = 4 * (lane >> 5);
     uint8_t *const lds = wave == 0 ? s_k0 : wave == 1 ? s_k1 : wave == 2 ? s_v0 : s_v1;
     __syncthreads();  // nobody reads the tiles
     if (it.part >= 0) {
         store_part32<D, T::kBytes / 128 / 32 * 32>(
-            lds, o, 1.f, a.part_o + ((int64_t)it.part + 32 * wave) * D, D, it.rows - 32 * wave,
+            lds, o, kLower, a.part_o + ((int64_t)it.part + 32 * wave) * D, D, it.rows - 32 * wave,
             lane);
         if (there && col == 0) {
             a.part_ml[2 * ((int64_t)it.part + mine)] = m_run;
@@ -408,9 +409,9 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
         return;
     }
     auto at = [&](int r) { return query_row(a.q, it.head, (int64_t)it.row + 32 * wave + r); };
-    store_rows32<D, kIn, D>(lds, o, l == 0.f ? 0.f : 1.f / l, a.O, at, it.rows - 32 * wave, 0,
+    store_rows32<D, kIn, D>(lds, o, l == 0.f ? 0.f : kLower / l, a.O, at, it.rows - 32 * wave, 0,
                             lane);
-    if (there && col == 0) a.lse[at(lane & 31)] = natural_lse(m_run, l);
+    if (there && col == 0) a.lse[at(lane & 31)] = natural_lse(m_run + kRaise<kIn>, l);
 }
 
 template <int D, int kIn>

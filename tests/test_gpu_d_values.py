@@ -156,3 +156,48 @@ def test_largest_scales(gpu, monkeypatch, rows, dtype, scale):
         close(O[0], mean, (2.0 ** -11 + 256 * F32) * size + u * mean.abs() + 2.0 ** -24 * 4, "O")
         close(lse[0], torch.full((1, 4), math.log(k)).double(),
               torch.full((1, 4), 16 * F32).double(), "lse")
+
+
+# ---- small probabilities in sums ---------------------------------------------------------
+
+@pytest.mark.parametrize("way", ["cross 16", "cross 128", "own", "prefix 16", "prefix 128"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [32, 64, 128, 160])
+def test_small_probabilities(gpu, monkeypatch, way, dtype, d):
+    """Every 32nd key has 2^19.64 times the probability of the others (20.5 of fp16's
+    smallest steps, were it 1) and a value of zero: the result is the sum of the small
+    ones, which keep their 11 bits (8 in bf16 cross attention)."""
+    kind, _, rows = way.partition(" ")
+    monkeypatch.setenv("F3S_CROSS_ROWS", rows or "16")
+    monkeypatch.setenv("F3S_PREFIX_ROWS", rows or "16")
+    gen = torch.Generator().manual_seed(d)
+    u, n, kv, g = half_step(dtype), 800, 2, 2
+    up = u if kind == "cross" else 2.0 ** -11
+    scale = 19.64 * math.log(2)
+    K, V = torch.zeros((n, kv, d)), 512 + 256 * torch.rand((n, kv, d), generator=gen)
+    K[::32, :, 0], V[::32] = 1, 0
+    Q = torch.zeros((3, kv * g, d))
+    Q[..., 0] = 1
+    Q, K, V = (x.to(dtype).to(DEV) for x in (Q, K, V))
+    if kind == "cross":
+        plan = gpu.CrossPlan([0, 3], [0, n], kv * g, kv, d, device=DEV)
+        O, lse = gpu.cross_forward(plan, Q, K, V, scale=scale)
+    else:
+        page = 16
+        cache = _cache(gpu, n // page + 1, page, kv, d)
+        pages = torch.arange(n // page, dtype=torch.int32, device=DEV).view(1, -1)
+        gpu.cache_write(cache, K[None], V[None], pages, _int32([n]))
+        K, V = (x[0] for x in gpu.cache_read(cache, pages, _int32([n]), n, torch.float32))
+        if kind == "own":
+            table, lens, more = pages.expand(3, -1).contiguous(), [n] * 3, {}
+        else:
+            table, lens = torch.zeros((3, 1), dtype=torch.int32, device=DEV), [0] * 3
+            more = dict(prefix=pages[0], prefix_len=n)
+        O, lse = (x[:, 0] for x in gpu.cache_attend(cache, Q[:, None], table, _int32(lens),
+                                                    scale=scale, **more))
+    for h in range(kv * g):
+        f = attention(Q[:, h].double(), K[:, h // g].double(), V[:, h // g].double(), scale, u)
+        # P's rounding, the probabilities' 32-bit error, O's own rounding
+        tol = (up + f["ep"][:, None]) * f["O"].abs() + u * f["O"].abs()
+        close(O[:, h], f["O"].cpu(), tol.cpu(), (way, h))
+        close(lse[:, h], f["lse"].cpu(), f["lse_tol"].cpu(), ("lse", way, h))
