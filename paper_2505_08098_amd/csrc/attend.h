@@ -23,6 +23,7 @@ struct AttendArgs {
     int32_t share;         // workgroups, about, that the own keys of a key head and row
                            // block are divided among
     int32_t own_items;     // workgroups per key head and row block: share + n_seqs
+    bool whole;            // or n_seqs: every sequence is one item
     bool direct;           // one workgroup has all keys: no partial results
     // the prefix, all sequences' rows together
     bool prefix_many;       // by the kernel of many rows
@@ -83,6 +84,10 @@ __device__ __forceinline__ OwnItem own_item(const AttendArgs &a, int i)
 {
     const int lane = threadIdx.x & 63;
     const int64_t cap = (int64_t)a.max_pages << a.few.page_shift;
+    if (a.whole) {
+        const int32_t keys = cache_keys(a.lens[i], cap);
+        return OwnItem{i, i, 1, units_of(keys), keys};
+    }
     int total = 0;
     for (int b = lane; b < a.n_seqs; b += 64) total += units_of(cache_keys(a.lens[b], cap));
     const int per = units_per_item(wave_sum(total), a.share);

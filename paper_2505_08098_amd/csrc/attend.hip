@@ -32,6 +32,12 @@ constexpr int64_t kManyScores = 6000000;
 //   64 sequences: 15.4, 15.2 and 21.3, 21.2;   21.5, 21.3 and 28.4, 28.0
 // (16 of 750 to 1,500: 21.3, 21.2 and 16.2, 16.1).
 constexpr int64_t kDirectUnits = 14;
+// Sequences up to which own keys are divided: every workgroup looks through all
+// lengths for its item, which grows with the square of their number.  One new token,
+// 8 key heads of 64, in us divided and whole: 8,193 sequences of up to 200 keys
+// 3,480 and 270, with one of 131,072 among them 3,477 and 1,016 (1 key head: 597 and
+// 45, 616 and 918); 32,768 sequences 50,000 and 1,080.
+constexpr int64_t kMostDivided = 8192;
 // What a piece of the prefix costs beside its keys (queries, partial results),
 // in units of 64 keys.
 constexpr int64_t kPieceCost = 3;
@@ -71,10 +77,10 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     // (no more than the table has places for)
     const int64_t most = ceil_div(cap_units * n_seqs, f3s::kLeastUnits);
     if (share > most) share = most;
-    if (share < 1 || a->direct) share = 1;  // (a sequence is one piece)
+    if (share < 1) share = 1;
     a->share = (int32_t)share;
-    a->own_items = a->direct || cap_units <= f3s::kLeastUnits ? n_seqs
-                                                              : (int32_t)(share + n_seqs);
+    a->whole = a->direct || cap_units <= f3s::kLeastUnits || n_seqs > kMostDivided;
+    a->own_items = a->whole ? n_seqs : (int32_t)(share + n_seqs);
     if (prefix_rows)
         a->prefix_many = prefix_rows == f3s::kManyRows;
     else
