@@ -4,6 +4,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <memory>
 #include <new>
 #include <vector>
 
@@ -70,7 +71,8 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
     }
     *st = F3S_ERR_TOO_LARGE;
     // (a row's number and a tile add up to less than 2^31)
-    if (q_ptr[n] * g > 0x7FFFF000 || k_ptr[n] > 0x7FFFF000 || (double)q_ptr[n] * n_heads / 16 + n_heads > 2147483647.0)
+    if (q_ptr[n] * g > 0x7FFFF000 || k_ptr[n] > 0x7FFFF000 ||
+        (double)q_ptr[n] * n_heads / 16 + n_heads > 2147483647.0)
         return nullptr;
     Division f, dq, dkv;
     const char *rows_env = getenv("F3S_CROSS_ROWS");
@@ -85,7 +87,8 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
              kUnits * f3s::dkv_waves(d) / f3s::dkv_halves(d));
     if (!f.fits() || !dq.fits() || !dkv.fits()) return nullptr;
 
-    f3s_cross_plan_s *p = new f3s_cross_plan_s;
+    std::unique_ptr<f3s_cross_plan_s, void (*)(f3s_cross_plan_t)> p(new f3s_cross_plan_s,
+                                                                    f3s_cross_destroy);
     p->n_heads = n_heads;
     p->n_kv = n_kv;
     p->g = (int32_t)g;
@@ -132,11 +135,7 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
         e = hipMemcpy(p->store, host.data(), bytes, hipMemcpyHostToDevice);
     }
     *st = f3s::status_of(e);
-    if (e != hipSuccess) {
-        f3s_cross_destroy(p);
-        return nullptr;
-    }
-    return p;
+    return e == hipSuccess ? p.release() : nullptr;
 }
 
 bool on_device(const f3s_cross_plan_s *p, hipStream_t stream)
