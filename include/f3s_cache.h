@@ -52,7 +52,8 @@ typedef struct {
  *   lens       device int32 [n_seqs], the lengths after this call
  * Two rows of one call must not lie at the same place (a page named twice):
  * what such a place then holds is not defined.  K and V must not overlap the
- * cache.  F3S_ERR_TOO_LARGE beyond 2^27 rows (sequences, tokens, key heads).
+ * cache.  F3S_ERR_TOO_LARGE from 2^27 rows on (sequences, tokens, key heads; from
+ * 2^28 up to d = 128, 2^29 up to 64, 2^30 at 32).
  * Asynchronous on `stream`; no allocation, no synchronisation.
  */
 f3s_status_t f3s_cache_write(const f3s_cache_t *cache, const void *K, const void *V,
@@ -92,7 +93,8 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
  *              256-byte aligned; needs no initialisation, must not overlap
  *              anything else of the call, and calls that overlap in time need
  *              one each.  NULL if that is 0
- * Inputs must be finite.  Scores, sums and statistics are fp32 (products of Q with
+ * Inputs must be finite, and so must every row below a sequence's length: one that
+ * is not may reach all of its tokens, those before it too.  Scores, sums and statistics are fp32 (products of Q with
  * codes, before and after scaling, and |V| times the number of keys have to stay
  * below 2^127); the products with V are f16, relative to the largest power of two
  * among the values that the token has seen so far: beside 2^-11 of its probability

@@ -27,10 +27,13 @@ constexpr int64_t kFewPrefixRows = 64;
 constexpr int64_t kManyScores = 6000000;
 // Units that a table has room for up to which no sequence is divided (so that one
 // launch does).  Calls over 250 to 500 and 445 to 890 own keys, 8 key heads of 128,
-// us on the GPU and from one call to the next, whole and in pieces:
-//    4 sequences:  9.5, 11.3 and 10.0, 14.3;   13.0, 13.3 and 10.3, 14.3
-//   64 sequences: 15.4, 15.2 and 21.3, 21.2;   21.5, 21.3 and 28.4, 28.0
-// (16 of 750 to 1,500: 21.3, 21.2 and 16.2, 16.1).
+// us from one call to the next and from one to the next in a captured graph, whole
+// and in pieces:
+//    4 sequences: 10.5,  8.5 and 14.6, 10.0;   12.6, 12.2 and 14.5, 10.1
+//   16 sequences: 10.5,  8.6 and 14.6, 10.3;   12.6, 12.3 and 14.5, 12.2
+//   64 sequences: 14.0, 14.1 and 21.1, 21.0;   19.9, 20.1 and 27.9, 27.9
+// (16 of 750 to 1,500 took 21.3 us on the GPU whole and 16.2 in pieces.)  A few
+// sequences that fill such a table would gain 2 us from pieces in a graph.
 constexpr int64_t kDirectUnits = 14;
 // Sequences up to which own keys are divided: every workgroup looks through all
 // lengths for its item, which grows with the square of their number.  One new token,

@@ -92,10 +92,9 @@ struct Division {
         return per;
     }
 
-    // `slots`: workgroups that run at once.  A range is divided into pieces of at
-    // most as many units for as many as `least` rows or more; what does not come out
-    // even is spread over them, so that the shortest has half as many rows (128 of
-    // 256: 320 rows as 128 and 192).
+    // `slots`: workgroups that run at once.  A range is divided evenly into the fewest
+    // pieces of at most so many units, those of `least` rows or more: the shortest
+    // piece has half of `least` (of 256: 320 rows are 128 and 192).
     void make(std::vector<Range> ranges, int32_t heads, int64_t tile, int64_t unit,
               int64_t least, int64_t slots, double launch = kLaunch)
     {

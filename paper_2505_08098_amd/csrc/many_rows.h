@@ -16,8 +16,13 @@
 //
 // 2 x 4,050 tokens, 32 heads of 128 over 8, 8,100 keys, bf16: 1,076 us, 1,000
 // TFLOP/s, where a library's product of 8,192^3 reaches 1,200.  The clock falls to
-// 1.9 GHz, the matrix units are busy 47% of its cycles and the vector unit as long
-// again, and more waves or earlier reads gain nothing: power seems to be the bound.
+// 1.9 GHz, the matrix units are busy 48% of its cycles, the vector unit as long again
+// and LDS 37% (12 of these 37 bank conflicts, below); more waves or earlier reads gained
+// nothing.  Power seems to be the bound; what the conflicts cost is not measured.
+//
+// P enters the value product in the inputs' type: rounded to nearest, a bf16 result
+// is off by 0.0023 of its size instead of the 0.0017 of its own rounding (fp16 0.0003
+// and 0.0002).  Two 16-bit terms of P would take half as many products again.
 #pragma once
 
 #include "few_rows.h"
@@ -58,8 +63,12 @@ __device__ __forceinline__ f16v zero16()
 // d a power of two: the loads write LDS themselves (16 bytes a lane), which
 // takes no registers.  A wave's load fills 1 KB in lane order, so rows cannot be
 // padded; instead the 16-byte pieces of a row change places, piece p of row r
-// standing at p ^ swizzle(r), such that the lanes of an operand read (8 rows of
-// one piece, or 4 rows of two neighbouring ones) meet different banks.
+// standing at p ^ swizzle(r).  At d = 128 the lanes of a plain operand read (rows32)
+// then meet different banks, but those of a transposed one (cols32: 4 rows of four
+// neighbouring pieces at a time) meet each bank twice, since a row moves its pieces
+// by two: a third of the forward's LDS cycles and a quarter of the backward's are
+// these conflicts (SQ_LDS_BANK_CONFLICT over SQ_LDS_IDX_ACTIVE: 1.69e7 of 5.04e7,
+// 1.67e7 of 6.65e7 and 3.29e7 of 1.34e8, 2 x 4,050 x 4,050, 16 heads of 128 over 4).
 // Other d: through registers, into padded rows.
 template <int D, int R = many_keys(D)>
 struct ManyTile {

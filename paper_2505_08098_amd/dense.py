@@ -1,6 +1,7 @@
 """Dense attention beside the sparse operator: cross attention over a ragged
 batch, and attention over an 8-bit key/value cache (include/f3s_cross.h,
-include/f3s_cache.h).  Argument marshalling only, like ``binding``.
+include/f3s_cache.h).  Argument marshalling only, like ``binding``: results carry
+no autograd graph, also where an operand requires gradients.
 
     plan = f3s.CrossPlan(q_ptr, k_ptr, heads, kv_heads, d)     # once per batch
     O, lse = f3s.cross_forward(plan, Q, K, V)
