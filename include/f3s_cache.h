@@ -52,8 +52,10 @@ typedef struct {
  *   lens       device int32 [n_seqs], the lengths after this call
  * Two rows of one call must not lie at the same place (a page named twice):
  * what such a place then holds is not defined.  K and V must not overlap the
- * cache.  F3S_ERR_TOO_LARGE from 2^27 rows on (sequences, tokens, key heads; from
- * 2^28 up to d = 128, 2^29 up to 64, 2^30 at 32).
+ * cache, nor its four parts each other, but that one place for keys and values takes
+ * the same rows as K and V (a cache that is only read may be laid out in any way).
+ * F3S_ERR_TOO_LARGE from 2^27 rows on (sequences, tokens, key heads; from 2^28 up
+ * to d = 128, 2^29 up to 64, 2^30 at 32).
  * Asynchronous on `stream`; no allocation, no synchronisation.
  */
 f3s_status_t f3s_cache_write(const f3s_cache_t *cache, const void *K, const void *V,

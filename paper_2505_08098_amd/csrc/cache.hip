@@ -186,6 +186,12 @@ struct Read {
 
 bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
+bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && na && nb && x < y + nb && y < x + na;
+}
+
 // Whether n bytes at p share any with the cache or, where they are written
 // (`out`), with what is read beside it.
 bool meets(const void *p, size_t n, const RowArgs &a, bool out)
@@ -198,12 +204,22 @@ bool meets(const void *p, size_t n, const RowArgs &a, bool out)
     } with[] = {{a.c.k, places * a.c.d}, {a.c.v, places * a.c.d}, {a.c.k_exp, places},
                 {a.c.v_exp, places}, {a.table, out ? seqs * a.max_pages * 4 : 0},
                 {a.lens, out ? seqs * 4 : 0}};
-    const uintptr_t x = (uintptr_t)p;
-    for (const auto &w : with) {
-        const uintptr_t y = (uintptr_t)w.p;
-        if (p && w.n && x < y + w.n && y < x + n) return true;
-    }
+    for (const auto &w : with)
+        if (overlap(p, n, w.p, w.n)) return true;
     return false;
+}
+
+// Whether rows that are written to the cache would be written over others, some of
+// its parts sharing memory.  (One place for K and V may get the same rows twice.)
+bool folded(const f3s_cache_t &c, bool same_rows)
+{
+    const size_t places = (size_t)c.n_pages * c.n_kv_heads * c.page_size;
+    const size_t codes = places * c.d;
+    if (overlap(c.k, codes, c.k_exp, places) || overlap(c.v, codes, c.k_exp, places) ||
+        overlap(c.k, codes, c.v_exp, places) || overlap(c.v, codes, c.v_exp, places))
+        return true;
+    if (same_rows && c.k == c.v && c.k_exp == c.v_exp) return false;
+    return overlap(c.k, codes, c.v, codes) || overlap(c.k_exp, places, c.v_exp, places);
 }
 
 }  // namespace
@@ -259,7 +275,7 @@ f3s_status_t f3s_cache_write(const f3s_cache_t *cache, const void *K, const void
         return f3s::set_status(F3S_ERR_UNSUPPORTED);
     if (a.rows == 0) return F3S_OK;
     const size_t bytes = (size_t)a.rows * cache->d * 2;
-    if (!K || !V || !f3s::aligned(K, 16) || !f3s::aligned(V, 16) ||
+    if (!K || !V || !f3s::aligned(K, 16) || !f3s::aligned(V, 16) || f3s::folded(*cache, K == V) ||
         f3s::meets(K, bytes, a, false) || f3s::meets(V, bytes, a, false))
         return f3s::set_status(F3S_ERR_INVALID_VALUE);
     return f3s::set_status(f3s::status_of(
@@ -277,9 +293,8 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
         return f3s::set_status(F3S_ERR_UNSUPPORTED);
     if (a.rows == 0 || (!K && !V)) return F3S_OK;
     const size_t bytes = (size_t)a.rows * cache->d * (dtype == F3S_DTYPE_F32 ? 4 : 2);
-    const uintptr_t k = (uintptr_t)K, v = (uintptr_t)V;
     if (!f3s::aligned(K, 16) || !f3s::aligned(V, 16) || f3s::meets(K, bytes, a, true) ||
-        f3s::meets(V, bytes, a, true) || (K && V && k < v + bytes && v < k + bytes))
+        f3s::meets(V, bytes, a, true) || f3s::overlap(K, bytes, V, bytes))
         return f3s::set_status(F3S_ERR_INVALID_VALUE);
     return f3s::set_status(
         f3s::status_of(f3s::with_d<f3s::Read>(cache->d, a, K, V, dtype, stream)));

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2505_08098_amd import dense
-from test_dense_refusals import A, HIP, INVALID, _attend, _cache
+from test_dense_refusals import A, HIP, INVALID, _attend, _cache, _read, _write
 
 no_gpu = pytest.mark.skipif(torch.cuda.is_available(),
                             reason="made-up addresses: only where nothing can launch")
@@ -75,3 +75,44 @@ def test_cross_workspace_over_an_input(gpu):
     assert torch.equal(O, want[0]) and torch.equal(lse, want[1])
     for a, b in zip((dQ, dK, dV), gpu.cross_backward(plan, Q, K, V, O, G, lse)):
         assert torch.equal(a, b) and math.isfinite(float(a.float().sum()))
+
+
+@no_gpu
+@pytest.mark.parametrize("over", [
+    dict(v=A), dict(v=A + 256), dict(k_exp=A), dict(v_exp=2 * A + 16384 - 16),
+    dict(v_exp=3 * A), dict(k_exp=4 * A + 16),
+])
+def test_cache_whose_parts_overlap_is_not_written(lib, over):
+    """(It may be read: K and V may be the same rows.)"""
+    assert _write(lib, _cache(**over)) == INVALID
+    assert _read(lib, _cache(**over)) == HIP
+    assert _attend(lib, _cache(**over)) == HIP
+    assert _write(lib, _cache(v=A + 16384, k_exp=4 * A - 256)) == HIP      # side by side
+
+
+@no_gpu
+def test_one_place_for_keys_and_values_takes_the_same_rows(lib):
+    one = _cache(v=A, v_exp=3 * A)
+    assert _write(lib, one, K=5 * A, V=5 * A) == HIP
+    assert _write(lib, one) == INVALID
+    assert _write(lib, _cache(v=A), K=5 * A, V=5 * A) == INVALID      # (powers apart)
+    assert _write(lib, _cache(v=A, k_exp=A + 64, v_exp=A + 64), K=5 * A, V=5 * A) == INVALID
+
+
+@pytest.mark.gpu
+def test_rows_that_are_keys_and_values(gpu):
+    dev = torch.device("cuda:0")
+    two, one = gpu.Cache.empty(6, 16, 2, 64), gpu.Cache.empty(6, 16, 2, 64)
+    one = gpu.Cache(one.k, one.k, one.k_exp, one.k_exp)
+    X = torch.randn((2, 40, 2, 64), device=dev).bfloat16()
+    table = torch.tensor([[0, 2, 4], [5, 3, 1]], dtype=torch.int32, device=dev)
+    lens = torch.tensor([40, 33], dtype=torch.int32, device=dev)
+    Q = torch.randn((2, 3, 6, 64), device=dev).bfloat16()
+    results = []
+    for cache in (two, one):
+        gpu.cache_write(cache, X, X, table, lens)
+        results.append(gpu.cache_attend(cache, Q, table, lens)
+                       + gpu.cache_read(cache, table, lens, 40, torch.bfloat16))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    with pytest.raises(gpu.F3SError):
+        gpu.cache_write(one, X, X.clone(), table, lens)
