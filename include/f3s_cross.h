@@ -79,13 +79,14 @@ f3s_status_t f3s_cross_forward(f3s_cross_plan_t plan, const void *Q, const void 
  *   delta_i = dO_i . O_i,  dS_ij = P_ij (dO_i . V_j - delta_i),
  *   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO,
  * dK and dV summed over the query heads of a key head.  dO, dQ as Q; dK, dV
- * as K; every element is written.  P and dS enter the products in dtype.  In fp16
- * P is taken times 2^12, so that probabilities down to 2^-26 keep 11 bits; dS is
- * not, and fp16 gradients need the usual scaling of the loss: a dS below 2^-14
- * loses bits.  Sums in fp32, gradients rounded once.  delta comes from the rounded
- * O: where one key has nearly all of a row's probability, dS is what is left of two
- * equal numbers and keeps that rounding (2^-9 of |dO . O| in bf16).  Otherwise as
- * the forward.
+ * as K; every element is written.  P comes from the scores and lse in fp32: at
+ * scaled scores of 2^20 it is off by some percent, and of fp16 inputs dV may be
+ * infinite from 2^24 on.  P and dS enter the products in dtype.  In fp16 P is taken
+ * times 2^12, so that probabilities down to 2^-26 keep 11 bits; dS is not, and fp16
+ * gradients need the usual scaling of the loss: a dS below 2^-14 loses bits.  Sums
+ * in fp32, gradients rounded once.  delta comes from the rounded O: where one key
+ * has nearly all of a row's probability, dS is what is left of two equal numbers
+ * and keeps that rounding (2^-9 of |dO . O| in bf16).  Otherwise as the forward.
  */
 f3s_status_t f3s_cross_backward(f3s_cross_plan_t plan, const void *Q, const void *K,
                                 const void *V, f3s_dtype_t dtype, const void *O,

@@ -99,6 +99,7 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) o[d] = zero16();
     float m_run = -INFINITY, l_run = 0.f;  // maximum, lowered by kRaise
+    uint64_t large = 0;  // lanes where it is from kLargeScore on
     int ref = 0;  // o holds multiples of 2^(ref - 127)
 
     constexpr int kSets = code_sets(D);
@@ -190,11 +191,11 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
         float mx = s[0][0];
 #pragma unroll
         for (int e = 1; e < 16 * kBlocks; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
-        mx = max_xor32(mx) * by - kRaise<kInF16>;
-        const float m_new = fmaxf(m_run, mx);
+        mx = rounded_product(max_xor32(mx), by);
         // (a maximum that has grown by less than 2^6 is not worth the products: the
         // probabilities may as well be 64 times larger, with the same 11 bits)
-        if (__ballot(m_new > m_run + 6.f) || top[b.kIndex] > ref) {
+        if (__ballot(mx - m_run > kRaise<kInF16> + 6.f) || top[b.kIndex] > ref) {
+            const float m_new = fmaxf(m_run, lowered<kInF16>(mx));
             float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
             l_run *= alpha;
             alpha = __builtin_ldexpf(alpha, ref - top[b.kIndex]);
@@ -202,8 +203,15 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) o[d] *= alpha;
             m_run = m_new;
+            large = __ballot(fabsf(m_run) >= kLargeScore && m_run > -INFINITY);
         }
         const float m_ref = m_run == -INFINITY ? 0.f : m_run;
+        if (large) {  // (see rounded_product)
+#pragma unroll
+            for (int e = 0; e < 16 * kBlocks; ++e)
+                s[e >> 4][e & 15] = rounded_product(s[e >> 4][e & 15], by);
+            by = 1.f;
+        }
         float sum = 0.f;
 #pragma unroll
         for (int h = 0; h < kBlocks; ++h)

@@ -156,10 +156,25 @@ __device__ __forceinline__ float from16(_Float16 x)
 // one below 2^-14 would be no normal number of f16 and lose bits, and where many
 // keys are alike all of them are off the same way (by 2.4% at 2^-19.6).  With 2^9,
 // and the 2^6 by which a maximum may lag behind (many_rows.h), all of f16 is used:
-// 11 bits down to 2^-23.  The running maximum is kept that much lower, which costs a
-// subtraction a tile.  bf16 has fp32's exponents.
+// 11 bits down to 2^-23.  The running maximum is kept that much lower, which costs
+// next to nothing.  bf16 has fp32's exponents.
 template <int kPV>
 constexpr int kRaise = kPV == kInF16 ? 9 : 0;
+// A maximum so lowered.  From kLargeScore on fp32's steps no longer hold the 9 (in
+// steps of 16 it would be 16, and the largest probability f16's infinity).
+constexpr float kLargeScore = 0x1p20f;
+template <int kPV>
+__device__ __forceinline__ float lowered(float m)
+{
+    return kRaise<kPV> ? m - (fabsf(m) < kLargeScore ? (float)kRaise<kPV> : 0.f) : m;
+}
+// a * b, rounded: not to be fused with the subtraction of its own maximum, which
+// would leave that rounding (2^7 and more from 2^31 on) in the exponent.
+__device__ __forceinline__ float rounded_product(float a, float b)
+{
+#pragma clang fp contract(off)
+    return a * b;
+}
 
 __device__ __forceinline__ float sum_xor16_32(float v)
 {
@@ -403,7 +418,7 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            x[e] = s[e >> 2][e & 3] * a.sl2;
+            x[e] = rounded_product(s[e >> 2][e & 3], a.sl2);
             if constexpr (kCache)
                 x[e] = __builtin_ldexpf(x[e], (int)((kx[e >> 2] >> (8 * (e & 3))) & 255) - 127);
         }
@@ -422,7 +437,7 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
 #pragma unroll
         for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
         mx = max_xor32(max_xor16(mx));
-        const float m_new = fmaxf(m_run, mx - kRaise<kPV>);
+        const float m_new = fmaxf(m_run, lowered<kPV>(mx));
         const float m_ref = m_new == -INFINITY ? 0.f : m_new;  // (no key yet)
         float alpha = __builtin_amdgcn_exp2f(m_run - m_ref);
         bool rescale = m_new > m_run;

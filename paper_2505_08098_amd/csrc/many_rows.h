@@ -329,6 +329,7 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) o[d] = zero16();
     float m_run = -INFINITY, l_run = 0.f;  // maximum, lowered by kRaise
+    uint64_t large = 0;  // lanes where it is from kLargeScore on
 
     T tk, tv;
     const uint32_t row_bytes = (uint32_t)a.n_kv * (2 * D);
@@ -371,23 +372,31 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
         float mx = s[0][0];
 #pragma unroll
         for (int e = 1; e < 16 * kBlocks; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
-        mx = max_xor32(mx) * a.sl2 - kRaise<kIn>;
-        const float m_new = fmaxf(m_run, mx);
+        mx = rounded_product(max_xor32(mx), a.sl2);
         // (a maximum that has grown by less than 2^6 is not worth the products: the
         // probabilities may as well be 64 times larger, with the same bits)
-        if (__ballot(m_new > m_run + 6.f)) {
+        if (__ballot(mx - m_run > kRaise<kIn> + 6.f)) {
+            const float m_new = fmaxf(m_run, lowered<kIn>(mx));
             const float alpha =
                 __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
             l_run *= alpha;
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) o[d] *= alpha;
             m_run = m_new;
+            large = __ballot(fabsf(m_run) >= kLargeScore);
         }
         const float m_ref = m_run == -INFINITY ? 0.f : m_run;
+        float by = a.sl2;
+        if (large) {  // (see rounded_product)
+#pragma unroll
+            for (int e = 0; e < 16 * kBlocks; ++e)
+                s[e >> 4][e & 15] = rounded_product(s[e >> 4][e & 15], by);
+            by = 1.f;
+        }
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 16 * kBlocks; ++e) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], a.sl2, -m_ref));
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], by, -m_ref));
             s[e >> 4][e & 15] = p;
             sum += p;
         }

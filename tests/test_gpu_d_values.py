@@ -201,3 +201,51 @@ def test_small_probabilities(gpu, monkeypatch, way, dtype, d):
         tol = (up + f["ep"][:, None]) * f["O"].abs() + u * f["O"].abs()
         close(O[:, h], f["O"].cpu(), tol.cpu(), (way, h))
         close(lse[:, h], f["lse"].cpu(), f["lse_tol"].cpu(), ("lse", way, h))
+
+
+# ---- the largest scores --------------------------------------------------------------------
+
+@pytest.mark.parametrize("way", ["cross 16", "cross 128", "own", "prefix 16", "prefix 128"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [3e4, 1e5, 1e6, 1e9, -1e5])
+def test_largest_scores(gpu, monkeypatch, way, dtype, scale):
+    """Scores so large that 32 bits hold no fractions of theirs, up to a key that
+    outweighs all others: the result is that key's value, and the largest score the
+    log-sum-exp."""
+    kind, _, rows = way.partition(" ")
+    monkeypatch.setenv("F3S_CROSS_ROWS", rows or "16")
+    monkeypatch.setenv("F3S_PREFIX_ROWS", rows or "16")
+    gen = torch.Generator().manual_seed(3)
+    n, kv, g, d = 320, 1, 2, 64
+    K, V = torch.zeros((n, kv, d)), torch.randn((n, kv, d), generator=gen)
+    # (multiples of 64, exact in 8 bits next to each other; the largest is the last but 3)
+    K[:, 0, 0] = 64.0 * (torch.arange(n) // 32 + 1)
+    K[n - 3, 0, 0] = 896
+    Q = torch.zeros((3, kv * g, d))
+    Q[..., 0] = 1 if scale > 0 else -1
+    Q, K, V = (x.to(dtype).to(DEV) for x in (Q, K, V))
+    if kind == "cross":
+        plan = gpu.CrossPlan([0, 3], [0, n], kv * g, kv, d, device=DEV)
+        O, lse = gpu.cross_forward(plan, Q, K, V, scale=scale)
+    else:
+        cache = _cache(gpu, n // 16 + 1, 16, kv, d)
+        pages = torch.arange(n // 16, dtype=torch.int32, device=DEV).view(1, -1)
+        gpu.cache_write(cache, K[None], V[None], pages, _int32([n]))
+        k, v = (x[0] for x in gpu.cache_read(cache, pages, _int32([n]), n, dtype))
+        assert torch.equal(k, K)
+        V = v
+        if kind == "own":
+            table, lens, more = pages.expand(3, -1).contiguous(), [n] * 3, {}
+        else:
+            table, lens = torch.zeros((3, 1), dtype=torch.int32, device=DEV), [0] * 3
+            more = dict(prefix=pages[0], prefix_len=n)
+        O, lse = (x[:, 0] for x in gpu.cache_attend(cache, Q[:, None], table, _int32(lens),
+                                                    scale=scale, **more))
+    # one weight over itself, a power of two or (128 rows) next to one: at most the
+    # rounding of 16 bits, and of the quotient
+    want = V[n - 3].double().expand(3, g, d).cpu()
+    u = half_step(dtype)
+    close(O, want, (2 * u + 4 * F32) * want.abs() + 2.0 ** -25, way)
+    # the score's and the logarithm's factor, and their roundings
+    close(lse, torch.full((3, g), 896 * abs(scale), dtype=torch.float64),
+          torch.full((3, g), 8 * F32 * 896 * abs(scale), dtype=torch.float64), ("lse", way))
