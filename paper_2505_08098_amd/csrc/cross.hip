@@ -1,16 +1,12 @@
 // f3s_cross_plan, f3s_cross_forward, f3s_cross_backward: the division of a
 // ragged batch among workgroups, checks, workspace.
-#include <math.h>
 #include <stdlib.h>
-#include <string.h>
 
 #include <memory>
 #include <new>
 #include <vector>
 
-#include "cross_backward.h"
-#include "cross_few.h"
-#include "dense_division.h"
+#include "dense_host.h"
 
 namespace {
 
@@ -20,9 +16,8 @@ using f3s::Division;
 using f3s::Range;
 using f3s::set_status;
 
-constexpr int64_t kUnits = 256;  // compute units
 // Workgroups that the kernel of few rows aims at.
-constexpr int64_t kFewWorkgroups = 4 * kUnits;
+constexpr int64_t kFewWorkgroups = 4 * f3s::kUnits;
 // What a launch that joins pieces costs there, in units of 64 keys, of which one
 // takes 0.4 us (d = 64) to 0.6 us (128).  One token of 4 sequences over 500 to 1,000
 // keys, 8 key heads, whole and in pieces: 8.0 and 6.7 us on the GPU and 9.2 and
@@ -33,14 +28,6 @@ constexpr double kFewLaunch = 10;
 // over 8,192 keys 8.6 and 10.8; 16 rows of 16 sequences over 2,048 keys 28.9 and
 // 26.7 (8 key heads of 128 in the last two).
 constexpr int64_t kFewLongest = 8;
-
-size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
-bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-bool overlaps(const void *a, size_t na, const void *b, size_t nb)
-{
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return na && nb && x < y + nb && y < x + na;
-}
 
 f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int32_t *q_len,
                            const int32_t *k_len, int32_t n, int32_t n_heads, int32_t n_kv,
@@ -81,10 +68,10 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
     if (few)
         f.make(fwd, n_kv, f3s::kFewRows, 64, 256, kFewWorkgroups, kFewLaunch);
     else
-        f.make(fwd, n_kv, f3s::kManyRows, 64, 256, kUnits * f3s::many_waves(d));
-    dq.make(fwd, n_kv, f3s::kManyRows, 64, 256, kUnits * f3s::dq_waves(d));
+        f.make(fwd, n_kv, f3s::kManyRows, 64, 256, f3s::kUnits * f3s::many_waves(d));
+    dq.make(fwd, n_kv, f3s::kManyRows, 64, 256, f3s::kUnits * f3s::dq_waves(d));
     dkv.make(keys, n_kv, f3s::kManyRows, 64, 256,
-             kUnits * f3s::dkv_waves(d) / f3s::dkv_halves(d));
+             f3s::kUnits * f3s::dkv_waves(d) / f3s::dkv_halves(d));
     if (!f.fits() || !dq.fits() || !dkv.fits()) return nullptr;
 
     std::unique_ptr<f3s_cross_plan_s, void (*)(f3s_cross_plan_t)> p(new f3s_cross_plan_s,
@@ -96,23 +83,8 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
     p->q_rows = q_ptr[n];
     p->k_rows = k_ptr[n];
     p->few = few;
-    p->n_fwd = (int32_t)f.items.size();
-    p->n_fwd_merge = (int32_t)f.merges.size();
-    p->fwd_merge_rows = f.merge_rows;
-    p->fwd_parts = f.parts;
-    p->n_dq = (int32_t)dq.items.size();
-    p->n_dq_merge = (int32_t)dq.merges.size();
-    p->dq_merge_rows = dq.merge_rows;
-    p->dq_parts = dq.parts;
-    p->n_dkv = (int32_t)dkv.items.size();
-    p->n_dkv_merge = (int32_t)dkv.merges.size();
-    p->dkv_merge_rows = dkv.merge_rows;
-    p->dkv_parts = dkv.parts;
-    const struct {
-        const void *src;
-        size_t bytes;
-        void **dst;
-    } lists[] = {
+    f3s::set_divisions(p.get(), f, dq, dkv);
+    const f3s::PlanList lists[] = {
         {f.items.data(), f.items.size() * sizeof(DenseItem), (void **)&p->fwd},
         {f.merges.data(), f.merges.size() * sizeof(DenseMerge), (void **)&p->fwd_merge},
         {dq.items.data(), dq.items.size() * sizeof(DenseItem), (void **)&p->dq},
@@ -120,49 +92,9 @@ f3s_cross_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const int
         {dkv.items.data(), dkv.items.size() * sizeof(DenseItem), (void **)&p->dkv},
         {dkv.merges.data(), dkv.merges.size() * sizeof(DenseMerge), (void **)&p->dkv_merge},
     };
-    size_t bytes = 0;
-    for (const auto &l : lists) bytes += round256(l.bytes);
-    std::vector<char> host(bytes);
-    hipError_t e = hipGetDevice(&p->device);
-    if (e == hipSuccess && bytes) e = f3s::limited_malloc(&p->store, bytes);
-    if (e == hipSuccess && bytes) {
-        size_t at = 0;
-        for (const auto &l : lists) {
-            if (l.bytes) memcpy(host.data() + at, l.src, l.bytes);
-            *l.dst = (char *)p->store + at;
-            at += round256(l.bytes);
-        }
-        e = hipMemcpy(p->store, host.data(), bytes, hipMemcpyHostToDevice);
-    }
+    const hipError_t e = f3s::store_lists(p.get(), lists, sizeof lists / sizeof *lists);
     *st = f3s::status_of(e);
     return e == hipSuccess ? p.release() : nullptr;
-}
-
-bool on_device(const f3s_cross_plan_s *p, hipStream_t stream)
-{
-    int dev = -1;
-    const hipError_t e = stream ? hipStreamGetDevice(stream, &dev) : hipGetDevice(&dev);
-    return e == hipSuccess && dev == p->device;
-}
-
-// Partial rows of d floats, then their records of `record` floats.
-size_t parts_bytes(int64_t rows, int32_t d, int32_t record)
-{
-    return rows ? round256((size_t)rows * d * 4) + round256((size_t)rows * record * 4) : 0;
-}
-
-// |scale| log2 e.  Scores that are left out are -inf and stay so under a factor
-// that is not 0: a scale of 0 counts as 2^-120, which turns every finite score
-// of an f16 or bf16 product below 2^100 into 0 as well.
-float base2_scale(float scale)
-{
-    const float s = f3s::scale_log2e(scale);
-    return s < 0x1p-120f ? 0x1p-120f : s;
-}
-
-bool workspace_ok(const void *w, size_t have, size_t need)
-{
-    return need == 0 || (w && aligned(w, 256) && have >= need);
 }
 
 }  // namespace
@@ -193,7 +125,7 @@ void f3s_cross_destroy(f3s_cross_plan_t p)
 
 size_t f3s_cross_forward_workspace_bytes(f3s_cross_plan_t p)
 {
-    return p ? parts_bytes(p->fwd_parts, p->d, 2) : 0;
+    return f3s::forward_workspace(p);
 }
 
 f3s_status_t f3s_cross_forward(f3s_cross_plan_t p, const void *Q, const void *K,
@@ -201,60 +133,20 @@ f3s_status_t f3s_cross_forward(f3s_cross_plan_t p, const void *Q, const void *K,
                                float scale, void *workspace, size_t workspace_bytes,
                                hipStream_t stream)
 {
-    if (!p || !isfinite(scale)) return set_status(F3S_ERR_INVALID_VALUE);
-    if (dtype != F3S_DTYPE_F16 && dtype != F3S_DTYPE_BF16)
-        return set_status(F3S_ERR_UNSUPPORTED);
-    if (p->q_rows == 0) return F3S_OK;
-    if (!on_device(p, stream)) return set_status(F3S_ERR_INVALID_VALUE);
-    if (!Q || !O || !lse || (p->k_rows && (!K || !V)) || !aligned(Q, 16) || !aligned(K, 16) ||
-        !aligned(V, 16) || !aligned(O, 16) || !aligned(lse, 4))
-        return set_status(F3S_ERR_INVALID_VALUE);
-    const size_t need = f3s_cross_forward_workspace_bytes(p);
-    if (!workspace_ok(workspace, workspace_bytes, need))
-        return set_status(F3S_ERR_INVALID_VALUE);
-    const size_t qb = (size_t)p->q_rows * p->n_heads * p->d * 2;
-    const size_t kb = (size_t)p->k_rows * p->n_kv * p->d * 2;
-    const size_t lb = (size_t)p->q_rows * p->n_heads * 4;
-    const struct {
-        const void *p;
-        size_t n;
-    } in[] = {{Q, qb}, {K, kb}, {V, kb}};
-    for (const auto &x : in)
-        if (overlaps(O, qb, x.p, x.n) || overlaps(lse, lb, x.p, x.n) ||
-            overlaps(workspace, need, x.p, x.n))
-            return set_status(F3S_ERR_INVALID_VALUE);
-    if (overlaps(O, qb, lse, lb) || overlaps(O, qb, workspace, need) ||
-        overlaps(lse, lb, workspace, need))
-        return set_status(F3S_ERR_INVALID_VALUE);
-    f3s::FewArgs a = {};
-    a.Q = Q;
-    a.K = K;
-    a.V = V;
-    a.O = O;
-    a.lse = lse;
-    a.q = f3s::query_rows(p->n_heads, p->g);
-    a.n_kv = p->n_kv;
-    a.sl2 = base2_scale(scale);
-    a.flip = signbit(scale) ? 0x80008000u : 0u;
-    a.part_o = (float *)workspace;
-    a.part_ml = (float *)((char *)workspace + round256((size_t)p->fwd_parts * p->d * 4));
-    const bool bf16 = dtype == F3S_DTYPE_BF16;
-    auto launch = p->few ? (bf16 ? f3s::launch_cross_few_bf16 : f3s::launch_cross_few_f16)
-                         : (bf16 ? f3s::launch_cross_many_bf16 : f3s::launch_cross_many_f16);
-    hipError_t e = launch(*p, a, stream);
-    if (e == hipSuccess && p->n_fwd_merge) {
-        const f3s::CrossMergeArgs m = {p->fwd_merge, a.part_o, a.part_ml, O, lse, a.q, 0};
-        e = bf16 ? f3s::launch_cross_merge_bf16(*p, m, stream)
-                 : f3s::launch_cross_merge_f16(*p, m, stream);
-    }
-    return set_status(f3s::status_of(e));
+    return f3s::dense_forward(
+        p, Q, K, V, dtype, O, lse, scale, workspace, workspace_bytes, stream,
+        [&](const f3s::FewArgs &a, bool bf16) {
+            if (p->few)
+                return bf16 ? f3s::launch_cross_few_bf16(*p, a, stream)
+                            : f3s::launch_cross_few_f16(*p, a, stream);
+            return bf16 ? f3s::launch_cross_many_bf16(*p, a, stream)
+                        : f3s::launch_cross_many_f16(*p, a, stream);
+        });
 }
 
 size_t f3s_cross_backward_workspace_bytes(f3s_cross_plan_t p)
 {
-    if (!p) return 0;
-    return round256((size_t)p->q_rows * p->n_heads * 8) + parts_bytes(p->dq_parts, p->d, 0) +
-           parts_bytes(p->dkv_parts, 2 * p->d, 0);
+    return f3s::backward_workspace(p);
 }
 
 f3s_status_t f3s_cross_backward(f3s_cross_plan_t p, const void *Q, const void *K,
@@ -263,61 +155,12 @@ f3s_status_t f3s_cross_backward(f3s_cross_plan_t p, const void *Q, const void *K
                                 void *dV, float scale, void *workspace,
                                 size_t workspace_bytes, hipStream_t stream)
 {
-    if (!p || !isfinite(scale)) return set_status(F3S_ERR_INVALID_VALUE);
-    if (dtype != F3S_DTYPE_F16 && dtype != F3S_DTYPE_BF16)
-        return set_status(F3S_ERR_UNSUPPORTED);
-    if (p->q_rows == 0 && p->k_rows == 0) return F3S_OK;
-    if (!on_device(p, stream)) return set_status(F3S_ERR_INVALID_VALUE);
-    const size_t qb = (size_t)p->q_rows * p->n_heads * p->d * 2;
-    const size_t kb = (size_t)p->k_rows * p->n_kv * p->d * 2;
-    const size_t lb = (size_t)p->q_rows * p->n_heads * 4;
-    const size_t need = f3s_cross_backward_workspace_bytes(p);
-    if (!workspace_ok(workspace, workspace_bytes, need))
-        return set_status(F3S_ERR_INVALID_VALUE);
-    struct Span {
-        const void *p;
-        size_t n;
-    };
-    const Span in[] = {{Q, qb}, {K, kb}, {V, kb}, {O, qb}, {dO, qb}, {lse, lb},
-                       {workspace, need}};
-    const Span out[] = {{dQ, qb}, {dK, kb}, {dV, kb}};
-    const Span &stats = in[5], &room = in[6];
-    for (const Span &x : in)
-        if ((x.n && !x.p) || !aligned(x.p, &x == &stats ? 4 : 16) ||
-            (&x != &room && overlaps(room.p, room.n, x.p, x.n)))
-            return set_status(F3S_ERR_INVALID_VALUE);
-    for (const Span &x : out) {
-        if ((x.n && !x.p) || !aligned(x.p, 16)) return set_status(F3S_ERR_INVALID_VALUE);
-        for (const Span &y : in)
-            if (overlaps(x.p, x.n, y.p, y.n)) return set_status(F3S_ERR_INVALID_VALUE);
-        for (const Span &y : out)
-            if (&x != &y && overlaps(x.p, x.n, y.p, y.n))
-                return set_status(F3S_ERR_INVALID_VALUE);
-    }
-    f3s::CrossBwdArgs a = {};
-    a.Q = Q;
-    a.K = K;
-    a.V = V;
-    a.O = O;
-    a.G = dO;
-    a.lse = lse;
-    a.dQ = dQ;
-    a.dK = dK;
-    a.dV = dV;
-    a.q = f3s::query_rows(p->n_heads, p->g);
-    a.n_kv = p->n_kv;
-    a.sl2 = base2_scale(scale);
-    a.scale = scale;
-    a.flip = signbit(scale) ? 0x80008000u : 0u;
-    char *w = (char *)workspace;
-    a.stats = (float2 *)w;
-    w += round256((size_t)p->q_rows * p->n_heads * 8);
-    a.part_dq = (float *)w;
-    w += parts_bytes(p->dq_parts, p->d, 0);
-    a.part_dkv = (float *)w;
-    return set_status(f3s::status_of(dtype == F3S_DTYPE_BF16
-                                         ? f3s::launch_cross_backward_bf16(*p, a, stream)
-                                         : f3s::launch_cross_backward_f16(*p, a, stream)));
+    return f3s::dense_backward(p, Q, K, V, dtype, O, dO, lse, dQ, dK, dV, scale, workspace,
+                               workspace_bytes, stream,
+                               [&](const f3s::CrossBwdArgs &a, bool bf16) {
+                                   return bf16 ? f3s::launch_cross_backward_bf16(*p, a, stream)
+                                               : f3s::launch_cross_backward_f16(*p, a, stream);
+                               });
 }
 
 }  // extern "C"

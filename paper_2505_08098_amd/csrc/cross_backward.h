@@ -49,29 +49,31 @@ constexpr int dq_waves(int d) { return d <= 32 ? 4 : d <= 64 ? 3 : d <= 128 ? 2 
 constexpr int dkv_halves(int d) { return d <= 128 ? 1 : 2; }
 constexpr int dkv_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
 
-template <int D, int kIn>
-__global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwdArgs a,
-                                                                        const DenseItem *items)
+template <int D, int kIn, typename Item>
+__device__ __forceinline__ void dense_dq(const CrossBwdArgs &a, const Item &it,
+                                         const WindowRule &rule)
 {
+    constexpr bool kWindow = std::is_same<Item, WindowItem>::value;
     using T = ManyTile<D, bwd_tile(D)>;
     constexpr int kTile = T::kRows;
     __shared__ __attribute__((aligned(16))) uint8_t s_k0[T::kBytes], s_k1[T::kBytes];
     __shared__ __attribute__((aligned(16))) uint8_t s_v0[T::kBytes], s_v1[T::kBytes];
-    const DenseItem it = items[blockIdx.x];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int mine = 32 * wave + (lane & 31);
     const bool there = mine < it.rows;
     const bool busy = 32 * wave < it.rows;
+    const RowPositions at_p = row_positions(a.q, it, wave, there ? mine : 0);
     const int64_t at = query_row(a.q, it.head, (int64_t)it.row + (there ? mine : 0));
 
     T tk, tv;
     const uint32_t row_bytes = (uint32_t)a.n_kv * (2 * D);
-    const uint64_t base = (uint64_t)it.other * row_bytes + (uint32_t)it.head * (2 * D);
+    const uint64_t base = (uint64_t)key_base(it) * row_bytes + (uint32_t)it.head * (2 * D);
     const uint8_t *const K = reinterpret_cast<const uint8_t *>(a.K) + base;
     const uint8_t *const V = reinterpret_cast<const uint8_t *>(a.V) + base;
     auto fetch = [&](int t, auto buf) {
-        const int first = kTile * t, last = it.others - 1 - first;
+        const KeyRun run = key_run(it, kTile * t);
+        const int first = run.key, last = kWindow ? max(run.left - 1, 0) : run.left - 1;
         const uint64_t at = (uint64_t)first * row_bytes;
         // (behind the range: the last row again)
         auto offset = [&](int row) { return (uint32_t)min(row, last) * row_bytes; };
@@ -105,7 +107,13 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
     auto work = [&](int t, auto buf) {
         if (!busy) return;
         const uint8_t *k = buf.kIndex ? s_k1 : s_k0, *v = buf.kIndex ? s_v1 : s_v0;
-        const int left = it.others - kTile * t;
+        const KeyRun run = key_run(it, kTile * t);
+        const int left = run.left;
+        if (kWindow &&
+            (left <= 0 || window_none(rule, at_p.first, at_p.last, run.key, min(left, kTile))))
+            return;
+        const bool some = left < kTile || (kWindow && !window_all(rule, at_p.first, at_p.last,
+                                                                  run.key, kTile));
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
             if (kTile > 32) __builtin_amdgcn_sched_barrier(0);  // (one block at a time)
@@ -118,10 +126,13 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.sl2, -lse2)) * (dp[e] - delta);
-            if (left < kTile) {
+            if (some) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (32 * b + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3) >= left) s[e] = 0.f;
+                for (int e = 0; e < 16; ++e) {
+                    const int key = 32 * b + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+                    if (key >= left || (kWindow && !window_sees(rule, at_p.mine, run.key + key)))
+                        s[e] = 0.f;
+                }
             }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
@@ -145,6 +156,14 @@ __global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwd
             lds, dq, a.scale, a.dQ,
             [&](int r) { return query_row(a.q, it.head, (int64_t)it.row + 32 * wave + r); }, rows,
             0, lane);
+}
+
+template <int D, int kIn>
+__global__ __launch_bounds__(kManyThreads, dq_waves(D)) void k_cross_dq(CrossBwdArgs a,
+                                                                        const DenseItem *items)
+{
+    const DenseItem it = items[blockIdx.x];
+    dense_dq<D, kIn>(a, it, {});
 }
 
 // d = 64 to 128: the sums of dK and dV leave no room for both K and V beside
@@ -177,10 +196,13 @@ struct DkvBuffer {
 
 // Columns D0 .. D1 - 1 of dK and dV (all of them up to d = 128; wider rows take
 // two workgroups, each with half of the sums in its registers).
-template <int D, int kIn, int D0, int D1>
-__device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem &it,
-                                          DkvBuffer<D> &s0, DkvBuffer<D> &s1, uint8_t *s_v)
+// s_p: positions of the query rows of both buffers (a window's).
+template <int D, int kIn, int D0, int D1, typename Item>
+__device__ __forceinline__ void dense_dkv(const CrossBwdArgs &a, const Item &it,
+                                          const WindowRule &rule, DkvBuffer<D> &s0,
+                                          DkvBuffer<D> &s1, uint8_t *s_v, int32_t *s_p)
 {
+    constexpr bool kWindow = std::is_same<Item, WindowItem>::value;
     using T = DkvTile<D>;
     using TV = ManyTile<D, kManyRows>;
     constexpr bool kVInLds = dkv_v_in_lds(D);
@@ -221,6 +243,9 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
                 kTile * t + (int)threadIdx.x < it.others ? sr.x - kPUpLog2<kIn>
                                                          : INFINITY;  // (P = 0)
             to.delta[threadIdx.x] = sr.y * kPDown;
+            if constexpr (kWindow)
+                s_p[kTile * buf.kIndex + threadIdx.x] =
+                    (int)row_token(a.q, (uint32_t)it.other + kTile * t + threadIdx.x) + it.shift;
         }
     };
     h8 k[D / 16], v[kVInLds ? 1 : D / 16];
@@ -245,6 +270,18 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
         if (!busy) return;
         const auto &from = buf.kIndex ? s1 : s0;
         const uint8_t *q = from.q, *g = from.g;
+        bool some = false;  // some query rows do not see some keys
+        int key = 0;        // the wave's first
+        if constexpr (kWindow) {
+            const int first = it.other + kTile * t;
+            const int last = it.other + min(kTile * (t + 1), it.others) - 1;
+            const int p0 = (int)row_token(a.q, first) + it.shift;
+            const int p1 = (int)row_token(a.q, last) + it.shift;
+            const int key0 = it.row - it.key0 + 32 * wave, n = min(32, it.rows - 32 * wave);
+            if (window_none(rule, p0, p1, key0, n)) return;
+            some = !window_all(rule, p0, p1, key0, n);
+            key = key0;
+        }
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
             if (kTile > 32) __builtin_amdgcn_sched_barrier(0);  // (one block at a time)
@@ -267,6 +304,24 @@ __device__ __forceinline__ void cross_dkv(const CrossBwdArgs &a, const DenseItem
                         __builtin_amdgcn_exp2f(fmaf(x[4 * r + e], a.sl2, -l[e]));
                     p[4 * r + e] = y;
                     x[4 * r + e] = y * fmaf(dp[4 * r + e], kPDown, -w[e]);
+                }
+            }
+            if constexpr (kWindow) {
+                if (some) {
+                    // (d = 64 has no registers left that would hold these until here)
+                    int l = lane;
+                    if constexpr (D == 64) asm volatile("" : "+v"(l));
+                    const int mine = key + (l & 31);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int row = 32 * b + 8 * r + 4 * (l >> 5);
+                        const i4 at_p =
+                            *reinterpret_cast<const i4 *>(&s_p[kTile * buf.kIndex + row]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!window_sees(rule, at_p[e], mine))
+                                p[4 * r + e] = x[4 * r + e] = 0.f;
+                    }
                 }
             }
 #pragma unroll
@@ -309,13 +364,13 @@ __global__ __launch_bounds__(kManyThreads, dkv_waves(D)) void k_cross_dkv(
     uint8_t s_v[dkv_v_in_lds(D) ? ManyTile<D, kManyRows>::kBytes : 16];
     const DenseItem it = items[blockIdx.x / dkv_halves(D)];
     if constexpr (dkv_halves(D) == 1) {
-        cross_dkv<D, kIn, 0, D>(a, it, s0, s1, s_v);
+        dense_dkv<D, kIn, 0, D>(a, it, {}, s0, s1, s_v, nullptr);
     } else {
         constexpr int kHalf = (D / 2 + 31) / 32 * 32;
         if (blockIdx.x & 1)
-            cross_dkv<D, kIn, kHalf, D>(a, it, s0, s1, s_v);
+            dense_dkv<D, kIn, kHalf, D>(a, it, {}, s0, s1, s_v, nullptr);
         else
-            cross_dkv<D, kIn, 0, kHalf>(a, it, s0, s1, s_v);
+            dense_dkv<D, kIn, 0, kHalf>(a, it, {}, s0, s1, s_v, nullptr);
     }
 }
 
@@ -352,15 +407,11 @@ __global__ __launch_bounds__(256) void k_cross_sum(CrossBwdArgs a, const DenseMe
     }
 }
 
+// The partial sums of a plan's dQ and of its dK and dV.
 template <int D, int kIn>
-hipError_t launch_cross_backward_d(const f3s_cross_plan_s &p, const CrossBwdArgs &a,
-                                   hipStream_t s)
+hipError_t launch_cross_sums_d(const f3s_cross_plan_s &p, const CrossBwdArgs &a, hipStream_t s)
 {
     constexpr int kPer = 256 / (D / 4);
-    if (p.n_dq) k_cross_dq<D, kIn><<<p.n_dq, kManyThreads, 0, s>>>(a, p.dq);
-    if (p.n_dkv)
-        k_cross_dkv<D, kIn><<<(unsigned)(p.n_dkv * dkv_halves(D)), kManyThreads, 0, s>>>(
-            a, p.dkv);
     if (p.n_dq_merge) {
         const int blocks = (p.dq_merge_rows + kPer - 1) / kPer;
         k_cross_sum<D, kIn, false><<<(unsigned)(p.n_dq_merge * blocks), 256, 0, s>>>(
@@ -372,6 +423,17 @@ hipError_t launch_cross_backward_d(const f3s_cross_plan_s &p, const CrossBwdArgs
             a, p.dkv_merge, blocks);
     }
     return hipGetLastError();
+}
+
+template <int D, int kIn>
+hipError_t launch_cross_backward_d(const f3s_cross_plan_s &p, const CrossBwdArgs &a,
+                                   hipStream_t s)
+{
+    if (p.n_dq) k_cross_dq<D, kIn><<<p.n_dq, kManyThreads, 0, s>>>(a, p.dq);
+    if (p.n_dkv)
+        k_cross_dkv<D, kIn><<<(unsigned)(p.n_dkv * dkv_halves(D)), kManyThreads, 0, s>>>(
+            a, p.dkv);
+    return launch_cross_sums_d<D, kIn>(p, a, s);
 }
 
 hipError_t launch_cross_backward_f16(const f3s_cross_plan_s &p, const CrossBwdArgs &a,

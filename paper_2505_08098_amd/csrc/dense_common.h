@@ -4,6 +4,7 @@
 
 #include "f3s_cache.h"
 #include "f3s_cross.h"
+#include "f3s_window.h"
 #include "kernel_common.h"
 
 namespace f3s {
@@ -12,6 +13,7 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef int i2v __attribute__((ext_vector_type(2)));
+typedef int i4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i2v lds_i2;
 
 // Workgroups of 256 threads that one launch takes (fewer than 2^32 threads).
@@ -62,7 +64,7 @@ struct DenseItem {
     int32_t others;   // rows of the other side (0: the results are zeros)
     int32_t part;     // first partial row, -1: the results are final
     int32_t piece;    // which part of a split range
-    int32_t pad;
+    int32_t tag;      // the range's
 };
 static_assert(sizeof(DenseItem) == 32, "DenseItem must be 32 bytes");
 
@@ -78,6 +80,78 @@ struct DenseMerge {
     int32_t pad[2];
 };
 static_assert(sizeof(DenseMerge) == 32, "DenseMerge must be 32 bytes");
+
+// ---- a window of keys --------------------------------------------------------------
+
+// The token at position p sees the key at position j <= p if j is one of the
+// sequence's first `sinks` or of the `window` newest ones that p counts among.
+struct WindowRule {
+    int32_t window, sinks;  // 0 .. 2^30
+};
+__host__ __device__ inline bool window_sees(const WindowRule &w, int32_t p, int32_t j)
+{
+    return j <= p && (p - j < w.window || j < w.sinks);
+}
+// Whether every one of the tokens at first .. last sees every one of the keys key ..
+// key + n - 1 (n >= 1); whether none of them sees any.
+__host__ __device__ inline bool window_all(const WindowRule &w, int32_t first, int32_t last,
+                                           int32_t key, int32_t n)
+{
+    const int32_t near = key > w.sinks ? key : w.sinks;  // the first that is no sink
+    return key + n - 1 <= first && (key + n <= w.sinks || last - near < w.window);
+}
+__host__ __device__ inline bool window_none(const WindowRule &w, int32_t first, int32_t last,
+                                            int32_t key, int32_t n)
+{
+    return key > last || (first - (key + n - 1) >= w.window && key >= w.sinks);
+}
+
+// The keys that some of the tokens at first .. last see, as a list: the `far` sinks
+// ahead of the window (keys 0 .. far - 1), filled up to whole units, then the keys
+// near .. last.  far is 0 where the window reaches the sinks.
+constexpr int32_t kWindowUnit = 64;
+struct WindowKeys {
+    int32_t far, near, end;
+};
+__host__ __device__ inline int32_t window_pad(int32_t far)
+{
+    return (far + kWindowUnit - 1) & ~(kWindowUnit - 1);
+}
+// `step`: what near is a multiple of (a page's tokens come in 16s).
+__host__ __device__ inline WindowKeys window_keys(const WindowRule &w, int32_t first,
+                                                  int32_t last, int32_t step)
+{
+    if (last < 0) return {0, 0, 0};
+    if (first < 0) first = 0;
+    int32_t near = w.window > first ? 0 : (first - w.window + 1) / step * step;
+    if (window_pad(w.sinks) >= near) near = 0;
+    return {near ? w.sinks : 0, near, last + 1};
+}
+__host__ __device__ inline int32_t window_length(const WindowKeys &k)
+{
+    return window_pad(k.far) + k.end - k.near;
+}
+// The key at place v of that list, and how many of the list's keys stand from there on
+// one behind the other (none where v is one of the places that fill a unit up; a key of
+// that number is there all the same).
+struct KeyRun {
+    int32_t key, left;
+};
+__host__ __device__ inline KeyRun window_run(const WindowKeys &k, int32_t v)
+{
+    const int32_t pad = window_pad(k.far);
+    return v < pad ? KeyRun{v, k.far - v} : KeyRun{k.near + (v - pad), k.end - k.near - (v - pad)};
+}
+
+// A DenseItem of a window plan.  Query rows that walk keys: other and others are places
+// of the list `keys`.  Key rows that walk query rows: as in DenseItem.
+struct WindowItem : DenseItem {
+    int32_t key0;     // the sequence's key 0, as a row of K
+    int32_t shift;    // position of a token, less its number (row_token)
+    WindowKeys keys;
+    int32_t fill[3];
+};
+static_assert(sizeof(WindowItem) == 64, "WindowItem must be 64 bytes");
 
 // ---- the cache's rules ---------------------------------------------------------
 
@@ -127,6 +201,12 @@ struct f3s_cross_plan_s {
     int32_t fwd_merge_rows = 0, dq_merge_rows = 0, dkv_merge_rows = 0;  // longest
     int64_t fwd_parts = 0, dq_parts = 0, dkv_parts = 0;                 // partial rows
     bool few = false;                  // every item has few rows
+};
+
+// A plan of f3s_window_plan, with items of its own kind.
+struct f3s_window_plan_s : f3s_cross_plan_s {
+    f3s::WindowRule rule = {};
+    f3s::WindowItem *window_fwd = nullptr, *window_dq = nullptr, *window_dkv = nullptr;
 };
 
 namespace f3s {

@@ -15,6 +15,7 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // each with the rows of the other side that it walks.
 struct Range {
     int64_t row, rows, other, others;
+    int32_t tag = 0;  // the caller's, handed on to its items
 };
 
 // A pass divided among workgroups, one to an item: a tile of rows of one head
@@ -118,8 +119,8 @@ struct Division {
         std::vector<Range> whole, rest;
         for (const Range &r : ranges) {
             const int64_t n = r.rows / tile * tile;
-            if (n) whole.push_back({r.row, n, r.other, r.others});
-            if (n < r.rows) rest.push_back({r.row + n, r.rows - n, r.other, r.others});
+            if (n) whole.push_back({r.row, n, r.other, r.others, r.tag});
+            if (n < r.rows) rest.push_back({r.row + n, r.rows - n, r.other, r.others, r.tag});
         }
         if (!whole.empty() && !rest.empty()) {
             const int64_t small = ceil_div(least, unit);
@@ -156,7 +157,7 @@ struct Division {
                         items.push_back({h, (int32_t)(r.row + at), (int32_t)rows,
                                          (int32_t)(r.other + b), (int32_t)(e - b),
                                          n > 1 ? (int32_t)(part + at * n + k * rows) : -1,
-                                         (int32_t)k, 0});
+                                         (int32_t)k, r.tag});
                     }
                 }
                 if (n == 1) continue;

@@ -25,6 +25,8 @@
 // and 0.0002).  Two 16-bit terms of P would take half as many products again.
 #pragma once
 
+#include <type_traits>
+
 #include "few_rows.h"
 
 namespace f3s {
@@ -304,23 +306,56 @@ __device__ __forceinline__ void store_part32(uint8_t *lds, const f16v (&x)[kCols
     }
 }
 
+// What many_rows, and the dQ pass of cross_backward.h, ask of an item of either kind.
+//
+// The positions of a wave's tokens: the first's, the last's and this lane's (none
+// where all keys are seen).
+struct RowPositions {
+    int32_t first, last, mine;
+};
+__device__ __forceinline__ RowPositions row_positions(const QueryRows &, const DenseItem &, int,
+                                                      int)
+{
+    return {};
+}
+__device__ __forceinline__ RowPositions row_positions(const QueryRows &q, const WindowItem &it,
+                                                      int wave, int mine)
+{
+    const int last = min(32 * wave + 31, it.rows - 1);
+    return {(int)row_token(q, it.row + 32 * wave) + it.shift,
+            (int)row_token(q, it.row + last) + it.shift,
+            (int)row_token(q, it.row + mine) + it.shift};
+}
+// The row of K that key 0 is, and the keys from place t of the walk on.
+__device__ __forceinline__ int32_t key_base(const DenseItem &it) { return it.other; }
+__device__ __forceinline__ int32_t key_base(const WindowItem &it) { return it.key0; }
+__device__ __forceinline__ KeyRun key_run(const DenseItem &it, int t)
+{
+    return {t, it.others - t};
+}
+__device__ __forceinline__ KeyRun key_run(const WindowItem &it, int t)
+{
+    return window_run(it.keys, it.other + t);
+}
+
 // Waves per SIMD that the registers leave room for.
 constexpr int many_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
 
-template <int D, int kIn>
-__global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
-    FewArgs a, const DenseItem *items)
+// Item: DenseItem (rows see all keys of their range) or WindowItem.
+template <int D, int kIn, typename Item>
+__device__ __forceinline__ void many_rows(const FewArgs &a, const Item &it, const WindowRule &rule)
 {
+    constexpr bool kWindow = std::is_same<Item, WindowItem>::value;
     using T = ManyTile<D>;
     constexpr int kKeys = T::kRows, kBlocks = kKeys / 32;
     __shared__ __attribute__((aligned(16))) uint8_t s_k0[T::kBytes], s_k1[T::kBytes];
     __shared__ __attribute__((aligned(16))) uint8_t s_v0[T::kBytes], s_v1[T::kBytes];
-    const DenseItem it = items[blockIdx.x];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int mine = 32 * wave + (lane & 31);  // this lane's query row
     const bool there = mine < it.rows;
     const bool busy = 32 * wave < it.rows;     // (the wave has rows at all)
+    const RowPositions at_p = row_positions(a.q, it, wave, there ? mine : 0);
 
     h8 q[D / 16];
     load_rows32<D>(q, a.Q, query_row(a.q, it.head, (int64_t)it.row + (there ? mine : 0)), there,
@@ -333,13 +368,14 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
 
     T tk, tv;
     const uint32_t row_bytes = (uint32_t)a.n_kv * (2 * D);
-    const uint64_t base = (uint64_t)it.other * row_bytes + (uint32_t)it.head * (2 * D);
+    const uint64_t base = (uint64_t)key_base(it) * row_bytes + (uint32_t)it.head * (2 * D);
     const uint8_t *const K = reinterpret_cast<const uint8_t *>(a.K) + base;
     const uint8_t *const V = reinterpret_cast<const uint8_t *>(a.V) + base;
     auto fetch = [&](int t, auto b) {
         // rows behind the range: its last one again (whatever stands there may
         // not be finite, and 0 times it is added)
-        const int first = kKeys * t, last = it.others - 1 - first;
+        const KeyRun run = key_run(it, kKeys * t);
+        const int first = run.key, last = kWindow ? max(run.left - 1, 0) : run.left - 1;
         const uint64_t at = (uint64_t)first * row_bytes;
         auto offset = [&](int row) { return (uint32_t)min(row, last) * row_bytes; };
         tk.fetch(b.kIndex ? s_k1 : s_k0, K + at, offset);
@@ -351,6 +387,11 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
     };
     auto work = [&](int t, auto b) {
         if (!busy) return;
+        const KeyRun run = key_run(it, kKeys * t);
+        const int left = run.left;
+        if (kWindow &&
+            (left <= 0 || window_none(rule, at_p.first, at_p.last, run.key, min(left, kKeys))))
+            return;
         const uint8_t *k = b.kIndex ? s_k1 : s_k0, *v = b.kIndex ? s_v1 : s_v0;
         f16v s[kBlocks];
 #pragma unroll
@@ -361,12 +402,13 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
             for (int h = 0; h < kBlocks; ++h)
                 s[h] = mfma32<kIn>(T::rows32(k, 32 * h, c, lane), q[c], s[h]);
         }
-        const int left = it.others - kKeys * t;
-        if (left < kKeys) {
+        if (left < kKeys ||
+            (kWindow && !window_all(rule, at_p.first, at_p.last, run.key, kKeys))) {
 #pragma unroll
             for (int e = 0; e < 16 * kBlocks; ++e) {
                 const int key = 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * (lane >> 5) + (e & 3);
-                if (key >= left) s[e >> 4][e & 15] = -INFINITY;
+                if (key >= left || (kWindow && !window_sees(rule, at_p.mine, run.key + key)))
+                    s[e >> 4][e & 15] = -INFINITY;
             }
         }
         float mx = s[0][0];
@@ -375,8 +417,10 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
         mx = rounded_product(max_xor32(mx), a.sl2);
         // (a maximum that has grown by less than 2^6 is not worth the products: the
         // probabilities may as well be 64 times larger, with the same bits)
-        if (__ballot(mx - m_run > kRaise<kIn> + 6.f)) {
-            const float m_new = fmaxf(m_run, lowered<kIn>(mx));
+        const bool grown = mx - m_run > kRaise<kIn> + 6.f;
+        if (__ballot(grown)) {
+            // (a window's rows that see other keys do not change a row's bits)
+            const float m_new = kWindow && !grown ? m_run : fmaxf(m_run, lowered<kIn>(mx));
             const float alpha =
                 __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
             l_run *= alpha;
@@ -388,10 +432,12 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
         const float m_ref = m_run == -INFINITY ? 0.f : m_run;
         float by = a.sl2;
         if (large) {  // (see rounded_product)
+            const bool its = !kWindow || (large >> lane & 1);
 #pragma unroll
             for (int e = 0; e < 16 * kBlocks; ++e)
-                s[e >> 4][e & 15] = rounded_product(s[e >> 4][e & 15], by);
-            by = 1.f;
+                s[e >> 4][e & 15] =
+                    its ? rounded_product(s[e >> 4][e & 15], by) : s[e >> 4][e & 15];
+            by = its ? 1.f : by;
         }
         float sum = 0.f;
 #pragma unroll
@@ -430,6 +476,14 @@ __global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
     store_rows32<D, kIn, D>(lds, o, l == 0.f ? 0.f : kLower / l, a.O, at, it.rows - 32 * wave, 0,
                             lane);
     if (there && col == 0) a.lse[at(lane & 31)] = natural_lse(m_run + kRaise<kIn>, l);
+}
+
+template <int D, int kIn>
+__global__ __launch_bounds__(kManyThreads, many_waves(D)) void k_cross_many(
+    FewArgs a, const DenseItem *items)
+{
+    const DenseItem it = items[blockIdx.x];
+    many_rows<D, kIn>(a, it, {});
 }
 
 template <int D, int kIn>

@@ -1,11 +1,16 @@
-"""Dense attention beside the sparse operator: cross attention over a ragged
-batch, and attention over an 8-bit key/value cache (include/f3s_cross.h,
-include/f3s_cache.h).  Argument marshalling only, like ``binding``: results carry
-no autograd graph, also where an operand requires gradients.
+"""Dense attention beside the sparse operator: cross attention and causal attention
+with a window over a ragged batch, and attention over an 8-bit key/value cache
+(include/f3s_cross.h, include/f3s_window.h, include/f3s_cache.h).  Argument marshalling
+only, like ``binding``: results carry no autograd graph, also where an operand requires
+gradients.
 
     plan = f3s.CrossPlan(q_ptr, k_ptr, heads, kv_heads, d)     # once per batch
     O, lse = f3s.cross_forward(plan, Q, K, V)
     dQ, dK, dV = f3s.cross_backward(plan, Q, K, V, O, dO, lse)
+
+    plan = f3s.WindowPlan(ptr, ptr, heads, kv_heads, d, window=4096, sinks=4)
+    O, lse = f3s.window_forward(plan, Q, K, V)
+    dQ, dK, dV = f3s.window_backward(plan, Q, K, V, O, dO, lse)
 
     cache = f3s.Cache.empty(n_pages, page_size, kv_heads, d)
     f3s.cache_write(cache, K, V, table, lens)                  # the newest tokens
@@ -46,6 +51,14 @@ def _lib():
                 ("f3s_cross_forward", ctypes.c_int,
                  [_vp] * 4 + [_i32, _vp, _vp, ctypes.c_float, _vp, _sz, _vp]),
                 ("f3s_cross_backward", ctypes.c_int,
+                 [_vp] * 4 + [_i32] + [_vp] * 6 + [ctypes.c_float, _vp, _sz, _vp]),
+                ("f3s_window_plan", _vp, [_vp, _vp, _vp, _vp] + [_i32] * 6),
+                ("f3s_window_destroy", None, [_vp]),
+                ("f3s_window_forward_workspace_bytes", _sz, [_vp]),
+                ("f3s_window_backward_workspace_bytes", _sz, [_vp]),
+                ("f3s_window_forward", ctypes.c_int,
+                 [_vp] * 4 + [_i32, _vp, _vp, ctypes.c_float, _vp, _sz, _vp]),
+                ("f3s_window_backward", ctypes.c_int,
                  [_vp] * 4 + [_i32] + [_vp] * 6 + [ctypes.c_float, _vp, _sz, _vp]),
                 ("f3s_cache_write", ctypes.c_int,
                  [cache, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _i32, _vp]),
@@ -135,15 +148,12 @@ def _size(x, name):
 
 # ---- cross attention ----------------------------------------------------------
 
-class CrossPlan:
-    """f3s_cross_plan: the work of a ragged batch.  Sequence b has the rows
-    q_ptr[b] .. q_ptr[b+1] - 1 of Q and k_ptr[b] .. k_ptr[b+1] - 1 of K and V
-    (host sequences of ints, first 0); with q_len / k_len only the first of
-    them, the others being padding.  ``heads`` query heads share ``kv_heads``
-    key heads (default: as many), ``d`` values each."""
+class _RaggedPlan:
+    """The work of a ragged batch, by the library's functions ``_NAME``_*."""
 
-    def __init__(self, q_ptr, k_ptr, heads, kv_heads=None, d=64, q_len=None, k_len=None,
-                 device="cuda"):
+    _NAME = None
+
+    def __init__(self, q_ptr, k_ptr, heads, kv_heads, d, q_len, k_len, device, *more):
         self._h = None
         L = _lib()
         q, k = _host_ints(q_ptr, "q_ptr"), _host_ints(k_ptr, "k_ptr")
@@ -161,11 +171,12 @@ class CrossPlan:
         if device.index is None:
             device = torch.device("cuda", torch.cuda.current_device())
         ptr = lambda a: None if a is None else a.ctypes.data_as(_vp)
+        name = self._NAME + "_plan"
         with _BuildOn(device):
-            h = L.f3s_cross_plan(ptr(q), ptr(k), ptr(lens[0]), ptr(lens[1]), q.size - 1,
-                                 heads, kv_heads, d)
+            h = getattr(L, name)(ptr(q), ptr(k), ptr(lens[0]), ptr(lens[1]), q.size - 1,
+                                 heads, kv_heads, d, *more)
         if not h:
-            raise F3SError(L.f3s_last_error(), "f3s_cross_plan")
+            raise F3SError(L.f3s_last_error(), name)
         self._h = h
         self.device = device
         self.heads, self.kv_heads, self.d = heads, kv_heads, d
@@ -173,8 +184,8 @@ class CrossPlan:
         self.k_shape = (int(k[-1]), self.kv_heads, self.d)
         self.lse_shape = self.q_shape[:2]
         self.scale = 1.0 / math.sqrt(self.d)
-        self._forward_bytes = L.f3s_cross_forward_workspace_bytes(h)
-        self._backward_bytes = L.f3s_cross_backward_workspace_bytes(h)
+        self._forward_bytes = getattr(L, self._NAME + "_forward_workspace_bytes")(h)
+        self._backward_bytes = getattr(L, self._NAME + "_backward_workspace_bytes")(h)
 
     @property
     def handle(self):
@@ -184,7 +195,7 @@ class CrossPlan:
 
     def close(self):
         if self._h is not None:
-            _lib().f3s_cross_destroy(self._h)
+            getattr(_lib(), self._NAME + "_destroy")(self._h)
             self._h = None
 
     def __del__(self):
@@ -200,7 +211,39 @@ class CrossPlan:
         self.close()
 
 
-def _cross_operands(plan, Q, K, V):
+class CrossPlan(_RaggedPlan):
+    """f3s_cross_plan: the work of a ragged batch.  Sequence b has the rows
+    q_ptr[b] .. q_ptr[b+1] - 1 of Q and k_ptr[b] .. k_ptr[b+1] - 1 of K and V
+    (host sequences of ints, first 0); with q_len / k_len only the first of
+    them, the others being padding.  ``heads`` query heads share ``kv_heads``
+    key heads (default: as many), ``d`` values each."""
+
+    _NAME = "f3s_cross"
+
+    def __init__(self, q_ptr, k_ptr, heads, kv_heads=None, d=64, q_len=None, k_len=None,
+                 device="cuda"):
+        super().__init__(q_ptr, k_ptr, heads, kv_heads, d, q_len, k_len, device)
+
+
+class WindowPlan(_RaggedPlan):
+    """f3s_window_plan: the work of causal self-attention over a ragged batch, sizes as
+    CrossPlan's.  The query rows of a sequence are its newest tokens (of nq query and nk
+    key rows, row i stands at position nk - nq + i); a token sees the newest ``window``
+    tokens up to itself (None: all) and the first ``sinks`` ones."""
+
+    _NAME = "f3s_window"
+
+    def __init__(self, q_ptr, k_ptr, heads, kv_heads=None, d=64, window=None, sinks=0,
+                 q_len=None, k_len=None, device="cuda"):
+        window = _MOST if window is None else _size(window, "window")
+        sinks = _size(sinks, "sinks")
+        super().__init__(q_ptr, k_ptr, heads, kv_heads, d, q_len, k_len, device, window, sinks)
+        self.window, self.sinks = window, sinks
+
+
+def _operands(plan, kind, Q, K, V):
+    if not isinstance(plan, kind):  # (the other's handle would lead anywhere)
+        raise TypeError(f"the plan must be a {kind.__name__}")
     dtype = _dtype_of(Q, "Q")
     _check(Q, "Q", dtype, plan.device, plan.q_shape)
     _check(K, "K", dtype, plan.device, plan.k_shape)
@@ -208,13 +251,8 @@ def _cross_operands(plan, Q, K, V):
     return dtype
 
 
-@_on_its_device
-def cross_forward(plan, Q, K, V, scale=None, out=None, lse=None):
-    """f3s_cross_forward: O = softmax(scale Q K^T) V within each sequence of
-    the plan.  Q [rows, heads, d], K and V [rows, kv_heads, d], fp16 or bf16;
-    ``stream=`` (default: torch's current one).  Returns (O, lse): O like Q,
-    lse fp32 [rows, heads]."""
-    dtype = _cross_operands(plan, Q, K, V)
+def _forward(plan, kind, Q, K, V, scale, out, lse):
+    dtype = _operands(plan, kind, Q, K, V)
     device = plan.device
     if out is None:
         out = _empty_like(Q, dtype)
@@ -226,20 +264,18 @@ def cross_forward(plan, Q, K, V, scale=None, out=None, lse=None):
         _check(lse, "lse", torch.float32, device, plan.lse_shape)
     nbytes = plan._forward_bytes
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    rc = _lib().f3s_cross_forward(
+    name = kind._NAME + "_forward"
+    rc = getattr(_lib(), name)(
         plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
         out.data_ptr(), lse.data_ptr(), plan.scale if scale is None else float(scale),
         ws.data_ptr() if nbytes else None, nbytes, _raw_stream(device.index))
     if rc:
-        _fail(rc, "f3s_cross_forward")
+        _fail(rc, name)
     return out, lse
 
 
-@_on_its_device
-def cross_backward(plan, Q, K, V, O, dO, lse, scale=None):
-    """f3s_cross_backward: (dQ, dK, dV), of the operands' shapes and type, for
-    dO = dL/dO and the forward's O and lse; ``stream=`` as cross_forward."""
-    dtype = _cross_operands(plan, Q, K, V)
+def _backward(plan, kind, Q, K, V, O, dO, lse, scale):
+    dtype = _operands(plan, kind, Q, K, V)
     device = plan.device
     _check(O, "O", dtype, device, plan.q_shape)
     _check(dO, "dO", dtype, device, plan.q_shape)
@@ -247,14 +283,45 @@ def cross_backward(plan, Q, K, V, O, dO, lse, scale=None):
     dQ, dK, dV = _empty_like(Q, dtype), _empty_like(K, dtype), _empty_like(V, dtype)
     nbytes = plan._backward_bytes
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    rc = _lib().f3s_cross_backward(
+    name = kind._NAME + "_backward"
+    rc = getattr(_lib(), name)(
         plan.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), _DTYPE_CODE[dtype],
         O.data_ptr(), dO.data_ptr(), lse.data_ptr(), dQ.data_ptr(), dK.data_ptr(),
         dV.data_ptr(), plan.scale if scale is None else float(scale),
         ws.data_ptr() if nbytes else None, nbytes, _raw_stream(device.index))
     if rc:
-        _fail(rc, "f3s_cross_backward")
+        _fail(rc, name)
     return dQ, dK, dV
+
+
+@_on_its_device
+def cross_forward(plan, Q, K, V, scale=None, out=None, lse=None):
+    """f3s_cross_forward: O = softmax(scale Q K^T) V within each sequence of
+    the plan.  Q [rows, heads, d], K and V [rows, kv_heads, d], fp16 or bf16;
+    ``stream=`` (default: torch's current one).  Returns (O, lse): O like Q,
+    lse fp32 [rows, heads]."""
+    return _forward(plan, CrossPlan, Q, K, V, scale, out, lse)
+
+
+@_on_its_device
+def cross_backward(plan, Q, K, V, O, dO, lse, scale=None):
+    """f3s_cross_backward: (dQ, dK, dV), of the operands' shapes and type, for
+    dO = dL/dO and the forward's O and lse; ``stream=`` as cross_forward."""
+    return _backward(plan, CrossPlan, Q, K, V, O, dO, lse, scale)
+
+
+@_on_its_device
+def window_forward(plan, Q, K, V, scale=None, out=None, lse=None):
+    """f3s_window_forward: O = softmax(scale Q K^T) V over the keys that each token of
+    the plan's sequences sees.  Operands, results and ``stream=`` as cross_forward."""
+    return _forward(plan, WindowPlan, Q, K, V, scale, out, lse)
+
+
+@_on_its_device
+def window_backward(plan, Q, K, V, O, dO, lse, scale=None):
+    """f3s_window_backward: (dQ, dK, dV), of the operands' shapes and type, for dO =
+    dL/dO and the forward's O and lse; ``stream=`` as cross_forward."""
+    return _backward(plan, WindowPlan, Q, K, V, O, dO, lse, scale)
 
 
 # ---- the cache -------------------------------------------------------------------
