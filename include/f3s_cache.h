@@ -74,6 +74,28 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
                             int32_t n_seqs, int32_t n_new, hipStream_t stream);
 
 /*
+ * Keep some of the n_new newest tokens of every sequence (those of a draft that were
+ * accepted) and drop the others: the rows of the kept tokens move to the front of the
+ * n_new, in order.
+ *   picks      device int32 [n_seqs, n_picks]: the kept tokens t of 0 .. n_new - 1,
+ *              ascending.  The first entry that is not larger than the one before it, is
+ *              outside 0 .. n_new - 1 or names a padding row (a negative position) ends
+ *              the list (-1, say)
+ *   new_lens   device int32 [n_seqs]: the lengths after this call, max(lens[b] - n_new, 0)
+ *              plus the number of tokens kept
+ * table and lens as above.  A row that has no place (its page is none) is not moved, and
+ * nothing is moved onto one.  The places behind the new length hold what they held or
+ * what was moved away.  Every page of the n_new tokens belongs to one sequence.  The
+ * cache's four parts must not share memory with each other or with the other arguments,
+ * nor new_lens with any of them.  Asynchronous on `stream`; no allocation, no
+ * synchronisation; deterministic.
+ */
+f3s_status_t f3s_cache_keep(const f3s_cache_t *cache, const int32_t *table, int32_t max_pages,
+                            const int32_t *lens, int32_t n_seqs, int32_t n_new,
+                            const int32_t *picks, int32_t n_picks, int32_t *new_lens,
+                            hipStream_t stream);
+
+/*
  * Attention of the n_new newest tokens of every sequence to a prefix that all
  * sequences share and to their own cached keys.  Token t sees the whole
  * prefix and its own positions up to lens[b] - n_new + t (itself, if it was

@@ -6,8 +6,9 @@
 
 and dense attention for decoders (see ``dense``): ``CrossPlan``, ``cross_forward``,
 ``cross_backward`` over an encoder's states; ``WindowPlan``, ``window_forward``,
-``window_backward``: causal, with a sliding window and sinks; ``Cache``, ``cache_write``, ``cache_read``,
-``cache_attend`` over an 8-bit key/value cache.
+``window_backward``: causal, with a sliding window and sinks; ``Cache``,
+``cache_write``, ``cache_read``, ``cache_keep``, ``cache_attend`` over an 8-bit key/value
+cache; ``PagePool``, ``pages_assign``: its pages.
 
 The compute path is the HIP library only (see ``binding``); ``workloads``
 holds the seeded synthetic inputs.
@@ -15,6 +16,6 @@ holds the seeded synthetic inputs.
 from .binding import (F3SError, Plan, PlanInfo, backward, forward,  # noqa: F401
                       forward_typed, load_library, probe_gather, probe_rows, probe_stream,
                       run, run_raw, run_trace, status_string, wall_clock_khz)
-from .dense import (Cache, CrossPlan, WindowPlan, cache_attend, cache_read,  # noqa: F401
-                    cache_write, cross_backward, cross_forward, window_backward,
-                    window_forward)
+from .dense import (Cache, CrossPlan, PagePool, WindowPlan, cache_attend,  # noqa: F401
+                    cache_keep, cache_read, cache_write, cross_backward, cross_forward,
+                    pages_assign, window_backward, window_forward)

@@ -1,7 +1,8 @@
-// Writing rows of keys and values into the paged 8-bit cache, and reading
-// them back (f3s_cache_write, f3s_cache_read; the format is in f3s_cache.h).
+// Writing rows of keys and values into the paged 8-bit cache, reading them back, and
+// moving those of accepted tokens (f3s_cache_write, f3s_cache_read, f3s_cache_keep; the
+// format is in f3s_cache.h).
 //
-// Both are bound by the bytes they move.  The lanes of one row hold 8 of its
+// Writing and reading are bound by the bytes they move.  The lanes of one row hold 8 of its
 // elements each, so that a row's 16-bit side is one 16-byte access per lane
 // and its codes one 8-byte access; the largest magnitude goes over those
 // lanes.  Each group of lanes takes the K and the V row of its token and key
@@ -132,6 +133,86 @@ __global__ __launch_bounds__(kThreads) void k_cache_read(RowArgs a, T *K, T *V)
         }
         *reinterpret_cast<t8 *>(out + to) = x;
     }
+}
+
+struct KeepArgs {
+    f3s_cache_t c;
+    const int32_t *table, *lens, *picks;
+    int32_t *new_lens;
+    int32_t max_pages, page_shift, n_new, n_picks;
+    int32_t blocks;  // workgroups of a sequence
+};
+
+// Kept tokens of a sequence move towards its front, so that the i-th goes to a place at
+// or before its own, and the later ones' own places lie behind it.  A thread has one
+// 16-byte piece of a row (of one key head, of K or V) of every token and moves them in
+// order, kAhead at a time, all loaded before the first is stored: no thread reads what
+// another writes.  The places of a round of picks are looked up once, a thread each.
+constexpr int kKeepAhead = 8;
+
+__global__ __launch_bounds__(kThreads) void k_cache_keep(KeepArgs a)
+{
+    __shared__ int64_t s_from[kThreads], s_to[kThreads];  // in tokens of one head, or -1
+    __shared__ int s_end;
+    const int b = (int)blockIdx.x / a.blocks, part = (int)blockIdx.x - b * a.blocks;
+    const int pieces = a.c.d / 16;
+    const int f = part * kThreads + (int)threadIdx.x;
+    const int head = f / (2 * pieces), side = f / pieces & 1, piece = f % pieces;
+    const bool mine = head < a.c.n_kv_heads;
+    uint8_t *const codes = reinterpret_cast<uint8_t *>(side ? a.c.v : a.c.k) + piece * 16;
+    uint8_t *const powers = side ? a.c.v_exp : a.c.k_exp;
+    const int32_t *const picks = a.picks + (int64_t)b * a.n_picks;
+    const int32_t *const table = a.table + (int64_t)b * a.max_pages;
+    const int64_t first = cache_position(a.lens[b], a.n_new, 0), front = first < 0 ? 0 : first;
+    // row of the cache of a place
+    auto row = [&](int64_t slot) {
+        const int64_t page = slot >> a.page_shift;
+        return ((page * a.c.n_kv_heads + head) << a.page_shift) +
+               (slot & ((1 << a.page_shift) - 1));
+    };
+    int kept = 0;
+    for (int at = 0; at < a.n_picks; at += kThreads) {
+        const int i = at + (int)threadIdx.x;
+        const int pick = i < a.n_picks ? picks[i] : -1;
+        const int before = i < a.n_picks && i ? picks[i - 1] : -1;
+        const bool ok = i < a.n_picks && pick > before && pick < a.n_new && first + pick >= 0;
+        if (threadIdx.x == 0) s_end = kThreads;
+        __syncthreads();
+        if (!ok) atomicMin(&s_end, (int)threadIdx.x);
+        int64_t from = -1, to = -1;
+        if (ok) {
+            from = cache_slot(table, a.max_pages, a.c.n_pages, a.page_shift, first + pick);
+            to = cache_slot(table, a.max_pages, a.c.n_pages, a.page_shift, front + i);
+            if (to == from || to < 0) from = -1;
+        }
+        s_from[threadIdx.x] = from;
+        s_to[threadIdx.x] = to;
+        __syncthreads();
+        const int n = s_end;
+        kept += n;
+        for (int k0 = 0; mine && k0 < n; k0 += kKeepAhead) {
+            u4 x[kKeepAhead];
+            uint8_t e[kKeepAhead];
+#pragma unroll
+            for (int k = 0; k < kKeepAhead; ++k) {
+                const int64_t slot = k0 + k < n ? s_from[k0 + k] : -1;
+                if (slot < 0) continue;
+                const int64_t r = row(slot);
+                x[k] = *reinterpret_cast<const u4 *>(codes + r * a.c.d);
+                if (piece == 0) e[k] = powers[r];
+            }
+#pragma unroll
+            for (int k = 0; k < kKeepAhead; ++k) {
+                if (k0 + k >= n || s_from[k0 + k] < 0) continue;
+                const int64_t r = row(s_to[k0 + k]);
+                *reinterpret_cast<u4 *>(codes + r * a.c.d) = x[k];
+                if (piece == 0) powers[r] = e[k];
+            }
+        }
+        if (n < kThreads) break;
+        __syncthreads();  // (the places and the end are used up)
+    }
+    if (part == 0 && threadIdx.x == 0) a.new_lens[b] = (int32_t)(front + kept);
 }
 
 // The instance of F<D> for one of the feature sizes.
@@ -298,6 +379,45 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
         return f3s::set_status(F3S_ERR_INVALID_VALUE);
     return f3s::set_status(
         f3s::status_of(f3s::with_d<f3s::Read>(cache->d, a, K, V, dtype, stream)));
+}
+
+f3s_status_t f3s_cache_keep(const f3s_cache_t *cache, const int32_t *table, int32_t max_pages,
+                            const int32_t *lens, int32_t n_seqs, int32_t n_new,
+                            const int32_t *picks, int32_t n_picks, int32_t *new_lens,
+                            hipStream_t stream)
+{
+    using f3s::overlap;
+    if (f3s_status_t st = f3s::check_cache(cache)) return f3s::set_status(st);
+    if (n_seqs < 0 || n_new < 0 || n_picks < 0 || max_pages < 0)
+        return f3s::set_status(F3S_ERR_INVALID_VALUE);
+    if (n_seqs == 0) return F3S_OK;
+    if (!lens || !new_lens || (max_pages && !table) || (n_picks && !picks) ||
+        !f3s::aligned(lens, 4) || !f3s::aligned(new_lens, 4) || !f3s::aligned(table, 4) ||
+        !f3s::aligned(picks, 4) || f3s::folded(*cache, false))
+        return f3s::set_status(F3S_ERR_INVALID_VALUE);
+    const int64_t threads = (int64_t)cache->n_kv_heads * (cache->d / 8);
+    const int64_t blocks = (threads + f3s::kThreads - 1) / f3s::kThreads;
+    if ((double)blocks * n_seqs > (double)f3s::kMostGrid || threads > 0x7FFFFFFF - f3s::kThreads)
+        return f3s::set_status(F3S_ERR_TOO_LARGE);
+    const size_t places = (size_t)cache->n_pages * cache->n_kv_heads * cache->page_size;
+    const size_t lb = (size_t)n_seqs * 4;
+    const struct {
+        const void *p;
+        size_t n;
+    } parts[] = {{cache->k, places * cache->d}, {cache->v, places * cache->d},
+                 {cache->k_exp, places}, {cache->v_exp, places}},
+      read[] = {{table, lb * max_pages}, {lens, lb}, {picks, lb * n_picks}};
+    for (const auto &y : read) {
+        if (overlap(new_lens, lb, y.p, y.n)) return f3s::set_status(F3S_ERR_INVALID_VALUE);
+        for (const auto &x : parts)
+            if (overlap(x.p, x.n, y.p, y.n)) return f3s::set_status(F3S_ERR_INVALID_VALUE);
+    }
+    for (const auto &x : parts)
+        if (overlap(x.p, x.n, new_lens, lb)) return f3s::set_status(F3S_ERR_INVALID_VALUE);
+    const f3s::KeepArgs a = {*cache, table, lens, picks, new_lens, max_pages,
+                             __builtin_ctz(cache->page_size), n_new, n_picks, (int32_t)blocks};
+    f3s::k_cache_keep<<<(unsigned)(blocks * n_seqs), f3s::kThreads, 0, stream>>>(a);
+    return f3s::set_status(f3s::status_of(hipGetLastError()));
 }
 
 }  // extern "C"

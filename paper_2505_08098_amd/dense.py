@@ -64,6 +64,12 @@ def _lib():
                  [cache, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _i32, _vp]),
                 ("f3s_cache_read", ctypes.c_int,
                  [cache, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _i32, _vp]),
+                ("f3s_cache_keep", ctypes.c_int,
+                 [cache, _vp, _i32, _vp, _i32, _i32, _vp, _i32, _vp, _vp]),
+                ("f3s_pages_assign_workspace_bytes", _sz, [_i32] * 3),
+                ("f3s_pages_assign", ctypes.c_int,
+                 [_vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _sz,
+                  _vp]),
                 ("f3s_cache_attend", ctypes.c_int,
                  [cache, _vp, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _vp, _i32,
                   ctypes.c_float, _vp, _sz, _vp]),
@@ -427,6 +433,26 @@ def cache_read(cache, table, lens, n, dtype=torch.float16):
 
 
 @_on_its_device
+def cache_keep(cache, table, lens, n, picks):
+    """f3s_cache_keep: of the ``n`` newest rows of every sequence keep those that
+    ``picks`` names (int32 [sequences, picks], ascending numbers of 0 .. n - 1, ended by
+    -1): they move to the front of the n.  Returns the new lengths (int32); ``stream=``
+    as cache_write."""
+    B, pages = _sequences(cache, table, lens)
+    n = _size(n, "n")
+    _check_device_tensor(picks, "picks", torch.int32, cache.device)
+    if picks.dim() != 2 or picks.shape[0] != B or picks.shape[1] > _MOST:
+        raise ValueError("picks must be [sequences, picks]")
+    new = torch.empty_like(lens)
+    rc = _lib().f3s_cache_keep(cache._ref, table.data_ptr(), pages, lens.data_ptr(), B, n,
+                               picks.data_ptr(), picks.shape[1], new.data_ptr(),
+                               _raw_stream(cache.device.index))
+    if rc:
+        _fail(rc, "f3s_cache_keep")
+    return new
+
+
+@_on_its_device
 def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, out=None,
                  lse=None):
     """f3s_cache_attend: the newest tokens of every sequence, Q [sequences, n,
@@ -478,3 +504,61 @@ def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, o
     if rc:
         _fail(rc, "f3s_cache_attend")
     return out, lse
+
+
+# ---- pages -----------------------------------------------------------------------
+
+class PagePool:
+    """The free pages of a cache, a list on the device: the first ``count`` (int32 [1])
+    entries of ``free`` (int32 [pages]).  Caches of several layers that share a table
+    share its pool."""
+
+    def __init__(self, free, count, page_size):
+        _check_device_tensor(free, "free", torch.int32)
+        _check_device_tensor(count, "count", torch.int32, free.device)
+        if free.dim() != 1 or count.numel() != 1 or not 1 <= free.numel() <= _MOST:
+            raise ValueError("free must be [pages], count one number")
+        self.free, self.count = free, count
+        self.device = free.device
+        self.page_size = _size(page_size, "page_size")
+        self._bytes = {}  # workspace of a call, by its sizes
+
+    @classmethod
+    def full(cls, n_pages, page_size, device="cuda"):
+        """All of ``n_pages`` pages, free."""
+        n = _size(n_pages, "n_pages")
+        return cls(torch.arange(n, dtype=torch.int32, device=device),
+                   torch.full((1,), n, dtype=torch.int32, device=device), page_size)
+
+
+@_on_its_device
+def pages_assign(pool, table, lens, new_lens, n=0):
+    """f3s_pages_assign: pages for lengths ``new_lens`` in a ``table`` (int32 [sequences,
+    pages]) that holds those of ``lens`` (int32 [sequences]); pages that are no longer
+    needed go back to the pool.  Table and pool are updated in place.  Returns (got,
+    slots): the lengths that the table then holds (int32; shorter than new_lens where the
+    pool ran out), and where the ``n`` newest tokens lie, page * page_size + place (int64
+    [sequences, n]; -1: nowhere).  ``stream=`` (default: torch's current one)."""
+    B, pages = _sequences(pool, table, lens)
+    _check(new_lens, "new_lens", torch.int32, pool.device, (B,))
+    n = _size(n, "n")
+    if n < 0:
+        raise ValueError("n must not be negative")
+    free, device = pool.free, pool.device
+    sizes = (B, pages, n)
+    nbytes = pool._bytes.get(sizes)
+    if nbytes is None:
+        if len(pool._bytes) >= 64:
+            pool._bytes.clear()
+        nbytes = pool._bytes[sizes] = _lib().f3s_pages_assign_workspace_bytes(*sizes)
+    got = torch.empty_like(lens)
+    slots = torch.empty((B, n), dtype=torch.int64, device=device)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    rc = _lib().f3s_pages_assign(
+        free.data_ptr(), pool.count.data_ptr(), free.numel(), table.data_ptr(), pages,
+        lens.data_ptr(), new_lens.data_ptr(), got.data_ptr(), slots.data_ptr() if n else None,
+        B, n, pool.page_size, ws.data_ptr() if nbytes else None, nbytes,
+        _raw_stream(device.index))
+    if rc:
+        _fail(rc, "f3s_pages_assign")
+    return got, slots
