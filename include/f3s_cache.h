@@ -142,6 +142,52 @@ size_t f3s_cache_attend_workspace_bytes(const f3s_cache_t *cache, int32_t max_pa
                                         int32_t n_seqs, int32_t n_new, int32_t n_heads,
                                         int32_t prefix_len);
 
+/*
+ * The same without a prefix and with a window: a token at position p sees its own
+ * sequence's positions j <= p with p - j < window (itself, if it was written, and the
+ * window - 1 before it) or j < sinks.  A token that sees no key gives O = 0, lse = -inf.
+ *   window, sinks   >= 0; from 2^30 on as 2^30
+ *   workspace       at least f3s_cache_attend_window_workspace_bytes(...) bytes
+ * Up to 64 query rows of a sequence and key head (n_new times n_heads / n_kv_heads) are
+ * worked on 16 at a time, more of them 128 at a time.  In the latter, keys that all 128
+ * rows see have their powers of two applied relative to the largest of their tile (K) or
+ * among the keys before (V), f16: beside what f3s_cache_attend says a key 2^15 times
+ * smaller than that has its score's part off by 2^-25 of the largest.  What a token does
+ * not see changes no bit of its result.
+ */
+f3s_status_t f3s_cache_attend_window(const f3s_cache_t *cache, const void *Q, f3s_dtype_t dtype,
+                                     void *O, float *lse, const int32_t *table,
+                                     int32_t max_pages, const int32_t *lens, int32_t n_seqs,
+                                     int32_t n_new, int32_t n_heads, int32_t window,
+                                     int32_t sinks, float scale, void *workspace,
+                                     size_t workspace_bytes, hipStream_t stream);
+size_t f3s_cache_attend_window_workspace_bytes(const f3s_cache_t *cache, int32_t max_pages,
+                                               int32_t n_seqs, int32_t n_new, int32_t n_heads,
+                                               int32_t window, int32_t sinks);
+
+/*
+ * The same as f3s_cache_attend, but that the n_new newest tokens are a tree (a draft with
+ * several continuations): token t sees the prefix, its sequence's positions before the
+ * n_new, itself and its ancestors, not its siblings or what follows them.
+ *   parents    device int32 [n_seqs, n_new]: the parent of token t, one of 0 .. t - 1;
+ *              any other number (-1, say) for a token without one.  (A sequence with
+ *              fewer drafted tokens than n_new has the last tokens of its text ahead of
+ *              them, each the parent of the next, as far as they reach; tokens without a
+ *              place, ahead of the sequence's start, see the prefix only)
+ *   n_new      at most 256 (else F3S_ERR_UNSUPPORTED)
+ *   workspace  at least f3s_cache_attend_tree_workspace_bytes(...) bytes
+ * Rows are worked on as in f3s_cache_attend_window.
+ */
+f3s_status_t f3s_cache_attend_tree(const f3s_cache_t *cache, const void *Q, f3s_dtype_t dtype,
+                                   void *O, float *lse, const int32_t *table, int32_t max_pages,
+                                   const int32_t *lens, int32_t n_seqs, int32_t n_new,
+                                   int32_t n_heads, const int32_t *parents,
+                                   const int32_t *prefix, int32_t prefix_len, float scale,
+                                   void *workspace, size_t workspace_bytes, hipStream_t stream);
+size_t f3s_cache_attend_tree_workspace_bytes(const f3s_cache_t *cache, int32_t max_pages,
+                                             int32_t n_seqs, int32_t n_new, int32_t n_heads,
+                                             int32_t prefix_len);
+
 #ifdef __cplusplus
 }
 #endif

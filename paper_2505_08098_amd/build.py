@@ -15,7 +15,8 @@ SOURCES = ["f3s_api.hip", "plan_kernels.hip", "fused3s.hip", "fused3s_bf16.hip",
            "fused3s_fp8.hip", "fused3s_ablation.hip", "fused3s_split_row.hip",
            "backward.hip", "backward_bf16.hip", "backward_noalloc.hip", "probe.hip",
            "transpose.hip", "worklist.hip", "radix.hip", "cache.hip", "pages.hip", "attend.hip",
-           "attend_f16.hip", "attend_bf16.hip", "cross.hip", "cross_few_f16.hip",
+           "attend_f16.hip", "attend_bf16.hip", "attend_window_f16.hip", "attend_window_bf16.hip",
+           "attend_tree_f16.hip", "attend_tree_bf16.hip", "cross.hip", "cross_few_f16.hip",
            "cross_few_bf16.hip", "cross_many_f16.hip", "cross_many_bf16.hip",
            "cross_backward_f16.hip", "cross_backward_bf16.hip", "window.hip", "window_f16.hip",
            "window_bf16.hip", "window_backward_f16.hip", "window_backward_bf16.hip"]

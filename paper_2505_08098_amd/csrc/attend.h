@@ -31,6 +31,11 @@ struct AttendArgs {
     int32_t prefix_splits, prefix_chunk;
     int64_t prefix_part;   // first partial row
     int2 *desc;            // per sequence: its first item and their number
+    // what f3s_cache_attend has none of
+    bool own_many;         // the own keys by the kernel of many rows
+    WindowRule rule;
+    int32_t splits;        // a window: pieces of every row block's keys
+    const int32_t *parents;  // a tree: [n_seqs, n_new]
 };
 
 // How the own keys of a batch are divided, from the lengths on the device.
@@ -113,48 +118,66 @@ __device__ __forceinline__ OwnItem own_item(const AttendArgs &a, int i)
     return OwnItem{-1, 0, 0, 0, 0};
 }
 
+// Workgroup wg of the prefix: one of its row blocks, key heads and pieces.
+__device__ __forceinline__ FewItem prefix_item(const AttendArgs &a, int wg)
+{
+    FewItem it = {};
+    const int rb = wg % a.prefix_blocks, sh = wg / a.prefix_blocks;
+    it.head = sh % a.few.n_kv;
+    const int split = sh / a.few.n_kv;
+    const int64_t all = (int64_t)a.rows * a.n_seqs;
+    it.row = (int64_t)rb * kFewRows;
+    it.rows = (int)(all - it.row < kFewRows ? all - it.row : kFewRows);
+    it.table = a.prefix;
+    it.begin = split * a.prefix_chunk;
+    it.end = min(a.prefix_len, it.begin + a.prefix_chunk);
+    it.table_len = ((a.prefix_len - 1) >> a.few.page_shift) + 1;
+    it.causal = false;
+    it.part = a.prefix_part + ((int64_t)split * a.few.n_kv + it.head) * all + it.row;
+    return it;
+}
+
+// Workgroup wg of the own keys; rows = 0 where there is nothing to do.
+__device__ __forceinline__ FewItem own_keys_item(const AttendArgs &a, int wg)
+{
+    FewItem it = {};
+    const int rb = wg % a.row_blocks, ih = wg / a.row_blocks;
+    it.head = ih % a.few.n_kv;
+    const int i = ih / a.few.n_kv;
+    const OwnItem o = own_item(a, i);
+    if (o.seq < 0) return it;
+    const int k = i - o.first;
+    if (k == 0 && it.head == 0 && rb == 0 && threadIdx.x == 0 && !a.direct)
+        a.desc[o.seq] = int2{o.first, o.items};
+    it.row = (int64_t)o.seq * a.rows + rb * kFewRows;
+    it.rows = min(kFewRows, a.rows - rb * kFewRows);
+    it.table = a.table + (int64_t)o.seq * a.max_pages;
+    it.table_len = a.max_pages;
+    it.begin = item_unit(o.units, k, o.items) * kUnit;
+    it.end = min(o.keys, item_unit(o.units, k + 1, o.items) * kUnit);
+    it.causal = a.n_new > 1;
+    it.first = rb * kFewRows;
+    const int64_t base = cache_position(a.lens[o.seq], a.n_new, 0);
+    // (behind the keys that there are, any limit does)
+    it.limit = (int)min(base + 1, (int64_t)o.keys);
+    it.base = (int)base;
+    it.part =
+        a.direct ? -1 : ((int64_t)i * a.few.n_kv + it.head) * a.rows + rb * kFewRows;
+    return it;
+}
+
+// Workgroups of the prefix in the kernel of few rows.
+__device__ __forceinline__ int few_prefix(const AttendArgs &a)
+{
+    return a.prefix_many ? 0 : a.prefix_splits * a.few.n_kv * a.prefix_blocks;
+}
+
 template <int D, int kIn>
 __global__ __launch_bounds__(64 * kFewWaves, few_waves(D, true)) void k_attend(AttendArgs a)
 {
-    FewItem it = {};
-    int wg = (int)blockIdx.x;
-    const int n_prefix = a.prefix_many ? 0 : a.prefix_splits * a.few.n_kv * a.prefix_blocks;
-    if (wg < n_prefix) {
-        const int rb = wg % a.prefix_blocks, sh = wg / a.prefix_blocks;
-        it.head = sh % a.few.n_kv;
-        const int split = sh / a.few.n_kv;
-        const int64_t all = (int64_t)a.rows * a.n_seqs;
-        it.row = (int64_t)rb * kFewRows;
-        it.rows = (int)(all - it.row < kFewRows ? all - it.row : kFewRows);
-        it.table = a.prefix;
-        it.begin = split * a.prefix_chunk;
-        it.end = min(a.prefix_len, it.begin + a.prefix_chunk);
-        it.table_len = ((a.prefix_len - 1) >> a.few.page_shift) + 1;
-        it.causal = false;
-        it.part = a.prefix_part + ((int64_t)split * a.few.n_kv + it.head) * all + it.row;
-    } else {
-        wg -= n_prefix;
-        const int rb = wg % a.row_blocks, ih = wg / a.row_blocks;
-        it.head = ih % a.few.n_kv;
-        const int i = ih / a.few.n_kv;
-        const OwnItem o = own_item(a, i);
-        if (o.seq < 0) return;
-        const int k = i - o.first;
-        if (k == 0 && it.head == 0 && rb == 0 && threadIdx.x == 0 && !a.direct)
-            a.desc[o.seq] = int2{o.first, o.items};
-        it.row = (int64_t)o.seq * a.rows + rb * kFewRows;
-        it.rows = min(kFewRows, a.rows - rb * kFewRows);
-        it.table = a.table + (int64_t)o.seq * a.max_pages;
-        it.table_len = a.max_pages;
-        it.begin = item_unit(o.units, k, o.items) * kUnit;
-        it.end = min(o.keys, item_unit(o.units, k + 1, o.items) * kUnit);
-        it.causal = a.n_new > 1;
-        it.first = rb * kFewRows;
-        // (behind the keys that there are, any limit does)
-        it.limit = (int)min(cache_position(a.lens[o.seq], a.n_new, 0) + 1, (int64_t)o.keys);
-        it.part = a.direct ? -1
-                           : ((int64_t)i * a.few.n_kv + it.head) * a.rows + rb * kFewRows;
-    }
+    const int wg = (int)blockIdx.x, n_prefix = few_prefix(a);
+    const FewItem it = wg < n_prefix ? prefix_item(a, wg) : own_keys_item(a, wg - n_prefix);
+    if (it.rows == 0) return;
     few_rows<D, kIn, true>(a.few, it);
 }
 
@@ -183,6 +206,18 @@ template <int D, int kIn>
 hipError_t launch_attend_prefix_d(const AttendArgs &a, hipStream_t s);
 
 template <int D, int kIn>
+void launch_attend_join_d(const AttendArgs &a, hipStream_t s)
+{
+    if (a.direct) return;
+    constexpr int kPer = 256 / (D / 4);
+    const int64_t rows = (int64_t)a.rows * a.n_seqs * a.few.n_kv;
+    if (rows <= kSplitJoins)
+        k_attend_join<D, kIn, true><<<(unsigned)rows, 256, 0, s>>>(a);
+    else
+        k_attend_join<D, kIn, false><<<(unsigned)((rows + kPer - 1) / kPer), 256, 0, s>>>(a);
+}
+
+template <int D, int kIn>
 hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s)
 {
     int64_t grid = (int64_t)a.own_items * a.few.n_kv * a.row_blocks;
@@ -193,15 +228,7 @@ hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s)
         grid += (int64_t)a.prefix_splits * a.few.n_kv * a.prefix_blocks;
     }
     k_attend<D, kIn><<<(unsigned)grid, 64 * kFewWaves, 0, s>>>(a);
-    if (!a.direct) {
-        constexpr int kPer = 256 / (D / 4);
-        const int64_t rows = (int64_t)a.rows * a.n_seqs * a.few.n_kv;
-        if (rows <= kSplitJoins)
-            k_attend_join<D, kIn, true><<<(unsigned)rows, 256, 0, s>>>(a);
-        else
-            k_attend_join<D, kIn, false>
-                <<<(unsigned)((rows + kPer - 1) / kPer), 256, 0, s>>>(a);
-    }
+    launch_attend_join_d<D, kIn>(a, s);
     return hipGetLastError();
 }
 

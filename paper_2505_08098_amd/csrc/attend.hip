@@ -1,8 +1,11 @@
-// f3s_cache_attend: checks, the division of the work, workspace.
+// f3s_cache_attend, f3s_cache_attend_window, f3s_cache_attend_tree: checks, the division
+// of the work, workspace.
 #include <math.h>
 #include <stdlib.h>
 
-#include "attend_many.h"
+#include <algorithm>
+
+#include "attend_masked.h"
 
 namespace f3s {
 f3s_status_t check_cache(const f3s_cache_t *c);
@@ -54,11 +57,19 @@ struct Layout {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Query rows of a sequence and key head from which the own keys of a masked call take the
+// kernel of many rows.
+constexpr int64_t kFewOwnRows = 64;
+// Workgroups that it aims at.
+int64_t own_workgroups(int32_t d) { return 2 * kUnits * f3s::own_waves(d); }
+
 // Everything of the arguments that follows from the sizes; false if a size is
 // beyond what the kernels count with.
-// prefix_rows: 16 or 128 query rows to a workgroup of the prefix, 0: by the rule.
+// prefix_rows: 16 or 128 query rows to a workgroup of the prefix, 0: by the rule; own_rows:
+// 16 or 128 to one of the own keys.
 bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_new,
-            int32_t n_heads, int32_t prefix_len, int prefix_rows, AttendArgs *a, Layout *w)
+            int32_t n_heads, int32_t prefix_len, int prefix_rows, AttendArgs *a, Layout *w,
+            int own_rows = f3s::kFewRows)
 {
     // (a key's number and a piece's length add up to less than 2^31)
     if ((double)n_new * n_heads * n_seqs > 0x7FFFFFFF || prefix_len > f3s::kMostTokens ||
@@ -73,10 +84,12 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     a->max_pages = max_pages;
     a->prefix_len = prefix_len;
     a->rows = (int32_t)rows;
-    a->row_blocks = (int32_t)ceil_div(rows, f3s::kFewRows);
+    a->own_many = own_rows == f3s::kManyRows;
+    a->row_blocks = (int32_t)ceil_div(rows, own_rows);
     const int64_t cap_units = ceil_div(cap, f3s::kUnit);
     a->direct = prefix_len == 0 && cap_units <= kDirectUnits;
-    int64_t share = ceil_div(kWorkgroups, (int64_t)c.n_kv_heads * a->row_blocks);
+    const int64_t aim = a->own_many ? own_workgroups(c.d) : kWorkgroups;
+    int64_t share = ceil_div(aim, (int64_t)c.n_kv_heads * a->row_blocks);
     // (no more than the table has places for)
     const int64_t most = ceil_div(cap_units * n_seqs, f3s::kLeastUnits);
     if (share > most) share = most;
@@ -136,6 +149,56 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     return true;
 }
 
+// The same for a window: the pieces of a row block's keys follow from the longest list of
+// keys that one can have, and every sequence has as many.
+bool divide_window(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_new,
+                   int32_t n_heads, const f3s::WindowRule &rule, AttendArgs *a, Layout *w)
+{
+    if ((double)n_new * n_heads * n_seqs > 0x7FFFFFFF ||
+        (double)max_pages * c.page_size > f3s::kMostTokens)
+        return false;
+    const int64_t g = n_heads / c.n_kv_heads, rows = n_new * g;
+    a->n_seqs = n_seqs;
+    a->n_new = n_new;
+    a->max_pages = max_pages;
+    a->rows = (int32_t)rows;
+    a->rule = rule;
+    a->own_many = rows > kFewOwnRows;
+    const int64_t tile = a->own_many ? f3s::kManyRows : f3s::kFewRows;
+    a->row_blocks = (int32_t)ceil_div(rows, tile);
+    const int64_t tokens = std::min<int64_t>(n_new, tile / g + 2);
+    const int64_t longest =
+        std::min<int64_t>((int64_t)max_pages * c.page_size,
+                          (int64_t)f3s::window_pad(rule.sinks) + rule.window + tokens + 15);
+    const int64_t units = ceil_div(longest, f3s::kUnit);
+    const int64_t one = (int64_t)n_seqs * c.n_kv_heads * a->row_blocks;  // workgroups, unsplit
+    int64_t splits = 1;
+    if (units > kDirectUnits) {
+        const int64_t aim = a->own_many ? own_workgroups(c.d) : kWorkgroups;
+        splits = std::max<int64_t>(1, std::min(aim / one, units / f3s::kLeastUnits));
+    }
+    a->splits = (int32_t)splits;
+    a->direct = splits == 1;
+    w->own_rows = a->direct ? 0 : (int64_t)n_seqs * splits * c.n_kv_heads * rows;
+    w->prefix_rows = 0;
+    if ((double)one * (double)splits > (double)f3s::kMostGrid ||
+        rows * n_seqs * c.n_kv_heads / 4 >= f3s::kMostGrid)
+        return false;
+    w->ml = round256((size_t)w->own_rows * c.d * 4);
+    w->desc = w->ml + round256((size_t)w->own_rows * 8);
+    w->bytes = a->direct ? 0 : w->desc + round256((size_t)n_seqs * 8);
+    return true;
+}
+
+// And for a tree.
+bool divide_tree(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_new,
+                 int32_t n_heads, int32_t prefix_len, int prefix_rows, AttendArgs *a, Layout *w)
+{
+    const int64_t rows = (int64_t)n_new * (n_heads / c.n_kv_heads);
+    return divide(c, max_pages, n_seqs, n_new, n_heads, prefix_len, prefix_rows, a, w,
+                  rows > kFewOwnRows ? f3s::kManyRows : f3s::kFewRows);
+}
+
 bool sizes_ok(const f3s_cache_t *c, int32_t max_pages, int32_t n_seqs, int32_t n_new,
               int32_t n_heads, int32_t prefix_len)
 {
@@ -150,6 +213,112 @@ bool overlaps(const void *a, size_t na, const void *b, size_t nb)
 {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
     return na && nb && x < y + nb && y < x + na;
+}
+
+// What a call passes, as the entry points have it.
+struct Call {
+    const f3s_cache_t *cache;
+    const void *Q;
+    f3s_dtype_t dtype;
+    void *O;
+    float *lse;
+    const int32_t *table;
+    int32_t max_pages;
+    const int32_t *lens;
+    int32_t n_seqs, n_new, n_heads;
+    const int32_t *prefix;
+    int32_t prefix_len;
+    const int32_t *parents;  // a tree's, or NULL
+    float scale;
+    void *workspace;
+    size_t workspace_bytes;
+};
+
+// The checks ahead of the division.
+f3s_status_t check_call(const Call &x)
+{
+    if (f3s_status_t st = f3s::check_cache(x.cache)) return st;
+    if (!sizes_ok(x.cache, x.max_pages, x.n_seqs, x.n_new, x.n_heads, x.prefix_len) ||
+        !isfinite(x.scale))
+        return F3S_ERR_INVALID_VALUE;
+    if (x.dtype != F3S_DTYPE_F16 && x.dtype != F3S_DTYPE_BF16) return F3S_ERR_UNSUPPORTED;
+    if (x.n_seqs == 0 || x.n_new == 0) return F3S_OK;
+    if (!x.Q || !x.O || !x.lse || !x.lens || (x.max_pages && !x.table) ||
+        (x.prefix_len && !x.prefix) || !aligned(x.Q, 16) || !aligned(x.O, 16) ||
+        !aligned(x.lse, 4) || !aligned(x.lens, 4) || !aligned(x.table, 4) ||
+        !aligned(x.prefix, 4) || !aligned(x.parents, 4))
+        return F3S_ERR_INVALID_VALUE;
+    return F3S_OK;
+}
+
+// Those behind it, and the arguments that are left.
+f3s_status_t finish_call(const Call &x, const Layout &w, AttendArgs *a)
+{
+    if (w.bytes &&
+        (!x.workspace || !aligned(x.workspace, 256) || x.workspace_bytes < w.bytes))
+        return F3S_ERR_INVALID_VALUE;
+    const f3s_cache_t *cache = x.cache;
+    const int64_t tokens = (int64_t)x.n_seqs * x.n_new;
+    const size_t qb = (size_t)tokens * x.n_heads * cache->d * 2;
+    const size_t lb = (size_t)tokens * x.n_heads * 4;
+    const size_t cb = (size_t)cache->n_pages * cache->n_kv_heads * cache->page_size;
+    const struct {
+        const void *p;
+        size_t n;
+    } in[] = {{x.Q, qb},
+              {cache->k, cb * cache->d},
+              {cache->v, cb * cache->d},
+              {cache->k_exp, cb},
+              {cache->v_exp, cb},
+              {x.table, (size_t)x.n_seqs * x.max_pages * 4},
+              {x.lens, (size_t)x.n_seqs * 4},
+              {x.prefix, ((size_t)x.prefix_len + cache->page_size - 1) / cache->page_size * 4},
+              {x.parents, x.parents ? (size_t)tokens * 4 : 0}};
+    // (partial results over lengths or pages that others still read would lead
+    // anywhere)
+    for (const auto &y : in)
+        if (overlaps(x.O, qb, y.p, y.n) || overlaps(x.lse, lb, y.p, y.n) ||
+            overlaps(x.workspace, w.bytes, y.p, y.n))
+            return F3S_ERR_INVALID_VALUE;
+    if (overlaps(x.O, qb, x.lse, lb) || overlaps(x.O, qb, x.workspace, w.bytes) ||
+        overlaps(x.lse, lb, x.workspace, w.bytes))
+        return F3S_ERR_INVALID_VALUE;
+    a->table = x.table;
+    a->lens = x.lens;
+    a->prefix = x.prefix;
+    a->parents = x.parents;
+    a->few.Q = x.Q;
+    a->few.O = x.O;
+    a->few.lse = x.lse;
+    a->few.q = f3s::query_rows(x.n_heads, x.n_heads / cache->n_kv_heads);
+    a->few.n_kv = cache->n_kv_heads;
+    a->few.sl2 = f3s::scale_log2e(x.scale);
+    a->few.flip = signbit(x.scale) ? 0x80008000u : 0u;
+    a->few.k = (const uint8_t *)cache->k;
+    a->few.v = (const uint8_t *)cache->v;
+    a->few.k_exp = cache->k_exp;
+    a->few.v_exp = cache->v_exp;
+    a->few.n_pages = cache->n_pages;
+    a->few.page_shift = __builtin_ctz(cache->page_size);
+    if (w.bytes) {
+        a->few.part_o = (float *)x.workspace;
+        a->few.part_ml = (float *)((char *)x.workspace + w.ml);
+        a->desc = (int2 *)((char *)x.workspace + w.desc);
+    }
+    return F3S_OK;
+}
+
+// F3S_PREFIX_ROWS, or 0.
+int prefix_rows_wanted()
+{
+    const char *rows = getenv("F3S_PREFIX_ROWS");
+    return rows && *rows ? atoi(rows) : 0;
+}
+
+// A window's numbers (a larger one is this one: positions are below 2^31).
+f3s::WindowRule window_rule(int32_t window, int32_t sinks)
+{
+    return {std::min(window, f3s::kMostTokens), std::min(sinks, f3s::kMostTokens)};
 }
 
 }  // namespace
@@ -183,71 +352,104 @@ f3s_status_t f3s_cache_attend(const f3s_cache_t *cache, const void *Q, f3s_dtype
                               hipStream_t stream)
 {
     using f3s::set_status;
-    if (f3s_status_t st = f3s::check_cache(cache)) return set_status(st);
-    if (!sizes_ok(cache, max_pages, n_seqs, n_new, n_heads, prefix_len) || !isfinite(scale))
-        return set_status(F3S_ERR_INVALID_VALUE);
-    if (dtype != F3S_DTYPE_F16 && dtype != F3S_DTYPE_BF16)
-        return set_status(F3S_ERR_UNSUPPORTED);
+    const Call x = {cache, Q, dtype, O, lse, table, max_pages, lens, n_seqs, n_new, n_heads,
+                    prefix, prefix_len, nullptr, scale, workspace, workspace_bytes};
+    if (f3s_status_t st = check_call(x)) return set_status(st);
     if (n_seqs == 0 || n_new == 0) return F3S_OK;
-    if (!Q || !O || !lse || !lens || (max_pages && !table) || (prefix_len && !prefix) ||
-        !aligned(Q, 16) || !aligned(O, 16) || !aligned(lse, 4) || !aligned(lens, 4) ||
-        !aligned(table, 4) || !aligned(prefix, 4))
-        return set_status(F3S_ERR_INVALID_VALUE);
     AttendArgs a = {};
     Layout w;
-    const char *rows = getenv("F3S_PREFIX_ROWS");
-    if (!divide(*cache, max_pages, n_seqs, n_new, n_heads, prefix_len,
-                rows && *rows ? atoi(rows) : 0, &a, &w))
+    if (!divide(*cache, max_pages, n_seqs, n_new, n_heads, prefix_len, prefix_rows_wanted(), &a,
+                &w))
         return set_status(F3S_ERR_TOO_LARGE);
-    if (w.bytes && (!workspace || !aligned(workspace, 256) || workspace_bytes < w.bytes))
-        return set_status(F3S_ERR_INVALID_VALUE);
-    const int64_t tokens = (int64_t)n_seqs * n_new;
-    const size_t qb = (size_t)tokens * n_heads * cache->d * 2, lb = (size_t)tokens * n_heads * 4;
-    const size_t cb = (size_t)cache->n_pages * cache->n_kv_heads * cache->page_size;
-    const struct {
-        const void *p;
-        size_t n;
-    } in[] = {{Q, qb},
-              {cache->k, cb * cache->d},
-              {cache->v, cb * cache->d},
-              {cache->k_exp, cb},
-              {cache->v_exp, cb},
-              {table, (size_t)n_seqs * max_pages * 4},
-              {lens, (size_t)n_seqs * 4},
-              {prefix, ((size_t)prefix_len + cache->page_size - 1) / cache->page_size * 4}};
-    // (partial results over lengths or pages that others still read would lead
-    // anywhere)
-    for (const auto &x : in)
-        if (overlaps(O, qb, x.p, x.n) || overlaps(lse, lb, x.p, x.n) ||
-            overlaps(workspace, w.bytes, x.p, x.n))
-            return set_status(F3S_ERR_INVALID_VALUE);
-    if (overlaps(O, qb, lse, lb) || overlaps(O, qb, workspace, w.bytes) ||
-        overlaps(lse, lb, workspace, w.bytes))
-        return set_status(F3S_ERR_INVALID_VALUE);
-    a.table = table;
-    a.lens = lens;
-    a.prefix = prefix;
-    a.few.Q = Q;
-    a.few.O = O;
-    a.few.lse = lse;
-    a.few.q = f3s::query_rows(n_heads, n_heads / cache->n_kv_heads);
-    a.few.n_kv = cache->n_kv_heads;
-    a.few.sl2 = f3s::scale_log2e(scale);
-    a.few.flip = signbit(scale) ? 0x80008000u : 0u;
-    a.few.k = (const uint8_t *)cache->k;
-    a.few.v = (const uint8_t *)cache->v;
-    a.few.k_exp = cache->k_exp;
-    a.few.v_exp = cache->v_exp;
-    a.few.n_pages = cache->n_pages;
-    a.few.page_shift = __builtin_ctz(cache->page_size);
-    if (w.bytes) {
-        a.few.part_o = (float *)workspace;
-        a.few.part_ml = (float *)((char *)workspace + w.ml);
-        a.desc = (int2 *)((char *)workspace + w.desc);
-    }
+    if (f3s_status_t st = finish_call(x, w, &a)) return set_status(st);
     return set_status(f3s::status_of(dtype == F3S_DTYPE_BF16
                                          ? f3s::launch_attend_bf16(a, cache->d, stream)
                                          : f3s::launch_attend_f16(a, cache->d, stream)));
+}
+
+size_t f3s_cache_attend_window_workspace_bytes(const f3s_cache_t *cache, int32_t max_pages,
+                                               int32_t n_seqs, int32_t n_new, int32_t n_heads,
+                                               int32_t window, int32_t sinks)
+{
+    if (!sizes_ok(cache, max_pages, n_seqs, n_new, n_heads, 0) || n_seqs == 0 || n_new == 0 ||
+        window < 0 || sinks < 0)
+        return 0;
+    AttendArgs a = {};
+    Layout w;
+    return divide_window(*cache, max_pages, n_seqs, n_new, n_heads, window_rule(window, sinks),
+                         &a, &w)
+               ? w.bytes
+               : 0;
+}
+
+f3s_status_t f3s_cache_attend_window(const f3s_cache_t *cache, const void *Q, f3s_dtype_t dtype,
+                                     void *O, float *lse, const int32_t *table,
+                                     int32_t max_pages, const int32_t *lens, int32_t n_seqs,
+                                     int32_t n_new, int32_t n_heads, int32_t window,
+                                     int32_t sinks, float scale, void *workspace,
+                                     size_t workspace_bytes, hipStream_t stream)
+{
+    using f3s::set_status;
+    const Call x = {cache, Q, dtype, O, lse, table, max_pages, lens, n_seqs, n_new, n_heads,
+                    nullptr, 0, nullptr, scale, workspace, workspace_bytes};
+    if (f3s_status_t st = check_call(x)) return set_status(st);
+    if (window < 0 || sinks < 0) return set_status(F3S_ERR_INVALID_VALUE);
+    if (n_seqs == 0 || n_new == 0) return F3S_OK;
+    AttendArgs a = {};
+    Layout w;
+    if (!divide_window(*cache, max_pages, n_seqs, n_new, n_heads, window_rule(window, sinks), &a,
+                       &w))
+        return set_status(F3S_ERR_TOO_LARGE);
+    if (f3s_status_t st = finish_call(x, w, &a)) return set_status(st);
+    return set_status(
+        f3s::status_of(dtype == F3S_DTYPE_BF16
+                           ? f3s::launch_attend_window_bf16(a, cache->d, stream)
+                           : f3s::launch_attend_window_f16(a, cache->d, stream)));
+}
+
+size_t f3s_cache_attend_tree_workspace_bytes(const f3s_cache_t *cache, int32_t max_pages,
+                                             int32_t n_seqs, int32_t n_new, int32_t n_heads,
+                                             int32_t prefix_len)
+{
+    if (!sizes_ok(cache, max_pages, n_seqs, n_new, n_heads, prefix_len) || n_seqs == 0 ||
+        n_new == 0 || n_new > f3s::kTreeTokens)
+        return 0;
+    // (enough for both kernels of the prefix)
+    size_t most = 0;
+    for (int rows : {f3s::kFewRows, f3s::kManyRows}) {
+        AttendArgs a = {};
+        Layout w;
+        if (!divide_tree(*cache, max_pages, n_seqs, n_new, n_heads, prefix_len, rows, &a, &w))
+            return 0;
+        most = std::max(most, w.bytes);
+    }
+    return most;
+}
+
+f3s_status_t f3s_cache_attend_tree(const f3s_cache_t *cache, const void *Q, f3s_dtype_t dtype,
+                                   void *O, float *lse, const int32_t *table, int32_t max_pages,
+                                   const int32_t *lens, int32_t n_seqs, int32_t n_new,
+                                   int32_t n_heads, const int32_t *parents,
+                                   const int32_t *prefix, int32_t prefix_len, float scale,
+                                   void *workspace, size_t workspace_bytes, hipStream_t stream)
+{
+    using f3s::set_status;
+    const Call x = {cache, Q, dtype, O, lse, table, max_pages, lens, n_seqs, n_new, n_heads,
+                    prefix, prefix_len, parents, scale, workspace, workspace_bytes};
+    if (f3s_status_t st = check_call(x)) return set_status(st);
+    if (n_new > f3s::kTreeTokens) return set_status(F3S_ERR_UNSUPPORTED);
+    if (n_seqs == 0 || n_new == 0) return F3S_OK;
+    if (!parents) return set_status(F3S_ERR_INVALID_VALUE);
+    AttendArgs a = {};
+    Layout w;
+    if (!divide_tree(*cache, max_pages, n_seqs, n_new, n_heads, prefix_len, prefix_rows_wanted(),
+                     &a, &w))
+        return set_status(F3S_ERR_TOO_LARGE);
+    if (f3s_status_t st = finish_call(x, w, &a)) return set_status(st);
+    return set_status(
+        f3s::status_of(dtype == F3S_DTYPE_BF16
+                           ? f3s::launch_attend_tree_bf16(a, cache->d, stream)
+                           : f3s::launch_attend_tree_f16(a, cache->d, stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,14 @@
+// Attention over the 8-bit cache with a mask (window), bf16 queries (see attend_masked.h).
+#include "attend_masked.h"
+#include "cross_few.h"
+
+namespace f3s {
+
+hipError_t launch_attend_window_bf16(const AttendArgs &a, int d, hipStream_t s)
+{
+#define F3S_CALL(D) launch_attend_window_d<D, kInBF16>(a, s)
+    F3S_FOR_D(d, F3S_CALL)
+#undef F3S_CALL
+}
+
+}  // namespace f3s

@@ -92,6 +92,17 @@ __host__ __device__ inline bool window_sees(const WindowRule &w, int32_t p, int3
 {
     return j <= p && (p - j < w.window || j < w.sinks);
 }
+// Bits 0 .. n of a word (none for n < 0, all from n = 31 on).
+__host__ __device__ inline uint32_t bits_to(int32_t n)
+{
+    return n < 0 ? 0u : n >= 31 ? ~0u : (2u << n) - 1;
+}
+// The keys key .. key + 31 that it sees, a bit each.
+__host__ __device__ inline uint32_t window_bits(const WindowRule &w, int32_t p, int32_t key)
+{
+    const int32_t upto = p - key;
+    return bits_to(upto) & (~bits_to(upto - w.window) | bits_to(w.sinks - key - 1));
+}
 // Whether every one of the tokens at first .. last sees every one of the keys key ..
 // key + n - 1 (n >= 1); whether none of them sees any.
 __host__ __device__ inline bool window_all(const WindowRule &w, int32_t first, int32_t last,

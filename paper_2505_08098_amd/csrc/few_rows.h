@@ -56,7 +56,61 @@ struct FewItem {
     int32_t first;       // rows of the first token before `row` (row's index in its sequence)
     bool causal;         // each next token sees one key more
     int64_t part;        // first partial row, -1: final
+    // Masks over the cache.  kWindowMask: begin and end are places of the list `keys`,
+    // limit is one more than the first token's position.  kTreeMask: the first token
+    // stands at position `base` (before the start: it is padding), bit j of a row's words
+    // says whether it sees position base + j, and it sees every position before base.
+    WindowKeys keys;
+    int32_t base;
 };
+
+// Which keys of its range a row sees beside the plain limit.
+constexpr int kNoMask = 0, kWindowMask = 1, kTreeMask = 2;
+
+// Tokens of a tree, and the words that hold a bit for each: one of ones ahead of them
+// (positions before the tree), one behind, so that 32 bits from any place are two words.
+constexpr int kTreeTokens = 256;
+constexpr int kTreeWords = kTreeTokens / 32 + 2;
+
+// The words of rows first .. first + kRows - 1 of a tree (row r: token r / g), by the
+// whole workgroup, ahead of a barrier.  A token's parent is one of those before it, any
+// other number none; so a walk up ends after as many steps as the token has tokens before
+// it.
+template <int kRows>
+__device__ __forceinline__ void tree_bits(uint32_t (*bits)[kTreeWords], int32_t *s_parents,
+                                          const int32_t *parents, int n, int first, int g,
+                                          int32_t base)
+{
+    for (int t = threadIdx.x; t < n; t += blockDim.x) s_parents[t] = parents[t];
+    __syncthreads();
+    if ((int)threadIdx.x >= kRows) return;
+    uint32_t *const row = bits[threadIdx.x];
+    const int token = (first + (int)threadIdx.x) / g;
+    const bool there = token < n && (int64_t)base + token >= 0;
+#pragma unroll
+    for (int w = 0; w < kTreeWords; ++w) row[w] = there && w == 0 ? ~0u : 0u;
+    // (a word at a time: ancestors come in falling order)
+    uint32_t word = 0;
+    int at = there ? token : -1, w = at >> 5;
+    while (at >= 0) {
+        if (at >> 5 != w) {
+            row[w + 1] = word;
+            word = 0;
+            w = at >> 5;
+        }
+        word |= 1u << (at & 31);
+        const int up = s_parents[at];
+        at = up >= 0 && up < at ? up : -1;
+    }
+    if (there) row[w + 1] = word;
+}
+// 32 of a row's bits from position `pos` on (pos - base < 256).
+__device__ __forceinline__ uint32_t tree_seen(const uint32_t *row, int32_t pos, int32_t base)
+{
+    const int at = max(pos - base, -32);
+    const uint32_t *w = row + (at >> 5) + 1;
+    return __builtin_amdgcn_alignbit(w[1], w[0], at & 31);
+}
 
 struct FewArgs {
     const void *Q, *K, *V;
@@ -300,9 +354,12 @@ __device__ __forceinline__ void join_row(const float *part_o, const float *part_
 // Rows up to which a workgroup joins one.
 constexpr int64_t kSplitJoins = 2048;
 
-template <int D, int kIn, bool kCache>
-__device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
+template <int D, int kIn, bool kCache, int kMask = kNoMask>
+__device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it,
+                                         const WindowRule &rule = {},
+                                         const uint32_t (*bits)[kTreeWords] = nullptr)
 {
+    static_assert(kCache || kMask == kNoMask, "");
     using T = FewTile<D, kCache>;
     constexpr int kPV = kCache ? kInF16 : kIn;  // type of the value product
     __shared__ __attribute__((aligned(16))) uint8_t s_tile[kFewWaves][T::kWaveBytes];
@@ -330,6 +387,14 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
     const int limit =
         it.causal ? max(it.begin, min(it.end, it.limit + (it.first + i) / a.q.g)) : it.end;
     const int least = it.causal ? max(it.begin, min(it.end, it.limit + it.first / a.q.g)) : it.end;
+    // kWindowMask: positions of the first, the last and this lane's token
+    const int p0 = it.limit - 1 + it.first / a.q.g;
+    const int p1 = it.limit - 1 + (it.first + it.rows - 1) / a.q.g;
+    const int p = it.limit - 1 + (it.first + i) / a.q.g;
+    // the keys at place t of the walk: the first one's position, and how many there are
+    auto run_at = [&](int t) {
+        return kMask == kWindowMask ? window_run(it.keys, t) : KeyRun{t, it.end - t};
+    };
 
     f4 o[D / 16];
 #pragma unroll
@@ -344,11 +409,12 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
     auto load = [&](int t) {
         if constexpr (kCache) {
             int64_t base[2];
+            const KeyRun run = run_at(t);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int pos = t + 16 * h;
+                const int pos = run.key + 16 * h;
                 const int n = pos >> a.page_shift;
-                int page = pos < it.end && n < it.table_len ? it.table[n] : -1;
+                int page = 16 * h < run.left && n < it.table_len ? it.table[n] : -1;
                 page = __builtin_amdgcn_readfirstlane(page);
                 pages[h] = page >= 0 && page < a.n_pages ? page : -1;
                 // (a page that is none reads page 0, whose keys are left out)
@@ -385,8 +451,13 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
     if (t < it.end) load(t);
     for (; t < it.end; t += kStep) {
         const bool ok0 = !kCache || pages[0] >= 0, ok1 = !kCache || pages[1] >= 0;
-        const bool whole = t + kFewKeys <= least && ok0 && ok1;
-        const int keys0 = ok0 ? min(it.end - t, 16) : 0, keys1 = ok1 ? min(it.end - t, 32) : 0;
+        const KeyRun run = run_at(t);
+        const bool all = kMask == kWindowMask
+                             ? run.left >= kFewKeys && window_all(rule, p0, p1, run.key, kFewKeys)
+                         : kMask == kTreeMask ? t + kFewKeys <= min(it.end, it.base)
+                                              : t + kFewKeys <= least;
+        const bool whole = all && ok0 && ok1;
+        const int keys0 = ok0 ? min(run.left, 16) : 0, keys1 = ok1 ? min(run.left, 32) : 0;
         const uint32_t kx[2] = {ke[0], ke[1]};
         uint32_t vx[2] = {ve[0], ve[1]};
         tile_fence<kFewWaves>();
@@ -423,10 +494,14 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it)
                 x[e] = __builtin_ldexpf(x[e], (int)((kx[e >> 2] >> (8 * (e & 3))) & 255) - 127);
         }
         if (!whole) {
+            const uint32_t seen = kMask == kTreeMask ? tree_seen(bits[i], t, it.base) : 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int key = 16 * (e >> 2) + 4 * g + (e & 3);
-                if (t + key >= limit || key >= (e < 4 ? keys0 : keys1)) {
+                const bool hidden = kMask == kWindowMask ? !window_sees(rule, p, run.key + key)
+                                    : kMask == kTreeMask ? !(seen >> key & 1)
+                                                         : t + key >= limit;
+                if (hidden || key >= (e < 4 ? keys0 : keys1)) {
                     x[e] = -INFINITY;
                     // (no power of its own: a row's sums are relative to what it sees)
                     if (kCache) vx[e >> 2] &= ~(255u << (8 * (e & 3)));

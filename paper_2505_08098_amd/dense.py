@@ -73,7 +73,15 @@ def _lib():
                 ("f3s_cache_attend", ctypes.c_int,
                  [cache, _vp, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _vp, _i32,
                   ctypes.c_float, _vp, _sz, _vp]),
-                ("f3s_cache_attend_workspace_bytes", _sz, [cache] + [_i32] * 5)):
+                ("f3s_cache_attend_workspace_bytes", _sz, [cache] + [_i32] * 5),
+                ("f3s_cache_attend_window", ctypes.c_int,
+                 [cache, _vp, _i32, _vp, _vp, _vp, _i32, _vp] + [_i32] * 5 +
+                 [ctypes.c_float, _vp, _sz, _vp]),
+                ("f3s_cache_attend_window_workspace_bytes", _sz, [cache] + [_i32] * 6),
+                ("f3s_cache_attend_tree", ctypes.c_int,
+                 [cache, _vp, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _vp, _vp, _i32,
+                  ctypes.c_float, _vp, _sz, _vp]),
+                ("f3s_cache_attend_tree_workspace_bytes", _sz, [cache] + [_i32] * 5)):
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, args
         _LIB = L
@@ -452,6 +460,59 @@ def cache_keep(cache, table, lens, n, picks):
     return new
 
 
+def _queries(cache, Q, table, lens):
+    """(dtype, sequences, new tokens, heads, pages of a table row), checked."""
+    B, pages = _sequences(cache, table, lens)
+    dtype = _dtype_of(Q, "Q")
+    if Q.dim() != 4 or Q.shape[2] < 1 or Q.shape[2] % cache.kv_heads:
+        raise ValueError("Q must be [sequences, n, heads, d], heads a multiple of kv_heads")
+    _, n, heads, _ = Q.shape
+    _check(Q, "Q", dtype, cache.device, (B, n, heads, cache.d))
+    return dtype, B, n, heads, pages
+
+
+def _prefix(cache, prefix, prefix_len):
+    """The prefix's length, checked."""
+    if prefix is None:
+        if prefix_len != 0:
+            raise ValueError("prefix and a positive prefix_len come together")
+        return prefix_len
+    prefix_len = _size(prefix_len, "prefix_len")
+    _check_device_tensor(prefix, "prefix", torch.int32, cache.device)
+    if prefix_len < 1:
+        raise ValueError("prefix and a positive prefix_len come together")
+    if prefix.dim() != 1 or prefix.numel() * cache.page_size < prefix_len:
+        raise ValueError("prefix must name enough pages for prefix_len tokens")
+    return prefix_len
+
+
+def _results(cache, Q, dtype, out, lse):
+    B, n, heads, _ = Q.shape
+    if out is None:
+        out = _empty_like(Q, dtype)
+    else:
+        _check(out, "out", dtype, cache.device, Q.shape)
+    if lse is None:
+        lse = torch.empty((B, n, heads), dtype=torch.float32, device=cache.device)
+    else:
+        _check(lse, "lse", torch.float32, cache.device, (B, n, heads))
+    return out, lse
+
+
+def _attend_workspace(cache, name, sizes):
+    """A call's workspace and its bytes (None and 0 where it needs none)."""
+    nbytes = cache._bytes.get((name, sizes))
+    if nbytes is None:
+        if max(sizes) > _MOST:
+            raise ValueError("more than 2^31 - 1 tokens or heads")
+        if len(cache._bytes) >= 64:  # (a prefix that grows)
+            cache._bytes.clear()
+        nbytes = getattr(_lib(), name + "_workspace_bytes")(cache._ref, *sizes)
+        cache._bytes[name, sizes] = nbytes
+    return (torch.empty(nbytes, dtype=torch.uint8, device=cache.device) if nbytes else None,
+            nbytes)
+
+
 @_on_its_device
 def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, out=None,
                  lse=None):
@@ -460,49 +521,63 @@ def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, o
     pages ``prefix`` (int32, shared by all sequences) and to their own cached
     keys up to themselves; ``stream=`` as cache_write.  Returns (O, lse): O
     like Q, lse fp32 [sequences, n, heads]."""
-    B, pages = _sequences(cache, table, lens)
-    dtype = _dtype_of(Q, "Q")
-    if Q.dim() != 4 or Q.shape[2] < 1 or Q.shape[2] % cache.kv_heads:
-        raise ValueError("Q must be [sequences, n, heads, d], heads a multiple of kv_heads")
-    _, n, heads, _ = shape = Q.shape
-    device = cache.device
-    _check(Q, "Q", dtype, device, (B, n, heads, cache.d))
-    if prefix is None:
-        if prefix_len != 0:
-            raise ValueError("prefix and a positive prefix_len come together")
-    else:
-        prefix_len = _size(prefix_len, "prefix_len")
-        _check_device_tensor(prefix, "prefix", torch.int32, device)
-        if prefix_len < 1:
-            raise ValueError("prefix and a positive prefix_len come together")
-        if prefix.dim() != 1 or prefix.numel() * cache.page_size < prefix_len:
-            raise ValueError("prefix must name enough pages for prefix_len tokens")
-    sizes = (pages, B, n, heads, prefix_len)
-    nbytes = cache._bytes.get(sizes)
-    if nbytes is None:
-        if max(sizes) > _MOST:
-            raise ValueError("more than 2^31 - 1 tokens or heads")
-        if len(cache._bytes) >= 64:  # (a prefix that grows)
-            cache._bytes.clear()
-        nbytes = _lib().f3s_cache_attend_workspace_bytes(cache._ref, *sizes)
-        cache._bytes[sizes] = nbytes
-    if out is None:
-        out = _empty_like(Q, dtype)
-    else:
-        _check(out, "out", dtype, device, shape)
-    if lse is None:
-        lse = torch.empty((B, n, heads), dtype=torch.float32, device=device)
-    else:
-        _check(lse, "lse", torch.float32, device, (B, n, heads))
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    dtype, B, n, heads, pages = _queries(cache, Q, table, lens)
+    prefix_len = _prefix(cache, prefix, prefix_len)
+    ws, nbytes = _attend_workspace(cache, "f3s_cache_attend", (pages, B, n, heads, prefix_len))
+    out, lse = _results(cache, Q, dtype, out, lse)
     rc = _lib().f3s_cache_attend(
         cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
         table.data_ptr(), pages, lens.data_ptr(), B, n, heads,
         None if prefix is None else prefix.data_ptr(), prefix_len,
         cache.scale if scale is None else float(scale), ws.data_ptr() if nbytes else None,
-        nbytes, _raw_stream(device.index))
+        nbytes, _raw_stream(cache.device.index))
     if rc:
         _fail(rc, "f3s_cache_attend")
+    return out, lse
+
+
+@_on_its_device
+def cache_attend_window(cache, Q, table, lens, window, sinks=0, scale=None, out=None, lse=None):
+    """f3s_cache_attend_window: as cache_attend without a prefix, but that a token sees
+    the newest ``window`` cached tokens up to itself and the first ``sinks`` ones only."""
+    dtype, B, n, heads, pages = _queries(cache, Q, table, lens)
+    window, sinks = _size(window, "window"), _size(sinks, "sinks")
+    if window < 0 or sinks < 0:
+        raise ValueError("window and sinks must not be negative")
+    ws, nbytes = _attend_workspace(cache, "f3s_cache_attend_window",
+                                   (pages, B, n, heads, window, sinks))
+    out, lse = _results(cache, Q, dtype, out, lse)
+    rc = _lib().f3s_cache_attend_window(
+        cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
+        table.data_ptr(), pages, lens.data_ptr(), B, n, heads, window, sinks,
+        cache.scale if scale is None else float(scale), ws.data_ptr() if nbytes else None,
+        nbytes, _raw_stream(cache.device.index))
+    if rc:
+        _fail(rc, "f3s_cache_attend_window")
+    return out, lse
+
+
+@_on_its_device
+def cache_attend_tree(cache, Q, table, lens, parents, prefix=None, prefix_len=0, scale=None,
+                      out=None, lse=None):
+    """f3s_cache_attend_tree: as cache_attend, but that the n newest tokens are a drafted
+    tree: each sees the prefix, its sequence's tokens before the n, its ancestors and
+    itself.  ``parents`` (int32 [sequences, n]): the number of each token's parent, below
+    its own, or -1."""
+    dtype, B, n, heads, pages = _queries(cache, Q, table, lens)
+    _check(parents, "parents", torch.int32, cache.device, (B, n))
+    prefix_len = _prefix(cache, prefix, prefix_len)
+    ws, nbytes = _attend_workspace(cache, "f3s_cache_attend_tree",
+                                   (pages, B, n, heads, prefix_len))
+    out, lse = _results(cache, Q, dtype, out, lse)
+    rc = _lib().f3s_cache_attend_tree(
+        cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
+        table.data_ptr(), pages, lens.data_ptr(), B, n, heads, parents.data_ptr(),
+        None if prefix is None else prefix.data_ptr(), prefix_len,
+        cache.scale if scale is None else float(scale), ws.data_ptr() if nbytes else None,
+        nbytes, _raw_stream(cache.device.index))
+    if rc:
+        _fail(rc, "f3s_cache_attend_tree")
     return out, lse
 
 

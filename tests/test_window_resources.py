@@ -8,7 +8,12 @@ import pytest
 from test_dense_resources import HEADS, THREE
 from test_kernel_resources import _room, kernels  # noqa: F401  (a fixture)
 
+FEW = {d: 4 if d <= 64 else 3 if d <= 160 else 2 for d in HEADS}
 ROOM = {
+    "k_attend_window": FEW,
+    "k_attend_tree": FEW,
+    "k_attend_own1": THREE,      # a window's and a tree's instances
+    "k_attend_own2": THREE,
     "k_window": THREE,
     "k_window_dq": {**THREE, 32: 4},
     "k_window_dkv": THREE,
@@ -19,7 +24,8 @@ ROOM = {
 def test_attention_kernels(kernels, kernel):  # noqa: F811
     seen, wrong = set(), []
     for name, (registers, spilled) in kernels.items():
-        m = re.search(r"\d%sILi(\d+)ELi(\d)EE" % kernel, name)
+        of, mask = (kernel[:-1], "Li%sE" % kernel[-1]) if kernel[-1].isdigit() else (kernel, "")
+        m = re.search(r"\d%sILi(\d+)ELi(\d)E%sE" % (of, mask), name)
         if not m:
             continue
         d, dtype = (int(x) for x in m.groups())
