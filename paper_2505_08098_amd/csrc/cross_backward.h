@@ -14,8 +14,7 @@
 // the operand of the second in place, each wave has 32 rows of its own side in
 // registers, and tiles of 32 rows of the other side (d = 32: 64) pass through LDS
 // for all four waves in two buffers.  As in the forward power is the bound, and in
-// k_cross_dkv LDS reads (one operand of every product, and V; a quarter of their
-// cycles are bank conflicts, many_rows.h): 2 x 4,050 x 4,050, 16 heads of 128 over 4,
+// k_cross_dkv LDS reads (one operand of every product, and V): 2 x 4,050 x 4,050, 16 heads of 128 over 4,
 // bf16, takes 413 us for dQ and 558 for dK and dV, 970 TFLOP/s of the 7 products.
 //
 // P and dS enter the second products in the inputs' type, as P does in the forward,
@@ -98,7 +97,8 @@ __device__ __forceinline__ void dense_dq(const CrossBwdArgs &a, const Item &it,
         delta = sum_xor32(delta);
     }
     load_rows32<D>(q, a.Q, at, there, a.flip, lane);
-    const float lse2 = there ? a.lse[at] * kLog2e : INFINITY;
+    float lse2 = there ? a.lse[at] * kLog2e : INFINITY;
+    if (kWindow && lse2 == -INFINITY) lse2 = INFINITY;  // (it sees nothing: P = 0)
     if (there && lane < 32 && it.piece == 0) a.stats[at] = float2{lse2, delta};
 
     f16v dq[D / 32];
@@ -292,6 +292,23 @@ __device__ __forceinline__ void dense_dkv(const CrossBwdArgs &a, const Item &it,
                 dp = mfma32<kIn>(T::rows32(g, 32 * b, c, lane),
                                  kVInLds ? TV::rows32(s_v, 32 * wave, c, lane) : v[c], dp);
             }
+            if constexpr (kWindow) {
+                if (some) {
+                    // (d = 64 has no register left that would hold it until here)
+                    int l = lane;
+                    if constexpr (D == 64) asm volatile("" : "+v"(l));
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int row = 32 * b + 8 * r + 4 * (l >> 5);
+                        const i4 at_p =
+                            *reinterpret_cast<const i4 *>(&s_p[kTile * buf.kIndex + row]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!window_sees(rule, at_p[e], key + (l & 31)))
+                                x[4 * r + e] = -INFINITY;
+                    }
+                }
+            }
             f16v p;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
@@ -304,24 +321,6 @@ __device__ __forceinline__ void dense_dkv(const CrossBwdArgs &a, const Item &it,
                         __builtin_amdgcn_exp2f(fmaf(x[4 * r + e], a.sl2, -l[e]));
                     p[4 * r + e] = y;
                     x[4 * r + e] = y * fmaf(dp[4 * r + e], kPDown, -w[e]);
-                }
-            }
-            if constexpr (kWindow) {
-                if (some) {
-                    // (d = 64 has no registers left that would hold these until here)
-                    int l = lane;
-                    if constexpr (D == 64) asm volatile("" : "+v"(l));
-                    const int mine = key + (l & 31);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int row = 32 * b + 8 * r + 4 * (l >> 5);
-                        const i4 at_p =
-                            *reinterpret_cast<const i4 *>(&s_p[kTile * buf.kIndex + row]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (!window_sees(rule, at_p[e], mine))
-                                p[4 * r + e] = x[4 * r + e] = 0.f;
-                    }
                 }
             }
 #pragma unroll

@@ -16,9 +16,9 @@
 //
 // 2 x 4,050 tokens, 32 heads of 128 over 8, 8,100 keys, bf16: 1,076 us, 1,000
 // TFLOP/s, where a library's product of 8,192^3 reaches 1,200.  The clock falls to
-// 1.9 GHz, the matrix units are busy 48% of its cycles, the vector unit as long again
-// and LDS 37% (12 of these 37 bank conflicts, below); more waves or earlier reads gained
-// nothing.  Power seems to be the bound; what the conflicts cost is not measured.
+// 1.9 GHz, the matrix units are busy 48% of its cycles and the vector unit as long again;
+// more waves or earlier reads gained nothing, LDS reads without bank conflicts 2%.  Power
+// seems to be the bound.
 //
 // P enters the value product in the inputs' type: rounded to nearest, a bf16 result
 // is off by 0.0023 of its size instead of the 0.0017 of its own rounding (fp16 0.0003
@@ -65,12 +65,13 @@ __device__ __forceinline__ f16v zero16()
 // d a power of two: the loads write LDS themselves (16 bytes a lane), which
 // takes no registers.  A wave's load fills 1 KB in lane order, so rows cannot be
 // padded; instead the 16-byte pieces of a row change places, piece p of row r
-// standing at p ^ swizzle(r).  At d = 128 the lanes of a plain operand read (rows32)
-// then meet different banks, but those of a transposed one (cols32: 4 rows of four
-// neighbouring pieces at a time) meet each bank twice, since a row moves its pieces
-// by two: a third of the forward's LDS cycles and a quarter of the backward's are
-// these conflicts (SQ_LDS_BANK_CONFLICT over SQ_LDS_IDX_ACTIVE: 1.69e7 of 5.04e7,
-// 1.67e7 of 6.65e7 and 3.29e7 of 1.34e8, 2 x 4,050 x 4,050, 16 heads of 128 over 4).
+// standing at p ^ swizzle(r).  The rows that share banks (16 / pieces rows stand in 256
+// bytes) differ in it by the piece's upper bits first, then by its lower ones: so the 16
+// rows of a plain operand read (rows32) meet different banks, and so do the 4 rows of
+// four neighbouring pieces of a transposed one (cols32).  A swizzle that moved
+// neighbouring rows apart by two pieces made the latter meet each bank twice (two
+// sequences of 8,100 tokens, window 1,024, 16 heads of 128 over 4: 792 us a training step instead of 713;
+// 2 x 4,050 tokens over 8,100 keys, 32 heads over 8: 1,080 us instead of 1,060).
 // Other d: through registers, into padded rows.
 template <int D, int R = many_keys(D)>
 struct ManyTile {
@@ -86,9 +87,10 @@ struct ManyTile {
     static __device__ __forceinline__ int swizzle(int row)
     {
         if constexpr (!kDirect) return 0;
-        // (256 bytes are all banks; every block of 32 rows alike)
-        const int r = kPieces >= 16 ? row : (row & 31) / (16 / kPieces);
-        return ((r & 7) << 1 | (r >> 3 & 1)) & (kPieces - 1);
+        // (256 bytes are all banks, which 16 / kPieces rows of short ones share)
+        if constexpr (kPieces >= 16) return (row & 3) << 2 | (row >> 2 & 3);
+        if constexpr (kPieces == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+        return row >> 2 & 3;
     }
 
     u4 r[kDirect ? 1 : kLoads];
