@@ -84,18 +84,11 @@ __device__ __forceinline__ int wave_prefix(int v, int lane)  // inclusive
     return v;
 }
 
-// Item i of the batch's own keys (every wave finds it by itself).
-__device__ __forceinline__ OwnItem own_item(const AttendArgs &a, int i)
+// Item i of the batch's own keys, divided by `per` units to an item.
+__device__ __forceinline__ OwnItem own_item_at(const AttendArgs &a, int i, int per)
 {
     const int lane = threadIdx.x & 63;
     const int64_t cap = (int64_t)a.max_pages << a.few.page_shift;
-    if (a.whole) {
-        const int32_t keys = cache_keys(a.lens[i], cap);
-        return OwnItem{i, i, 1, units_of(keys), keys};
-    }
-    int total = 0;
-    for (int b = lane; b < a.n_seqs; b += 64) total += units_of(cache_keys(a.lens[b], cap));
-    const int per = units_per_item(wave_sum(total), a.share);
     int before = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
         const int b = b0 + lane;
@@ -116,6 +109,20 @@ __device__ __forceinline__ OwnItem own_item(const AttendArgs &a, int i)
         before += __builtin_amdgcn_readlane(upto, 63);
     }
     return OwnItem{-1, 0, 0, 0, 0};
+}
+
+// Item i (every wave finds it by itself).
+__device__ __forceinline__ OwnItem own_item(const AttendArgs &a, int i)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t cap = (int64_t)a.max_pages << a.few.page_shift;
+    if (a.whole) {
+        const int32_t keys = cache_keys(a.lens[i], cap);
+        return OwnItem{i, i, 1, units_of(keys), keys};
+    }
+    int total = 0;
+    for (int b = lane; b < a.n_seqs; b += 64) total += units_of(cache_keys(a.lens[b], cap));
+    return own_item_at(a, i, units_per_item(wave_sum(total), a.share));
 }
 
 // Workgroup wg of the prefix: one of its row blocks, key heads and pieces.

@@ -60,8 +60,12 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Query rows of a sequence and key head from which the own keys of a masked call take the
 // kernel of many rows.
 constexpr int64_t kFewOwnRows = 64;
-// Workgroups that it aims at.
-int64_t own_workgroups(int32_t d) { return 2 * kUnits * f3s::own_waves(d); }
+// What one of its workgroups costs beside its keys, in units of 64 keys, and what a byte of
+// partial results does (2.7 us a unit of 128 values; 5 TB/s).
+constexpr int64_t kOwnCost = 4;
+constexpr double kUnitTime = 2.7e-6, kPartRate = 5e12;
+// Units of a piece of a window, at least, where the workgroups fill the GPU without it.
+constexpr int64_t kWorthUnits = 16;
 
 // Everything of the arguments that follows from the sizes; false if a size is
 // beyond what the kernels count with.
@@ -88,8 +92,7 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     a->row_blocks = (int32_t)ceil_div(rows, own_rows);
     const int64_t cap_units = ceil_div(cap, f3s::kUnit);
     a->direct = prefix_len == 0 && cap_units <= kDirectUnits;
-    const int64_t aim = a->own_many ? own_workgroups(c.d) : kWorkgroups;
-    int64_t share = ceil_div(aim, (int64_t)c.n_kv_heads * a->row_blocks);
+    int64_t share = ceil_div(kWorkgroups, (int64_t)c.n_kv_heads * a->row_blocks);
     // (no more than the table has places for)
     const int64_t most = ceil_div(cap_units * n_seqs, f3s::kLeastUnits);
     if (share > most) share = most;
@@ -97,6 +100,12 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     a->share = (int32_t)share;
     a->whole = a->direct || cap_units <= f3s::kLeastUnits || n_seqs > kMostDivided;
     a->own_items = a->whole ? n_seqs : (int32_t)(share + n_seqs);
+    if (a->own_many && !a->whole) {
+        // one round of workgroups, or half as many again as sequences
+        const int64_t fit =
+            kUnits * f3s::own_waves(c.d) / ((int64_t)c.n_kv_heads * a->row_blocks);
+        a->own_items = (int32_t)std::max<int64_t>(fit, n_seqs + n_seqs / 2);
+    }
     if (prefix_rows)
         a->prefix_many = prefix_rows == f3s::kManyRows;
     else
@@ -173,9 +182,32 @@ bool divide_window(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int3
     const int64_t units = ceil_div(longest, f3s::kUnit);
     const int64_t one = (int64_t)n_seqs * c.n_kv_heads * a->row_blocks;  // workgroups, unsplit
     int64_t splits = 1;
-    if (units > kDirectUnits) {
-        const int64_t aim = a->own_many ? own_workgroups(c.d) : kWorkgroups;
-        splits = std::max<int64_t>(1, std::min(aim / one, units / f3s::kLeastUnits));
+    if (a->own_many) {
+        // whole rounds of workgroups, and what the pieces' results cost
+        const int64_t slots = kUnits * f3s::own_waves(c.d);
+        double best = INFINITY;
+        for (int64_t n = 1; n == 1 || (n <= units / f3s::kLeastUnits && one * n <= 4 * slots); ++n) {
+            const double join = n == 1 ? 0.0
+                                       : 2 + (double)one * n * f3s::kManyRows * (c.d + 2) * 8 /
+                                                 kPartRate / (kUnitTime * c.d / 128);
+            const double t =
+                (double)ceil_div(one * n, slots) * (double)(ceil_div(units, n) + kOwnCost) + join;
+            if (t < best) {
+                best = t;
+                splits = n;
+            }
+        }
+    } else if (units > kDirectUnits) {
+        // As many workgroups as run at once.  One token over windows of 1,024, 4,096 and
+        // 16,384 keys, 8 key heads of 128, us by number of pieces:
+        //    8 sequences, 16 units: 15.7 whole, 13.3 (2), 10.8 (4)
+        //   32 sequences, 16 units: 18.3 whole, 20.2 (2), 23.5 (4)
+        //    8 sequences, 64 units: 51.1 whole, 21.3 (4), 20.3 (12), 22.3 (16)
+        //   64 sequences, 64 units: 104 whole, 117 (2), 107 (3), 113 (4)
+        //   16 sequences, 256 units: 222 whole, 105 (4), 103 (6), 110 (16)
+        const int64_t aim = kUnits * f3s::few_waves(c.d, true);
+        splits = std::min(aim / one, units / (one < kUnits ? (int64_t)f3s::kLeastUnits : kWorthUnits));
+        splits = std::max<int64_t>(splits, 1);
     }
     a->splits = (int32_t)splits;
     a->direct = splits == 1;

@@ -21,6 +21,12 @@ namespace f3s {
 
 constexpr int own_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
 
+// A number that is the same for all lanes, where the compiler might not see it.
+__device__ __forceinline__ int32_t uniform(int32_t x)
+{
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
 // Keys that some row of a block sees, in a window: tokens first .. last of a sequence of
 // `keys` cached ones whose first new token stands at `base`.
 __device__ __forceinline__ WindowKeys own_window(const WindowRule &rule, int32_t base, int first,
@@ -96,10 +102,40 @@ __global__ __launch_bounds__(64 * kFewWaves, few_waves(D, true)) void k_attend_t
     few_rows<D, kIn, true, kTreeMask>(a.few, it, {}, s_bits);
 }
 
-// A number that is the same for all lanes, where the compiler might not see it.
-__device__ __forceinline__ int32_t uniform(int32_t x)
+// Item i where the own keys are divided into at most a.own_items items (at least as many
+// as sequences) of as few units as that allows: a round of the compute units ends when
+// its longest item does.  16 trees of 63 tokens behind 8 to 128 units, 32 heads of 128
+// over 8: 178 us a call where shares happen to fill a round, 190 to 219 where not.
+__device__ __forceinline__ OwnItem fitted_item(const AttendArgs &a, int i)
 {
-    return __builtin_amdgcn_readfirstlane(x);
+    const int lane = threadIdx.x & 63;
+    const int64_t cap = (int64_t)a.max_pages << a.few.page_shift;
+    if (a.whole) return own_item(a, i);
+    // units of this lane's sequence of the first 64, and of any
+    const int mine =
+        lane < a.n_seqs ? units_of(cache_keys(a.lens[lane], cap)) : 0;
+    auto units = [&](int b) {
+        return b < 64 ? mine : units_of(cache_keys(a.lens[b], cap));
+    };
+    int total = 0, longest = 0;
+    for (int b = lane; b < a.n_seqs; b += 64) {
+        total += units(b);
+        longest = max(longest, units(b));
+    }
+    total = uniform(wave_sum(total));
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) longest = max(longest, __shfl_xor(longest, s));
+    int low = units_per_item(total, a.own_items), high = max(uniform(longest), low);
+    while (low < high) {
+        const int per = low + (high - low) / 2;
+        int items = 0;
+        for (int b = lane; b < a.n_seqs; b += 64) items += items_of(units(b), per);
+        if (uniform(wave_sum(items)) <= a.own_items)
+            high = per;
+        else
+            low = per + 1;
+    }
+    return own_item_at(a, i, low);
 }
 
 template <int D, int kIn, int kMask>
@@ -126,7 +162,7 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
     int32_t base;
     WindowKeys list;
     if constexpr (kTree) {
-        const OwnItem o = own_item(a, i);
+        const OwnItem o = fitted_item(a, i);
         if (o.seq < 0) return;
         seq = o.seq;
         base = (int32_t)cache_position(uniform(a.lens[seq]), a.n_new, 0);
