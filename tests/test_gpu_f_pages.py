@@ -76,6 +76,7 @@ def _check(gpu, gen, B, M, page, n, most, n_pages, steps=4):
     (1024, 128, 16, 32, 2048, 60000),                     # the largest by one workgroup
     (1025, 20, 16, 3, 320, 9000), (3, 70000, 16, 1, 1120000, 150000),
     (40, 10, 16, 900, 160, 300), (2500, 3, 128, 1, 384, 5000),
+    (16384, 2, 16, 1, 32, 20000), (20001, 2, 16, 1, 32, 30000),   # the last of three launches
 ])
 def test_against_the_definition(gpu, B, M, page, n, most, n_pages):
     gen = torch.Generator().manual_seed(B + M)

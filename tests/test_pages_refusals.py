@@ -81,7 +81,7 @@ def test_assign_workspace():
     size = dense._lib().f3s_pages_assign_workspace_bytes
     assert size(1024, 128, 32) == 0 and size(1, 1 << 17, 1) == 0
     for more in ((1025, 1, 1), (1024, 129, 1), (1024, 1, 33)):
-        assert size(*more) >= 8 * more[0]
+        assert size(*more) > 4 * more[0]
         assert _assign(B=more[0], pages=more[1], n=more[2], nbytes=size(*more)) == HIP
         assert _assign(B=more[0], pages=more[1], n=more[2], nbytes=size(*more) - 1) == INVALID
     for bad in ((0, 5, 5), (-1, 5, 5), (5, -1, 5), (5, 5, -1), (2**31 - 1, 5, 5)):
