@@ -112,7 +112,7 @@ __device__ __forceinline__ void dense_dq(const CrossBwdArgs &a, const Item &it,
         if (kWindow &&
             (left <= 0 || window_none(rule, at_p.first, at_p.last, run.key, min(left, kTile))))
             return;
-        const bool some = left < kTile || (kWindow && !window_all(rule, at_p.first, at_p.last,
+        const bool some = kWindow && (left < kTile || !window_all(rule, at_p.first, at_p.last,
                                                                   run.key, kTile));
 #pragma unroll
         for (int b = 0; b < kTile / 32; ++b) {
@@ -126,13 +126,19 @@ __device__ __forceinline__ void dense_dq(const CrossBwdArgs &a, const Item &it,
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.sl2, -lse2)) * (dp[e] - delta);
-            if (some) {
+            if constexpr (kWindow) {
+                if (some) {
+                    const uint32_t bits =
+                        lane_bits(window_bits(rule, at_p.mine, run.key + 32 * b) &
+                                      bits_to(left - 32 * b - 1),
+                                  lane);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int key = 32 * b + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
-                    if (key >= left || (kWindow && !window_sees(rule, at_p.mine, run.key + key)))
-                        s[e] = 0.f;
+                    for (int e = 0; e < 16; ++e) s[e] = kept_value(s[e], bits, e);
                 }
+            } else if (left < kTile) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (32 * b + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3) >= left) s[e] = 0.f;
             }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
@@ -196,11 +202,10 @@ struct DkvBuffer {
 
 // Columns D0 .. D1 - 1 of dK and dV (all of them up to d = 128; wider rows take
 // two workgroups, each with half of the sums in its registers).
-// s_p: positions of the query rows of both buffers (a window's).
 template <int D, int kIn, int D0, int D1, typename Item>
 __device__ __forceinline__ void dense_dkv(const CrossBwdArgs &a, const Item &it,
                                           const WindowRule &rule, DkvBuffer<D> &s0,
-                                          DkvBuffer<D> &s1, uint8_t *s_v, int32_t *s_p)
+                                          DkvBuffer<D> &s1, uint8_t *s_v)
 {
     constexpr bool kWindow = std::is_same<Item, WindowItem>::value;
     using T = DkvTile<D>;
@@ -243,9 +248,6 @@ __device__ __forceinline__ void dense_dkv(const CrossBwdArgs &a, const Item &it,
                 kTile * t + (int)threadIdx.x < it.others ? sr.x - kPUpLog2<kIn>
                                                          : INFINITY;  // (P = 0)
             to.delta[threadIdx.x] = sr.y * kPDown;
-            if constexpr (kWindow)
-                s_p[kTile * buf.kIndex + threadIdx.x] =
-                    (int)row_token(a.q, (uint32_t)it.other + kTile * t + threadIdx.x) + it.shift;
         }
     };
     h8 k[D / 16], v[kVInLds ? 1 : D / 16];
@@ -294,19 +296,22 @@ __device__ __forceinline__ void dense_dkv(const CrossBwdArgs &a, const Item &it,
             }
             if constexpr (kWindow) {
                 if (some) {
-                    // (d = 64 has no register left that would hold it until here)
+                    // The rows that see a key stand one behind the other: from the first of
+                    // the token at its position on to the last of its window's last token,
+                    // or, for a sink, without end.
                     int l = lane;
-                    if constexpr (D == 64) asm volatile("" : "+v"(l));
+                    // (d = 64 and 128 have no register left that would hold it until here)
+                    if constexpr (D == 64 || D == 128) asm volatile("" : "+v"(l));
+                    const int j = key + (l & 31);
+                    auto row = [&](int64_t r) { return (int)max(min(r, (int64_t)64), (int64_t)0); };
+                    const int64_t from =
+                        (int64_t)(j - it.shift) * a.q.g - (it.other + kTile * t + 32 * b);
+                    const int64_t to =
+                        j < rule.sinks ? 64 : from + (int64_t)rule.window * a.q.g;
+                    const uint32_t bits =
+                        lane_bits(bits_to(row(to) - 1) & ~bits_to(row(from) - 1), l);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int row = 32 * b + 8 * r + 4 * (l >> 5);
-                        const i4 at_p =
-                            *reinterpret_cast<const i4 *>(&s_p[kTile * buf.kIndex + row]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (!window_sees(rule, at_p[e], key + (l & 31)))
-                                x[4 * r + e] = -INFINITY;
-                    }
+                    for (int e = 0; e < 16; ++e) x[e] = kept_score(x[e], bits, e);
                 }
             }
             f16v p;
@@ -363,13 +368,13 @@ __global__ __launch_bounds__(kManyThreads, dkv_waves(D)) void k_cross_dkv(
     uint8_t s_v[dkv_v_in_lds(D) ? ManyTile<D, kManyRows>::kBytes : 16];
     const DenseItem it = items[blockIdx.x / dkv_halves(D)];
     if constexpr (dkv_halves(D) == 1) {
-        dense_dkv<D, kIn, 0, D>(a, it, {}, s0, s1, s_v, nullptr);
+        dense_dkv<D, kIn, 0, D>(a, it, {}, s0, s1, s_v);
     } else {
         constexpr int kHalf = (D / 2 + 31) / 32 * 32;
         if (blockIdx.x & 1)
-            dense_dkv<D, kIn, kHalf, D>(a, it, {}, s0, s1, s_v, nullptr);
+            dense_dkv<D, kIn, kHalf, D>(a, it, {}, s0, s1, s_v);
         else
-            dense_dkv<D, kIn, 0, kHalf>(a, it, {}, s0, s1, s_v, nullptr);
+            dense_dkv<D, kIn, 0, kHalf>(a, it, {}, s0, s1, s_v);
     }
 }
 

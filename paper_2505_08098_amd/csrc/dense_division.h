@@ -61,6 +61,8 @@ struct Division {
     }
     static constexpr double kOver = 2;  // an item's beginning and end, in units
     static constexpr double kJoin = 1;  // a piece's partial results
+    // Adding one more partial result of a row, in units (128 of them: 19 us).
+    static constexpr double kPartSum = 0.07;
     // The launch that joins them, 5 us, where a unit takes 1.1 (f16, d = 64).
     static constexpr double kLaunch = 5;
     static constexpr int64_t kMostPieces = 16;
@@ -93,11 +95,37 @@ struct Division {
         return per;
     }
 
+    // Units of a piece of `rest` that take the least time, from `least` on: rounds of
+    // pieces, and the adding of a row's partial results one behind the other.
+    static int64_t best_rest(const std::vector<Range> &rest, int32_t heads, int64_t unit,
+                             int64_t least, int64_t slots)
+    {
+        int64_t best = least;
+        double takes = 0;
+        for (int64_t s = least; s <= 16 * least; s *= 2) {
+            double n = 0, most = 0;
+            for (const Range &r : rest) {
+                const double k = (double)pieces(ceil_div(r.others, unit), s);
+                n += k * heads;
+                most = k > most ? k : most;
+            }
+            const double t = (double)ceil_div((int64_t)n, slots) * (double)(s + kOver + kJoin) +
+                             kPartSum * most;
+            if (s == least || t < takes) {
+                takes = t;
+                best = s;
+            }
+        }
+        return best;
+    }
+
     // `slots`: workgroups that run at once.  A range is divided evenly into the fewest
     // pieces of at most so many units, those of `least` rows or more: the shortest
-    // piece has half of `least` (of 256: 320 rows are 128 and 192).
+    // piece has half of `least` (of 256: 320 rows are 128 and 192).  fit_rest: what is
+    // left behind whole tiles walks far more than they do (the sinks of a window, that all
+    // later rows see), so that its pieces are longer where that takes less.
     void make(std::vector<Range> ranges, int32_t heads, int64_t tile, int64_t unit,
-              int64_t least, int64_t slots, double launch = kLaunch)
+              int64_t least, int64_t slots, double launch = kLaunch, bool fit_rest = false)
     {
         double tiles = 0;
         for (const Range &r : ranges) tiles += (double)ceil_div(r.rows, tile) * heads;
@@ -123,8 +151,9 @@ struct Division {
             if (n < r.rows) rest.push_back({r.row + n, r.rows - n, r.other, r.others, r.tag});
         }
         if (!whole.empty() && !rest.empty()) {
-            const int64_t small = ceil_div(least, unit);
+            int64_t small = ceil_div(least, unit);
             double t = 0, n = 0;
+            if (fit_rest) small = best_rest(rest, heads, unit, small, slots);
             per = best_pieces(whole, heads, tile, unit, least, slots, launch, &t);
             for (const Range &r : rest)
                 n += (double)pieces(ceil_div(r.others, unit), small) * heads;

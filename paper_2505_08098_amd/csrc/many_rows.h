@@ -340,6 +340,26 @@ __device__ __forceinline__ KeyRun key_run(const WindowItem &it, int t)
     return window_run(it.keys, it.other + t);
 }
 
+// Masks of an accumulator by bits: of 32 rows a lane holds 16, and of its bits it takes
+// those.  Element e stands at bit 8 (e / 4) + e % 4 of what is left: two instructions an
+// element (one bit widened to a word, a select by its bits).
+__device__ __forceinline__ uint32_t lane_bits(uint32_t bits, int lane)
+{
+    return bits >> (4 * (lane >> 5));
+}
+__device__ __forceinline__ uint32_t element_mask(uint32_t bits, int e)
+{
+    return (uint32_t)__builtin_amdgcn_sbfe((int)bits, 8 * (e >> 2) + (e & 3), 1);
+}
+__device__ __forceinline__ float kept_score(float x, uint32_t bits, int e)  // or -inf
+{
+    return masked_score(x, element_mask(bits, e));
+}
+__device__ __forceinline__ float kept_value(float x, uint32_t bits, int e)  // or 0
+{
+    return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & element_mask(bits, e));
+}
+
 // Waves per SIMD that the registers leave room for.
 constexpr int many_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
 
@@ -404,13 +424,23 @@ __device__ __forceinline__ void many_rows(const FewArgs &a, const Item &it, cons
             for (int h = 0; h < kBlocks; ++h)
                 s[h] = mfma32<kIn>(T::rows32(k, 32 * h, c, lane), q[c], s[h]);
         }
-        if (left < kKeys ||
-            (kWindow && !window_all(rule, at_p.first, at_p.last, run.key, kKeys))) {
+        if constexpr (kWindow) {
+            if (left < kKeys || !window_all(rule, at_p.first, at_p.last, run.key, kKeys)) {
+#pragma unroll
+                for (int h = 0; h < kBlocks; ++h) {
+                    const uint32_t bits =
+                        lane_bits(window_bits(rule, at_p.mine, run.key + 32 * h) &
+                                      bits_to(left - 32 * h - 1),
+                                  lane);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[h][e] = kept_score(s[h][e], bits, e);
+                }
+            }
+        } else if (left < kKeys) {
 #pragma unroll
             for (int e = 0; e < 16 * kBlocks; ++e) {
                 const int key = 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * (lane >> 5) + (e & 3);
-                if (key >= left || (kWindow && !window_sees(rule, at_p.mine, run.key + key)))
-                    s[e >> 4][e & 15] = -INFINITY;
+                if (key >= left) s[e >> 4][e & 15] = -INFINITY;
             }
         }
         float mx = s[0][0];

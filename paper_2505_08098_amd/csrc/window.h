@@ -38,16 +38,15 @@ __global__ __launch_bounds__(kManyThreads, dkv_waves(D)) void k_window_dkv(
     __shared__ DkvBuffer<D> s0, s1;
     __shared__ __attribute__((aligned(16)))
     uint8_t s_v[dkv_v_in_lds(D) ? ManyTile<D, kManyRows>::kBytes : 16];
-    __shared__ __attribute__((aligned(16))) int32_t s_p[2 * DkvTile<D>::kRows];
     const WindowItem it = items[blockIdx.x / dkv_halves(D)];
     if constexpr (dkv_halves(D) == 1) {
-        dense_dkv<D, kIn, 0, D>(a, it, rule, s0, s1, s_v, s_p);
+        dense_dkv<D, kIn, 0, D>(a, it, rule, s0, s1, s_v);
     } else {
         constexpr int kHalf = (D / 2 + 31) / 32 * 32;
         if (blockIdx.x & 1)
-            dense_dkv<D, kIn, kHalf, D>(a, it, rule, s0, s1, s_v, s_p);
+            dense_dkv<D, kIn, kHalf, D>(a, it, rule, s0, s1, s_v);
         else
-            dense_dkv<D, kIn, 0, kHalf>(a, it, rule, s0, s1, s_v, s_p);
+            dense_dkv<D, kIn, 0, kHalf>(a, it, rule, s0, s1, s_v);
     }
 }
 

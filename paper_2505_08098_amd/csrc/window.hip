@@ -112,7 +112,8 @@ f3s_window_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const in
     Division f, dq, dkv;
     f.make(queries, n_kv, tile, f3s::kWindowUnit, 256, f3s::kUnits * f3s::many_waves(d));
     dq.make(queries, n_kv, tile, f3s::kWindowUnit, 256, f3s::kUnits * f3s::dq_waves(d));
-    dkv.make(keys, n_kv, tile, 64, 256, f3s::kUnits * f3s::dkv_waves(d) / f3s::dkv_halves(d));
+    dkv.make(keys, n_kv, tile, 64, 256, f3s::kUnits * f3s::dkv_waves(d) / f3s::dkv_halves(d),
+             Division::kLaunch, true);
     if (!f.fits() || !dq.fits() || !dkv.fits()) return nullptr;
 
     std::unique_ptr<f3s_window_plan_s, void (*)(f3s_window_plan_t)> p(new f3s_window_plan_s,
