@@ -68,7 +68,8 @@ __device__ __forceinline__ f16v zero16()
 // standing at p ^ swizzle(r).  The rows that share banks (16 / pieces rows stand in 256
 // bytes) differ in it by the piece's upper bits first, then by its lower ones: so the 16
 // rows of a plain operand read (rows32) meet different banks, and so do the 4 rows of
-// four neighbouring pieces of a transposed one (cols32).  A swizzle that moved
+// four neighbouring pieces of a transposed one (cols32), and so do those that store every
+// other piece of neighbouring rows (attend_many.h).  A swizzle that moved
 // neighbouring rows apart by two pieces made the latter meet each bank twice (two
 // sequences of 8,100 tokens, window 1,024, 16 heads of 128 over 4: 792 us a training step instead of 713;
 // 2 x 4,050 tokens over 8,100 keys, 32 heads over 8: 1,080 us instead of 1,060).
@@ -88,8 +89,8 @@ struct ManyTile {
     {
         if constexpr (!kDirect) return 0;
         // (256 bytes are all banks, which 16 / kPieces rows of short ones share)
-        if constexpr (kPieces >= 16) return (row & 3) << 2 | (row >> 2 & 3);
-        if constexpr (kPieces == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+        if constexpr (kPieces >= 16) return (row & 3) << 2 | ((row >> 2 & 3) ^ (row & 1));
+        if constexpr (kPieces == 8) return (row >> 1 & 1) << 2 | ((row >> 2 & 3) ^ (row >> 1 & 1));
         return row >> 2 & 3;
     }
 
