@@ -243,15 +243,15 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
         const KeyRun run = run_of(t);
 #pragma unroll
         for (int j = 0; j <= kLoads; ++j) {
-            const int row = row_of(j), at = (run.key + row) >> shift;
-            page[j] = row < run.left && at < a.max_pages ? table[at] : -1;
+            // (by all threads, of one that is not there the last one's)
+            page[j] = table[(run.key + min(row_of(j), run.left - 1)) >> shift];
         }
     };
     auto fetch = [&](int t, auto b) {
         if (t >= n) return;
         constexpr int w = kSets > 1 ? decltype(b)::kIndex : 0;
         const KeyRun run = run_of(t);
-        // Row of the cache of a key; of one that is not there any row.
+        // Row of the cache of a key; of one whose page is none any row.
         auto place = [&](int j) -> int64_t {
             const int its = (unsigned)page[j] < (unsigned)a.few.n_pages ? page[j] : 0;
             return (((int64_t)its * a.few.n_kv + head) << shift) +
@@ -264,13 +264,12 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
             kr[w][j] = *reinterpret_cast<const u4 *>(a.few.k + at);
             vr[w][j] = *reinterpret_cast<const u4 *>(a.few.v + at);
         }
-        ok[w] = (unsigned)page[kLoads] < (unsigned)a.few.n_pages;
+        ok[w] = row_of(kLoads) < run.left && (unsigned)page[kLoads] < (unsigned)a.few.n_pages;
         const int64_t r = place(kLoads);
         ke[w] = a.few.k_exp[r];
         ve[w] = a.few.v_exp[r];
     };
     auto put = [&](int t, auto b, auto seen_by_all) {
-        if (t >= n) return;
         constexpr int w = kSets > 1 ? decltype(b)::kIndex : 0;
         constexpr int at = b.kIndex;
         constexpr bool all = decltype(seen_by_all)::value;
@@ -336,10 +335,8 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
         }
         products_done();
     };
-    auto work = [&](int t, auto b, auto seen_by_all) {
-        if (!busy) return;
-        constexpr int at = b.kIndex;
-        const CodeTile<D> &from = at ? s1 : s0;
+    auto scores = [&](auto b) {
+        const CodeTile<D> &from = b.kIndex ? s1 : s0;
 #pragma unroll
         for (int h = 0; h < kBlocks; ++h) s[h] = zero16();
 #pragma unroll
@@ -348,6 +345,11 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
             for (int h = 0; h < kBlocks; ++h)
                 s[h] = mfma32<kIn>(T::rows32(from.k, 32 * h, c, lane), q[c], s[h]);
         }
+    };
+    auto work = [&](int t, auto b, auto seen_by_all) {
+        if (!busy) return;
+        constexpr int at = b.kIndex;
+        const CodeTile<D> &from = at ? s1 : s0;
         if constexpr (decltype(seen_by_all)::value) {
             float by = times[at];
             const uint64_t all = keys[at];
@@ -449,6 +451,7 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
         for (int k = 1; k < kSets + 3; ++k) id[k] = next(id[k - 1], all.value);
         auto step = [&](auto here, auto other) {
             __syncthreads();  // tile id[0] is there, and nobody reads the other buffer
+            scores(here);
             put(id[1], other, all);
             fetch(id[1 + kSets], other);
             look(id[2 + kSets]);
