@@ -164,10 +164,9 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
             *reinterpret_cast<h8 *>(pv + ((2 * c + 1) ^ sw) * 16) = codes_to<kInF16>(vhi, vp);
         }
     };
-    auto work = [&](auto b) {
-        if (!busy) return;
+    f16v s[kBlocks];
+    auto scores = [&](auto b) {
         const CodeTile<D> &from = b.kIndex ? s1 : s0;
-        f16v s[kBlocks];
 #pragma unroll
         for (int h = 0; h < kBlocks; ++h) s[h] = zero16();
 #pragma unroll
@@ -176,6 +175,10 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
             for (int h = 0; h < kBlocks; ++h)
                 s[h] = mfma32<kIn>(T::rows32(from.k, 32 * h, c, lane), q[c], s[h]);
         }
+    };
+    auto work = [&](auto b) {
+        if (!busy) return;
+        const CodeTile<D> &from = b.kIndex ? s1 : s0;
         float by = times[b.kIndex];
         const uint64_t all = keys[b.kIndex];
         if (kBlocks > 1 ? ~all : ~(uint32_t)all) {
@@ -233,10 +236,11 @@ __global__ __launch_bounds__(kManyThreads, prefix_waves(D)) void k_attend_prefix
     const int n = (end - begin + kKeys - 1) / kKeys;
     auto step = [&](int t, auto here, auto next) {
         __syncthreads();  // tile t is there, and nobody reads the other buffer
-        if (t + 1 < n) {
-            put(next);
-            fetch(min(t + 1 + kSets, n - 1), next);
-        }
+        // (the products first, and nothing that ends their block: they go on while the
+        // next tile is widened; behind the last one that is done once more, for nobody)
+        scores(here);
+        put(next);
+        fetch(min(t + 1 + kSets, n - 1), next);
         work(here);
     };
     fetch(0, Buffer<0>());
