@@ -32,7 +32,7 @@ struct AttendArgs {
     int64_t prefix_part;   // first partial row
     int2 *desc;            // per sequence: its first item and their number
     // what f3s_cache_attend has none of
-    bool own_many;         // the own keys by the kernel of many rows
+    int32_t own_rows;      // query rows of a workgroup of the own keys: 16, 128 or 256
     WindowRule rule;
     int32_t splits;        // a window: pieces of every row block's keys
     const int32_t *parents;  // a tree: [n_seqs, n_new]

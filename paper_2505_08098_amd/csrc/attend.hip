@@ -60,6 +60,17 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Query rows of a sequence and key head from which the own keys of a masked call take the
 // kernel of many rows.
 constexpr int64_t kFewOwnRows = 64;
+// Rows of a workgroup there.
+int own_rows_of(int32_t d, int64_t rows)
+{
+    if (rows <= kFewOwnRows) return f3s::kFewRows;
+    return f3s::own_wide(d) && rows > f3s::kManyRows ? 2 * f3s::kManyRows : f3s::kManyRows;
+}
+// Workgroups that run at once.
+int64_t own_slots(int32_t d, int own_rows)
+{
+    return kUnits * f3s::own_groups(d, own_rows / 32);
+}
 // What one of its workgroups costs beside its keys, in units of 64 keys, and what a byte of
 // partial results does (2.7 us a unit of 128 values; 5 TB/s).
 constexpr int64_t kOwnCost = 4;
@@ -70,7 +81,7 @@ constexpr int64_t kWorthUnits = 16;
 // Everything of the arguments that follows from the sizes; false if a size is
 // beyond what the kernels count with.
 // prefix_rows: 16 or 128 query rows to a workgroup of the prefix, 0: by the rule; own_rows:
-// 16 or 128 to one of the own keys.
+// those of one of the own keys.
 bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_new,
             int32_t n_heads, int32_t prefix_len, int prefix_rows, AttendArgs *a, Layout *w,
             int own_rows = f3s::kFewRows)
@@ -88,7 +99,7 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     a->max_pages = max_pages;
     a->prefix_len = prefix_len;
     a->rows = (int32_t)rows;
-    a->own_many = own_rows == f3s::kManyRows;
+    a->own_rows = own_rows;
     a->row_blocks = (int32_t)ceil_div(rows, own_rows);
     const int64_t cap_units = ceil_div(cap, f3s::kUnit);
     a->direct = prefix_len == 0 && cap_units <= kDirectUnits;
@@ -100,10 +111,9 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     a->share = (int32_t)share;
     a->whole = a->direct || cap_units <= f3s::kLeastUnits || n_seqs > kMostDivided;
     a->own_items = a->whole ? n_seqs : (int32_t)(share + n_seqs);
-    if (a->own_many && !a->whole) {
+    if (own_rows > f3s::kFewRows && !a->whole) {
         // one round of workgroups, or half as many again as sequences
-        const int64_t fit =
-            kUnits * f3s::own_waves(c.d) / ((int64_t)c.n_kv_heads * a->row_blocks);
+        const int64_t fit = own_slots(c.d, own_rows) / ((int64_t)c.n_kv_heads * a->row_blocks);
         a->own_items = (int32_t)std::max<int64_t>(fit, n_seqs + n_seqs / 2);
     }
     if (prefix_rows)
@@ -172,8 +182,8 @@ bool divide_window(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int3
     a->max_pages = max_pages;
     a->rows = (int32_t)rows;
     a->rule = rule;
-    a->own_many = rows > kFewOwnRows;
-    const int64_t tile = a->own_many ? f3s::kManyRows : f3s::kFewRows;
+    a->own_rows = own_rows_of(c.d, rows);
+    const int64_t tile = a->own_rows;
     a->row_blocks = (int32_t)ceil_div(rows, tile);
     const int64_t tokens = std::min<int64_t>(n_new, tile / g + 2);
     const int64_t longest =
@@ -182,13 +192,13 @@ bool divide_window(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int3
     const int64_t units = ceil_div(longest, f3s::kUnit);
     const int64_t one = (int64_t)n_seqs * c.n_kv_heads * a->row_blocks;  // workgroups, unsplit
     int64_t splits = 1;
-    if (a->own_many) {
+    if (a->own_rows > f3s::kFewRows) {
         // whole rounds of workgroups, and what the pieces' results cost
-        const int64_t slots = kUnits * f3s::own_waves(c.d);
+        const int64_t slots = own_slots(c.d, a->own_rows);
         double best = INFINITY;
         for (int64_t n = 1; n == 1 || (n <= units / f3s::kLeastUnits && one * n <= 4 * slots); ++n) {
             const double join = n == 1 ? 0.0
-                                       : 2 + (double)one * n * f3s::kManyRows * (c.d + 2) * 8 /
+                                       : 2 + (double)one * n * tile * (c.d + 2) * 8 /
                                                  kPartRate / (kUnitTime * c.d / 128);
             const double t =
                 (double)ceil_div(one * n, slots) * (double)(ceil_div(units, n) + kOwnCost) + join;
@@ -228,7 +238,7 @@ bool divide_tree(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_
 {
     const int64_t rows = (int64_t)n_new * (n_heads / c.n_kv_heads);
     return divide(c, max_pages, n_seqs, n_new, n_heads, prefix_len, prefix_rows, a, w,
-                  rows > kFewOwnRows ? f3s::kManyRows : f3s::kFewRows);
+                  own_rows_of(c.d, rows));
 }
 
 bool sizes_ok(const f3s_cache_t *c, int32_t max_pages, int32_t n_seqs, int32_t n_new,

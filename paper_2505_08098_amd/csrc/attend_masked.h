@@ -19,7 +19,10 @@
 
 namespace f3s {
 
-constexpr int own_waves(int d) { return d <= 64 ? 3 : d <= 128 ? 2 : 1; }
+// Workgroups of w waves that a compute unit holds: what the registers leave room for.
+constexpr int own_groups(int d, int w) { return w == 8 ? 1 : d <= 64 ? 3 : d <= 128 ? 2 : 1; }
+// Whether there is a kernel of 256 rows (two waves per SIMD as one workgroup).
+constexpr bool own_wide(int d) { return d > 64 && d <= 128; }
 
 // A number that is the same for all lanes, where the compiler might not see it.
 __device__ __forceinline__ int32_t uniform(int32_t x)
@@ -138,25 +141,27 @@ __device__ __forceinline__ OwnItem fitted_item(const AttendArgs &a, int i)
     return own_item_at(a, i, low);
 }
 
-template <int D, int kIn, int kMask>
-__global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(AttendArgs a)
+// W waves, 32 rows each.
+template <int D, int kIn, int kMask, int W>
+__global__ __launch_bounds__(64 * W, W / 4 * own_groups(D, W)) void k_attend_own(AttendArgs a)
 {
     using T = ManyTile<D, code_keys(D)>;
+    constexpr int kThreads = 64 * W, kRows = 32 * W;
     constexpr int kKeys = T::kRows, kBlocks = kKeys / 32;
     constexpr int kCodes = D / 16;  // 16-byte pieces of a row of codes
-    constexpr int kLoads = (kKeys * kCodes + kManyThreads - 1) / kManyThreads;
-    constexpr bool kEven = kKeys * kCodes % kManyThreads == 0;
+    constexpr int kLoads = (kKeys * kCodes + kThreads - 1) / kThreads;
+    constexpr bool kEven = kKeys * kCodes % kThreads == 0;
     constexpr bool kTree = kMask == kTreeMask;
     __shared__ CodeTile<D> s0, s1;
     // the powers of a tile's keys (K | V << 8)
     __shared__ __attribute__((aligned(16))) uint32_t s_powers[2][kKeys];
-    __shared__ uint32_t s_bits[kTree ? kManyRows : 1][kTreeWords];
+    __shared__ uint32_t s_bits[kTree ? kRows : 1][kTreeWords];
     __shared__ int32_t s_parents[kTree ? kTreeTokens : 1];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int rb = (int)blockIdx.x % a.row_blocks, ih = (int)blockIdx.x / a.row_blocks;
     const int head = ih % a.few.n_kv, i = ih / a.few.n_kv;
-    const int first = rb * kManyRows, rows = min(kManyRows, a.rows - first);
+    const int first = rb * kRows, rows = min(kRows, a.rows - first);
     const int shift = a.few.page_shift, g = a.few.q.g;
     int seq, begin, end;
     int32_t base;
@@ -197,7 +202,7 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
     load_rows32<D>(q, a.few.Q, query_row(a.few.q, head, row0 + (there ? mine : 0)), there,
                    a.few.flip, lane);
     if constexpr (kTree)
-        tree_bits<kManyRows>(s_bits, s_parents, a.parents + (int64_t)seq * a.n_new, a.n_new,
+        tree_bits<kRows>(s_bits, s_parents, a.parents + (int64_t)seq * a.n_new, a.n_new,
                              first, g, base);
 
     f16v o[D / 32];
@@ -234,7 +239,7 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
     float times[2];
     int top[2], most = 0;
     auto row_of = [&](int j) {
-        const int f = (int)threadIdx.x + kManyThreads * j;
+        const int f = (int)threadIdx.x + kThreads * j;
         return j == kLoads ? (int)threadIdx.x % kKeys
                            : kEven ? f / kCodes : min(f / kCodes, kKeys - 1);
     };
@@ -259,7 +264,7 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
         };
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int f = (int)threadIdx.x + kManyThreads * j;
+            const int f = (int)threadIdx.x + kThreads * j;
             const int64_t at = place(j) * D + f % kCodes * 16;
             kr[w][j] = *reinterpret_cast<const u4 *>(a.few.k + at);
             vr[w][j] = *reinterpret_cast<const u4 *>(a.few.v + at);
@@ -288,7 +293,7 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
         }
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int f = (int)threadIdx.x + kManyThreads * j, row = f / kCodes;
+            const int f = (int)threadIdx.x + kThreads * j, row = f / kCodes;
             const int its = __builtin_amdgcn_ds_bpermute(4 * row, mine);
             if (!kEven && row >= kKeys) continue;
             const int c = f % kCodes, sw = T::swizzle(row & 31);
@@ -480,7 +485,11 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
     walk(std::false_type());
 
     const float l = __builtin_ldexpf(sum_xor32(l_run), -kRaise<kInF16>);
-    uint8_t *const lds = wave == 0 ? s0.k : wave == 1 ? s0.v : wave == 2 ? s1.k : s1.v;
+    // (two waves to a buffer where there are eight)
+    constexpr int kOwn = T::kBytes * 4 / W;
+    const int part4 = wave & 3;
+    uint8_t *const lds =
+        (part4 == 0 ? s0.k : part4 == 1 ? s0.v : part4 == 2 ? s1.k : s1.v) + wave / 4 * kOwn;
     __syncthreads();  // nobody reads the tiles
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -489,7 +498,7 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
             o[d][k] = __builtin_ldexpf(o[d][k], ref - 127 - kRaise<kInF16>);
     if (!a.direct) {
         const int64_t part = ((int64_t)i * a.few.n_kv + head) * a.rows + first + 32 * wave;
-        store_part32<D, T::kBytes / 128 / 32 * 32>(lds, o, 1.f, a.few.part_o + part * D, D,
+        store_part32<D, kOwn / 128 / 32 * 32>(lds, o, 1.f, a.few.part_o + part * D, D,
                                                    rows - 32 * wave, lane);
         if (there && lane < 32) {
             a.few.part_ml[2 * (part + lane)] = m_run;
@@ -503,12 +512,24 @@ __global__ __launch_bounds__(kManyThreads, own_waves(D)) void k_attend_own(Atten
     if (there && lane < 32) a.few.lse[at(lane)] = natural_lse(m_run + kRaise<kInF16>, l);
 }
 
+template <int D, int kIn, int kMask>
+void launch_attend_own_d(const AttendArgs &a, int64_t grid, hipStream_t s)
+{
+    if constexpr (own_wide(D)) {
+        if (a.own_rows == 2 * kManyRows) {
+            k_attend_own<D, kIn, kMask, 8><<<(unsigned)grid, 512, 0, s>>>(a);
+            return;
+        }
+    }
+    k_attend_own<D, kIn, kMask, 4><<<(unsigned)grid, 256, 0, s>>>(a);
+}
+
 template <int D, int kIn>
 hipError_t launch_attend_window_d(const AttendArgs &a, hipStream_t s)
 {
     const int64_t grid = (int64_t)a.n_seqs * a.splits * a.few.n_kv * a.row_blocks;
-    if (a.own_many)
-        k_attend_own<D, kIn, kWindowMask><<<(unsigned)grid, kManyThreads, 0, s>>>(a);
+    if (a.own_rows > kFewRows)
+        launch_attend_own_d<D, kIn, kWindowMask>(a, grid, s);
     else
         k_attend_window<D, kIn><<<(unsigned)grid, 64 * kFewWaves, 0, s>>>(a);
     launch_attend_join_d<D, kIn>(a, s);
@@ -526,9 +547,9 @@ hipError_t launch_attend_tree_d(const AttendArgs &a, hipStream_t s)
     } else {
         prefix = (int64_t)a.prefix_splits * a.few.n_kv * a.prefix_blocks;
     }
-    if (a.own_many) {
+    if (a.own_rows > kFewRows) {
         if (prefix) k_attend_tree<D, kIn><<<(unsigned)prefix, 64 * kFewWaves, 0, s>>>(a);
-        k_attend_own<D, kIn, kTreeMask><<<(unsigned)own, kManyThreads, 0, s>>>(a);
+        launch_attend_own_d<D, kIn, kTreeMask>(a, own, s);
     } else {
         k_attend_tree<D, kIn><<<(unsigned)(prefix + own), 64 * kFewWaves, 0, s>>>(a);
     }

@@ -12,8 +12,10 @@ FEW = {d: 4 if d <= 64 else 3 if d <= 160 else 2 for d in HEADS}
 ROOM = {
     "k_attend_window": FEW,
     "k_attend_tree": FEW,
-    "k_attend_own1": THREE,      # a window's and a tree's instances
-    "k_attend_own2": THREE,
+    "k_attend_own14": THREE,     # a window's and a tree's instances, four and eight waves
+    "k_attend_own24": THREE,
+    "k_attend_own18": {96: 2, 128: 2},
+    "k_attend_own28": {96: 2, 128: 2},
     "k_window": THREE,
     "k_window_dq": {**THREE, 32: 4},
     "k_window_dkv": THREE,
@@ -24,7 +26,9 @@ ROOM = {
 def test_attention_kernels(kernels, kernel):  # noqa: F811
     seen, wrong = set(), []
     for name, (registers, spilled) in kernels.items():
-        of, mask = (kernel[:-1], "Li%sE" % kernel[-1]) if kernel[-1].isdigit() else (kernel, "")
+        of, mask = kernel, ""
+        if kernel[-1].isdigit():
+            of, mask = kernel[:-2], "Li%sELi%sE" % (kernel[-2], kernel[-1])
         m = re.search(r"\d%sILi(\d+)ELi(\d)E%sE" % (of, mask), name)
         if not m:
             continue
@@ -33,4 +37,4 @@ def test_attention_kernels(kernels, kernel):  # noqa: F811
             wrong.append((d, dtype, registers, spilled))
         seen.add((d, dtype))
     assert not wrong
-    assert len(seen) == 2 * len(HEADS)
+    assert len(seen) == 2 * len(ROOM[kernel])
