@@ -406,6 +406,17 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it,
     uint32_t ke[2] = {0, 0}, ve[2] = {0, 0};
     int pages[2] = {0, 0};  // of the tile in kr, vr; -1: none
 
+    // Page numbers of a tile's halves, looked up a tile ahead of its rows.
+    int ahead[2] = {-1, -1};
+    auto look = [&](int t) {
+        const KeyRun run = run_at(t);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int n = (run.key + 16 * h) >> a.page_shift;
+            ahead[h] = 16 * h < run.left && n < it.table_len ? it.table[n] : -1;
+        }
+    };
+    constexpr int kStep = kFewKeys * kFewWaves;
     auto load = [&](int t) {
         if constexpr (kCache) {
             int64_t base[2];
@@ -413,9 +424,7 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it,
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int pos = run.key + 16 * h;
-                const int n = pos >> a.page_shift;
-                int page = 16 * h < run.left && n < it.table_len ? it.table[n] : -1;
-                page = __builtin_amdgcn_readfirstlane(page);
+                const int page = __builtin_amdgcn_readfirstlane(ahead[h]);
                 pages[h] = page >= 0 && page < a.n_pages ? page : -1;
                 // (a page that is none reads page 0, whose keys are left out)
                 base[h] = ((((int64_t)max(pages[h], 0) * a.n_kv + it.head) << a.page_shift) +
@@ -433,6 +442,7 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it,
                 kr[j] = *reinterpret_cast<const u4 *>(a.k + at);
                 vr[j] = *reinterpret_cast<const u4 *>(a.v + at);
             }
+            if (t + kStep < it.end) look(t + kStep);
         } else {
 #pragma unroll
             for (int j = 0; j < T::kLoads; ++j) {
@@ -447,8 +457,10 @@ __device__ __forceinline__ void few_rows(const FewArgs &a, const FewItem &it,
     };
 
     int t = it.begin + kFewKeys * wave;
-    constexpr int kStep = kFewKeys * kFewWaves;
-    if (t < it.end) load(t);
+    if (t < it.end) {
+        if constexpr (kCache) look(t);
+        load(t);
+    }
     for (; t < it.end; t += kStep) {
         const bool ok0 = !kCache || pages[0] >= 0, ok1 = !kCache || pages[1] >= 0;
         const KeyRun run = run_at(t);
