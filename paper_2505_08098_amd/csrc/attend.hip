@@ -75,6 +75,10 @@ int64_t own_slots(int32_t d, int own_rows)
 // partial results does (2.7 us a unit of 128 values; 5 TB/s).
 constexpr int64_t kOwnCost = 4;
 constexpr double kUnitTime = 2.7e-6, kPartRate = 5e12;
+// Units of a piece of a prefix that fills up what the own keys of a tree leave idle (16
+// trees of 63 tokens, 32 heads of 128 over 8, own keys of 8 to 128 units behind 32: 157 us
+// with pieces of 16, 161 of 11, 168 of 8, 171 whole).
+constexpr int64_t kBesideUnits = 16;
 // Units of a piece of a window, at least, where the workgroups fill the GPU without it.
 constexpr int64_t kWorthUnits = 16;
 
@@ -122,14 +126,19 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
         a->prefix_many = all > kFewPrefixRows &&
                          (double)all * prefix_len * c.n_kv_heads > kManyScores;
     a->prefix_many = a->prefix_many && prefix_len;
-    a->prefix_blocks =
-        (int32_t)ceil_div(all, a->prefix_many ? f3s::kManyRows : f3s::kFewRows);
+    // (a tree's many rows take the prefix in the launch of the own keys)
+    const bool beside = own_rows > f3s::kFewRows && a->prefix_many;
+    a->prefix_blocks = (int32_t)ceil_div(all, beside           ? own_rows
+                                              : a->prefix_many ? f3s::kManyRows
+                                                               : f3s::kFewRows);
     a->prefix_splits = a->prefix_chunk = 0;
     if (prefix_len) {
         const int64_t units = ceil_div(prefix_len, f3s::kUnit);
         const int64_t one = (int64_t)c.n_kv_heads * a->prefix_blocks;  // workgroups, unsplit
         int64_t per;
-        if (a->prefix_many) {
+        if (beside) {
+            per = ceil_div(units, ceil_div(units, kBesideUnits));
+        } else if (a->prefix_many) {
             // pieces that fill their rounds, at most kMostChunk keys each
             const int64_t slots = kUnits * f3s::many_waves(c.d);
             double best = INFINITY;

@@ -159,14 +159,26 @@ __global__ __launch_bounds__(64 * W, W / 4 * own_groups(D, W)) void k_attend_own
     __shared__ int32_t s_parents[kTree ? kTreeTokens : 1];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int rb = (int)blockIdx.x % a.row_blocks, ih = (int)blockIdx.x / a.row_blocks;
+    // a tree's prefix: workgroups behind those of the own keys
+    const int n_own = a.own_items * a.few.n_kv * a.row_blocks;
+    const bool prefix = kTree && (int)blockIdx.x >= n_own;
+    const int wg = (int)blockIdx.x - (prefix ? n_own : 0);
+    const int blocks = prefix ? a.prefix_blocks : a.row_blocks;
+    const int rb = wg % blocks, ih = wg / blocks;
     const int head = ih % a.few.n_kv, i = ih / a.few.n_kv;
-    const int first = rb * kRows, rows = min(kRows, a.rows - first);
+    const int first = rb * kRows, rows = min(kRows, a.rows * (prefix ? a.n_seqs : 1) - first);
     const int shift = a.few.page_shift, g = a.few.q.g;
     int seq, begin, end;
     int32_t base;
     WindowKeys list;
-    if constexpr (kTree) {
+    if (prefix) {
+        // all sequences' rows as one's, and all keys ahead of its tree
+        seq = 0;
+        base = kMostTokens;
+        list = {0, 0, a.prefix_len};
+        begin = i * a.prefix_chunk;
+        end = min(a.prefix_len, begin + a.prefix_chunk);
+    } else if constexpr (kTree) {
         const OwnItem o = fitted_item(a, i);
         if (o.seq < 0) return;
         seq = o.seq;
@@ -189,8 +201,12 @@ __global__ __launch_bounds__(64 * W, W / 4 * own_groups(D, W)) void k_attend_own
         begin = p.begin;
         end = p.end;
     }
-    const int32_t *const table = a.table + (int64_t)seq * a.max_pages;
+    const int32_t *const table = prefix ? a.prefix : a.table + (int64_t)seq * a.max_pages;
     const int64_t row0 = (int64_t)seq * a.rows + first;  // of the key head's rows
+    // first partial row
+    const int64_t part0 =
+        prefix ? a.prefix_part + ((int64_t)i * a.few.n_kv + head) * a.rows * a.n_seqs + first
+               : ((int64_t)i * a.few.n_kv + head) * a.rows + first;
     const int mine = 32 * wave + (lane & 31);
     const bool there = mine < rows;
     const bool busy = 32 * wave < rows;
@@ -201,7 +217,7 @@ __global__ __launch_bounds__(64 * W, W / 4 * own_groups(D, W)) void k_attend_own
     h8 q[D / 16];
     load_rows32<D>(q, a.few.Q, query_row(a.few.q, head, row0 + (there ? mine : 0)), there,
                    a.few.flip, lane);
-    if constexpr (kTree)
+    if (kTree && !prefix)
         tree_bits<kRows>(s_bits, s_parents, a.parents + (int64_t)seq * a.n_new, a.n_new,
                              first, g, base);
 
@@ -497,7 +513,7 @@ __global__ __launch_bounds__(64 * W, W / 4 * own_groups(D, W)) void k_attend_own
         for (int k = 0; k < 16; ++k)
             o[d][k] = __builtin_ldexpf(o[d][k], ref - 127 - kRaise<kInF16>);
     if (!a.direct) {
-        const int64_t part = ((int64_t)i * a.few.n_kv + head) * a.rows + first + 32 * wave;
+        const int64_t part = part0 + 32 * wave;
         store_part32<D, kOwn / 128 / 32 * 32>(lds, o, 1.f, a.few.part_o + part * D, D,
                                                    rows - 32 * wave, lane);
         if (there && lane < 32) {
@@ -540,18 +556,19 @@ template <int D, int kIn>
 hipError_t launch_attend_tree_d(const AttendArgs &a, hipStream_t s)
 {
     const int64_t own = (int64_t)a.own_items * a.few.n_kv * a.row_blocks;
-    int64_t prefix = 0;  // by the kernel of few rows
-    if (a.prefix_many) {
-        const hipError_t e = launch_attend_prefix_d<D, kIn>(a, s);
-        if (e != hipSuccess) return e;
-    } else {
-        prefix = (int64_t)a.prefix_splits * a.few.n_kv * a.prefix_blocks;
-    }
+    const int64_t prefix = (int64_t)a.prefix_splits * a.few.n_kv * a.prefix_blocks;
     if (a.own_rows > kFewRows) {
-        if (prefix) k_attend_tree<D, kIn><<<(unsigned)prefix, 64 * kFewWaves, 0, s>>>(a);
-        launch_attend_own_d<D, kIn, kTreeMask>(a, own, s);
+        // (the prefix by one kernel or the other)
+        if (prefix && !a.prefix_many)
+            k_attend_tree<D, kIn><<<(unsigned)prefix, 64 * kFewWaves, 0, s>>>(a);
+        launch_attend_own_d<D, kIn, kTreeMask>(a, own + (a.prefix_many ? prefix : 0), s);
     } else {
-        k_attend_tree<D, kIn><<<(unsigned)(prefix + own), 64 * kFewWaves, 0, s>>>(a);
+        if (a.prefix_many) {
+            const hipError_t e = launch_attend_prefix_d<D, kIn>(a, s);
+            if (e != hipSuccess) return e;
+        }
+        k_attend_tree<D, kIn>
+            <<<(unsigned)(own + (a.prefix_many ? 0 : prefix)), 64 * kFewWaves, 0, s>>>(a);
     }
     launch_attend_join_d<D, kIn>(a, s);
     return hipGetLastError();
