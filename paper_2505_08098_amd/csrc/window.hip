@@ -6,34 +6,27 @@
 
 #include "dense_host.h"
 #include "window.h"
+#include "window_ranges.h"
 
 namespace {
 
 using f3s::DenseItem;
 using f3s::DenseMerge;
 using f3s::Division;
-using f3s::Range;
 using f3s::set_status;
 using f3s::WindowItem;
-using f3s::WindowKeys;
 using f3s::WindowRule;
 
 // Largest window and number of sinks (a larger one is this one: positions are below
 // 2^31).
 constexpr int32_t kMostWindow = 1 << 30;
 
-// What the items of a range share (its tag).
-struct Shared {
-    int32_t key0, shift;
-    WindowKeys keys;
-};
-
-std::vector<WindowItem> window_items(const Division &d, const std::vector<Shared> &shared)
+std::vector<WindowItem> window_items(const Division &d, const std::vector<f3s::WindowShared> &shared)
 {
     std::vector<WindowItem> out(d.items.size());
     for (size_t i = 0; i < out.size(); ++i) {
         static_cast<DenseItem &>(out[i]) = d.items[i];
-        const Shared &s = shared[d.items[i].tag];
+        const f3s::WindowShared &s = shared[d.items[i].tag];
         out[i].key0 = s.key0;
         out[i].shift = s.shift;
         out[i].keys = s.keys;
@@ -56,7 +49,8 @@ f3s_window_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const in
     }
     if (q_ptr[0] != 0 || k_ptr[0] != 0) return nullptr;
     const WindowRule rule = {std::min(window, kMostWindow), std::min(sinks, kMostWindow)};
-    const int64_t g = n_heads / n_kv, tile = f3s::kManyRows;
+    const int64_t g = n_heads / n_kv, tile = f3s::kWindowTile;
+    static_assert(f3s::kWindowTile == f3s::kManyRows, "");
     double tiles = 0;
     for (int32_t b = 0; b < n; ++b) {
         if (q_ptr[b + 1] < q_ptr[b] || k_ptr[b + 1] < k_ptr[b]) return nullptr;
@@ -71,48 +65,11 @@ f3s_window_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const in
         (double)q_ptr[n] * n_heads / 16 + n_heads > 2147483647.0 ||
         tiles * n_kv > Division::kMostTiles)
         return nullptr;
-    // every tile of rows is a range of its own, since each walks other rows
-    std::vector<Range> queries, keys;
-    std::vector<Shared> shared;
-    for (int32_t b = 0; b < n; ++b) {
-        const int64_t q0 = q_ptr[b], k0 = k_ptr[b], q = q_ptr[b + 1] - q0, k = k_ptr[b + 1] - k0;
-        const int64_t ql = q_len ? q_len[b] : q, kl = k_len ? k_len[b] : k;
-        // position of query token t, as rows are numbered: t + shift
-        const int64_t shift = kl - ql - q0;
-        auto share = [&](WindowKeys w) {
-            shared.push_back({(int32_t)k0, (int32_t)shift, w});
-            return (int32_t)shared.size() - 1;
-        };
-        for (int64_t r = 0; r < ql * g; r += tile) {
-            const int64_t rows = std::min(tile, ql * g - r), at = q0 * g + r;
-            const WindowKeys w =
-                f3s::window_keys(rule, (int32_t)(at / g + shift),
-                                 (int32_t)((at + rows - 1) / g + shift), 1);
-            queries.push_back({at, rows, 0, f3s::window_length(w), share(w)});
-        }
-        // keys: the sinks by themselves (unless the window reaches all of them anyway)
-        const int64_t far = rule.window < kl ? std::min<int64_t>(rule.sinks, kl) : 0;
-        for (int64_t j = 0; j < kl;) {
-            const int64_t rows = std::min(tile, (j < far ? far : kl) - j);
-            // tokens that see the first of them, up to those that see the last
-            const int64_t least = std::max<int64_t>(j + ql - kl, 0);
-            const int64_t most =
-                j < far ? ql
-                        : std::min<int64_t>(ql, std::max<int64_t>(
-                                                    j + rows - 1 + rule.window + ql - kl, 0));
-            const int64_t tokens = std::max<int64_t>(most - least, 0);
-            keys.push_back({k0 + j, rows, tokens ? (q0 + least) * g : 0, tokens * g,
-                            share({0, 0, 0})});
-            j += rows;
-        }
-        // (rows that are padding walk nothing: their results are zeros)
-        if (ql < q) queries.push_back({(q0 + ql) * g, (q - ql) * g, 0, 0, share({0, 0, 0})});
-        if (kl < k) keys.push_back({k0 + kl, k - kl, 0, 0, share({0, 0, 0})});
-    }
+    const f3s::WindowRanges r = f3s::window_ranges(q_ptr, k_ptr, q_len, k_len, n, g, rule);
     Division f, dq, dkv;
-    f.make(queries, n_kv, tile, f3s::kWindowUnit, 256, f3s::kUnits * f3s::many_waves(d));
-    dq.make(queries, n_kv, tile, f3s::kWindowUnit, 256, f3s::kUnits * f3s::dq_waves(d));
-    dkv.make(keys, n_kv, tile, 64, 256, f3s::kUnits * f3s::dkv_waves(d) / f3s::dkv_halves(d),
+    f.make(r.queries, n_kv, tile, f3s::kWindowUnit, 256, f3s::kUnits * f3s::many_waves(d));
+    dq.make(r.queries, n_kv, tile, f3s::kWindowUnit, 256, f3s::kUnits * f3s::dq_waves(d));
+    dkv.make(r.keys, n_kv, tile, 64, 256, f3s::kUnits * f3s::dkv_waves(d) / f3s::dkv_halves(d),
              Division::kLaunch, true);
     if (!f.fits() || !dq.fits() || !dkv.fits()) return nullptr;
 
@@ -126,8 +83,9 @@ f3s_window_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const in
     p->k_rows = k_ptr[n];
     p->rule = rule;
     f3s::set_divisions(p.get(), f, dq, dkv);
-    const std::vector<WindowItem> fi = window_items(f, shared), qi = window_items(dq, shared),
-                                  ki = window_items(dkv, shared);
+    const std::vector<WindowItem> fi = window_items(f, r.shared),
+                                  qi = window_items(dq, r.shared),
+                                  ki = window_items(dkv, r.shared);
     const f3s::PlanList lists[] = {
         {fi.data(), fi.size() * sizeof(WindowItem), (void **)&p->window_fwd},
         {f.merges.data(), f.merges.size() * sizeof(DenseMerge), (void **)&p->fwd_merge},
