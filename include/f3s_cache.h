@@ -148,12 +148,13 @@ size_t f3s_cache_attend_workspace_bytes(const f3s_cache_t *cache, int32_t max_pa
  * window - 1 before it) or j < sinks.  A token that sees no key gives O = 0, lse = -inf.
  *   window, sinks   >= 0; from 2^30 on as 2^30
  *   workspace       at least f3s_cache_attend_window_workspace_bytes(...) bytes
- * Up to 64 query rows of a sequence and key head (n_new times n_heads / n_kv_heads) are
- * worked on 16 at a time, more of them 128 at a time.  In the latter, keys that all 128
- * rows see have their powers of two applied relative to the largest of their tile (K) or
- * among the keys before (V), f16: beside what f3s_cache_attend says a key 2^15 times
- * smaller than that has its score's part off by 2^-25 of the largest.  What a token does
- * not see changes no bit of its result.
+ * Query rows of a sequence and key head (n_new times n_heads / n_kv_heads) are worked on 16
+ * at a time, or 128 or 256 where they are many (environment F3S_OWN_ROWS=16, 128 or, for d
+ * of 96 and 128, 256 forces one; read by every call, that for the workspace's size too).  In
+ * the latter two, keys that all of these rows see have their powers of two applied relative
+ * to the largest of their tile (K) or among the keys before (V), f16: beside what
+ * f3s_cache_attend says a key 2^15 times smaller than that has its score's part off by 2^-25
+ * of the largest.  What a token does not see changes no bit of its result.
  */
 f3s_status_t f3s_cache_attend_window(const f3s_cache_t *cache, const void *Q, f3s_dtype_t dtype,
                                      void *O, float *lse, const int32_t *table,
@@ -176,7 +177,7 @@ size_t f3s_cache_attend_window_workspace_bytes(const f3s_cache_t *cache, int32_t
  *              place, ahead of the sequence's start, see the prefix only)
  *   n_new      at most 256 (else F3S_ERR_UNSUPPORTED)
  *   workspace  at least f3s_cache_attend_tree_workspace_bytes(...) bytes
- * Rows are worked on as in f3s_cache_attend_window.
+ * Rows are worked on as in f3s_cache_attend_window, a prefix as in f3s_cache_attend.
  */
 f3s_status_t f3s_cache_attend_tree(const f3s_cache_t *cache, const void *Q, f3s_dtype_t dtype,
                                    void *O, float *lse, const int32_t *table, int32_t max_pages,

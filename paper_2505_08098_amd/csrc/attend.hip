@@ -57,14 +57,30 @@ struct Layout {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Query rows of a sequence and key head from which the own keys of a masked call take the
-// kernel of many rows.
-constexpr int64_t kFewOwnRows = 64;
-// Rows of a workgroup there.
-int own_rows_of(int32_t d, int64_t rows)
+// Query rows to a workgroup of a masked call's own keys.  The kernel of 16 takes up to 32
+// rows of a sequence and key head, and more where all of them are few workgroups; that of
+// 256 takes 4,096 and more (d = 96, 128).  Us in graphs over windows of 4,000 keys, 8 key
+// heads of 128, with 16, 128 and 256 rows:
+//    1 sequence:   64 rows 15.4, 20.6; 192 rows 23.2, 25.4; 256 rows 25.3, 26.3
+//   16 sequences:  32 rows 40.6, 43.3;  48 rows 55.2, 47.5;  64 rows 64.6, 49.0
+//   64 sequences (of 2,000):  32 rows 69.5, 68.7;  48 rows 95.7, 76.2
+// (trees: 32 rows 73.7, 93.1 and 64 rows 137, 108 of 64 sequences)
+//    1 sequence:   1,024 rows 40.8, 41.9; 4,096 rows 102.5, 97.8; 8,192 rows 174, 162
+//    8 sequences:  1,024 rows 152.5, 156.5; 4,096 rows 581, 570
+constexpr int64_t kFewOwnRows = 32;
+constexpr int64_t kFewOwnBlocks = 112;
+constexpr int64_t kManyOwnRows = 4096;
+int own_rows_of(const f3s_cache_t &c, int32_t n_seqs, int64_t rows)
 {
-    if (rows <= kFewOwnRows) return f3s::kFewRows;
-    return f3s::own_wide(d) && rows > f3s::kManyRows ? 2 * f3s::kManyRows : f3s::kManyRows;
+    const char *wanted = getenv("F3S_OWN_ROWS");
+    const int n = wanted && *wanted ? atoi(wanted) : 0;
+    if (n == f3s::kFewRows || n == f3s::kManyRows ||
+        (n == 2 * f3s::kManyRows && f3s::own_wide(c.d)))
+        return n;
+    if (rows <= kFewOwnRows ||
+        (double)n_seqs * c.n_kv_heads * (double)ceil_div(rows, f3s::kFewRows) <= kFewOwnBlocks)
+        return f3s::kFewRows;
+    return f3s::own_wide(c.d) && rows >= kManyOwnRows ? 2 * f3s::kManyRows : f3s::kManyRows;
 }
 // Workgroups that run at once.
 int64_t own_slots(int32_t d, int own_rows)
@@ -191,7 +207,7 @@ bool divide_window(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int3
     a->max_pages = max_pages;
     a->rows = (int32_t)rows;
     a->rule = rule;
-    a->own_rows = own_rows_of(c.d, rows);
+    a->own_rows = own_rows_of(c, n_seqs, rows);
     const int64_t tile = a->own_rows;
     a->row_blocks = (int32_t)ceil_div(rows, tile);
     const int64_t tokens = std::min<int64_t>(n_new, tile / g + 2);
@@ -247,7 +263,7 @@ bool divide_tree(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_
 {
     const int64_t rows = (int64_t)n_new * (n_heads / c.n_kv_heads);
     return divide(c, max_pages, n_seqs, n_new, n_heads, prefix_len, prefix_rows, a, w,
-                  own_rows_of(c.d, rows));
+                  own_rows_of(c, n_seqs, rows));
 }
 
 bool sizes_ok(const f3s_cache_t *c, int32_t max_pages, int32_t n_seqs, int32_t n_new,

@@ -1,6 +1,5 @@
 """Attention over the 8-bit cache with a window or a tree of drafted tokens, on the GPU
-against plain 64-bit attention: by the kernel of 16 query rows and by that of 128 (from 65
-rows of a sequence and key head on)."""
+against plain 64-bit attention: by the kernels of 16, 128 and 256 query rows."""
 import math
 
 import pytest
@@ -139,11 +138,16 @@ WINDOWS = [
 ]
 
 
+ROWS = ["16", "128", "256"]  # (256: d = 96 and 128 only, else by the rule)
+
+
+@pytest.mark.parametrize("rows", ROWS)
 @pytest.mark.parametrize("room", [0, 3000])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("d,page,kv,g,lens,n,window,sinks", WINDOWS)
-def test_window(gpu, dtype, d, page, kv, g, lens, n, window, sinks, room):
+def test_window(gpu, monkeypatch, rows, dtype, d, page, kv, g, lens, n, window, sinks, room):
     """Tables of the sequences' size, and with room for more (pieces)."""
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     _window_case(gpu, dtype, d, page, kv, g, lens, n, window, sinks, room=room)
 
 
@@ -152,7 +156,9 @@ def test_window(gpu, dtype, d, page, kv, g, lens, n, window, sinks, room):
     (64, 16, 2, 4, [4000, 70, 1], 2, 3000, 4), (128, 64, 1, 8, [3500, 2222], 30, 1500, 100),
     (128, 16, 1, 1, [2500], 1, 2100, 0), (256, 32, 1, 4, [2600], 25, 2000, 1),
 ])
-def test_long_windows(gpu, dtype, d, page, kv, g, lens, n, window, sinks):
+@pytest.mark.parametrize("rows", ROWS)
+def test_long_windows(gpu, monkeypatch, rows, dtype, d, page, kv, g, lens, n, window, sinks):
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     _window_case(gpu, dtype, d, page, kv, g, lens, n, window, sinks, room=5000)
 
 
@@ -204,30 +210,39 @@ TREES = [
 ]
 
 
+@pytest.mark.parametrize("rows", ROWS)
 @pytest.mark.parametrize("shape", ["random", "wrong"])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("d,page,kv,g,lens,n,P", TREES)
-def test_tree(gpu, dtype, d, page, kv, g, lens, n, P, shape):
+def test_tree(gpu, monkeypatch, rows, dtype, d, page, kv, g, lens, n, P, shape):
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     _tree_case(gpu, dtype, d, page, kv, g, lens, n, P, shape)
     _tree_case(gpu, dtype, d, page, kv, g, lens, n, P, shape, room=2000, seed=1)
 
 
 @pytest.mark.parametrize("shape", ["chain", "star", "none"])
 @pytest.mark.parametrize("g,n", [(1, 40), (4, 40), (2, 256)])
-def test_tree_shapes(gpu, shape, g, n):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_tree_shapes(gpu, monkeypatch, rows, shape, g, n):
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     _tree_case(gpu, torch.float16, 64, 16, 1, g, [300, 45, n], n, 0, shape)
 
 
+@pytest.mark.parametrize("own", ROWS)
 @pytest.mark.parametrize("rows", ["16", "128"])
 @pytest.mark.parametrize("g,n", [(2, 4), (4, 30)])
-def test_tree_behind_a_prefix(gpu, monkeypatch, rows, g, n):
-    """The prefix by the kernel of 16 query rows and by that of 128."""
+def test_tree_behind_a_prefix(gpu, monkeypatch, rows, own, g, n):
+    """The prefix by the kernel of 16 query rows and by that of 128, beside the own keys where
+    these go by many rows."""
     monkeypatch.setenv("F3S_PREFIX_ROWS", rows)
+    monkeypatch.setenv("F3S_OWN_ROWS", own)
     _tree_case(gpu, torch.bfloat16, 128, 32, 2, g, [(7 * b) % 50 for b in range(20)], n, 321,
                "random")
 
 
-def test_a_chain_is_cache_attend(gpu):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_a_chain_is_cache_attend(gpu, monkeypatch, rows):
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     for n, g in ((5, 2), (40, 4)):
         cache, Q, table, lens, _, _ = _setup(gpu, torch.float16, 64, 16, 2, g, [200, 77], n)
         chain = (torch.arange(n, dtype=torch.int32, device=DEV) - 1).expand(2, n).contiguous()
@@ -243,8 +258,10 @@ def test_a_chain_is_cache_attend(gpu):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("spread", [6, 60])
-def test_values_of_different_sizes(gpu, dtype, spread):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_values_of_different_sizes(gpu, monkeypatch, rows, dtype, spread):
     """Values that differ by 2^120 (bf16): what a row sees counts, not what others do."""
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     spread = min(spread, 6) if dtype == torch.float16 else spread
     for n, g in ((3, 2), (40, 3)):
         _window_case(gpu, dtype, 64, 16, 1, g, [300, 90], n, 50, 3, spread=spread)
@@ -253,15 +270,19 @@ def test_values_of_different_sizes(gpu, dtype, spread):
 
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1e-30, 5.0])
 @pytest.mark.parametrize("n,g", [(3, 2), (40, 3)])
-def test_scales(gpu, scale, n, g):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_scales(gpu, monkeypatch, rows, scale, n, g):
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     _window_case(gpu, torch.float16, 64, 16, 1, g, [200], n, 50, 3, scale=scale)
     _tree_case(gpu, torch.float16, 64, 16, 1, g, [200], n, 33, "random", scale=scale)
 
 
 @pytest.mark.parametrize("n,g", [(6, 2), (40, 3)])
 @pytest.mark.parametrize("large", [2.0 ** 60, 3.0])
-def test_what_a_token_does_not_see_changes_no_bit(gpu, n, g, large):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_what_a_token_does_not_see_changes_no_bit(gpu, monkeypatch, rows, n, g, large):
     """Other tokens' keys, values and queries, much larger or alike."""
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     dtype = torch.bfloat16
     lens, window, sinks = [300], 60, 2
     cache, Q, table, lens_d, _, gen = _setup(gpu, dtype, 64, 16, 1, g, lens, n)
@@ -292,8 +313,10 @@ def test_what_a_token_does_not_see_changes_no_bit(gpu, n, g, large):
 
 
 @pytest.mark.parametrize("n,g", [(5, 2), (40, 3)])
-def test_bad_pages_and_lengths(gpu, n, g):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_bad_pages_and_lengths(gpu, monkeypatch, rows, n, g):
     """Pages that are none, lengths below zero and beyond the table."""
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     lens = [100, 61, -5, 200, 64]
     cache, Q, table, _, _, gen = _setup(gpu, torch.float16, 64, 16, 1, g, [100, 61, 1, 112, 64],
                                         n)
@@ -311,7 +334,9 @@ def test_bad_pages_and_lengths(gpu, n, g):
 
 
 @pytest.mark.parametrize("n,g", [(2, 2), (40, 2)])
-def test_captured_with_changing_lengths(gpu, n, g):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_captured_with_changing_lengths(gpu, monkeypatch, rows, n, g):
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     # (every row below a length has to be there: all of 500 are written first)
     cache, Q, table, lens, _, gen = _setup(gpu, torch.float16, 64, 16, 2, g, [500, 500, 500], n,
                                            room=1500)
@@ -340,8 +365,10 @@ def test_captured_with_changing_lengths(gpu, n, g):
             assert torch.equal(a, b)
 
 
-def test_calls_side_by_side(gpu):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_calls_side_by_side(gpu, monkeypatch, rows):
     """On streams of their own, each with its own workspace."""
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     cases = [_setup(gpu, torch.float16, 64, 16, 2, 4, [1500, 900], n, seed=n) for n in (1, 30)]
     parents = [(torch.arange(n, dtype=torch.int32, device=DEV) // 2 - 1).expand(2, n).contiguous()
                for n in (1, 30)]
@@ -388,9 +415,11 @@ def test_nothing_to_do_and_refusals(gpu):
         gpu.cache_attend_window(cache, q[:1], t, lens, 5)
 
 
-def test_two_steps_of_a_draft(gpu):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_two_steps_of_a_draft(gpu, monkeypatch, rows):
     """The operators as a step of generation uses them: pages for a tree, its rows, its
     attention, the accepted branch kept; then the next token over a window."""
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     B, n, page, kv, g, d, M = 3, 7, 16, 1, 2, 64, 8
     gen = torch.Generator().manual_seed(9)
     pool = gpu.PagePool.full(B * M, page, device=DEV)

@@ -53,8 +53,10 @@ def test_window_of_keys_beyond_4_gib(gpu):
     assert bool(((got - want).abs() <= 4 * u * spread).all())
 
 
-def test_cache_rows_beyond_4_gib(gpu):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_cache_rows_beyond_4_gib(gpu, monkeypatch, rows):
     """Pages whose codes lie beyond 4 GiB: written, attended to, moved."""
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     kv, page, d = 8, 64, 128
     n_pages = 80_000                    # 5.2 GB of codes
     cache = gpu.Cache.empty(n_pages, page, kv, d, device=DEV)
@@ -103,8 +105,10 @@ def test_a_pool_with_slots_beyond_32_bits(gpu):
 
 
 @pytest.mark.parametrize("d,kv,g", [(64, 2, 2), (128, 1, 4), (96, 1, 1)])
-def test_given_results_and_what_lies_beside_them(gpu, d, kv, g):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_given_results_and_what_lies_beside_them(gpu, monkeypatch, rows, d, kv, g):
     """Results into rows of larger buffers: what stands before and behind stays."""
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     n, H = 150, kv * g
     gen = torch.Generator(device=DEV).manual_seed(3)
     Q = torch.randn((n, H, d), generator=gen, device=DEV).half()
@@ -172,8 +176,10 @@ def test_large_scores(gpu):
 
 
 @pytest.mark.parametrize("what", ["window", "tree"])
-def test_thousands_of_sequences(gpu, what):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_thousands_of_sequences(gpu, monkeypatch, rows, what):
     """More than the kernels divide one by one."""
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     B, kv, d, page = 9000, 1, 32, 16
     gen = torch.Generator(device=DEV).manual_seed(5)
     cache = gpu.Cache.empty(B * 7, page, kv, d, device=DEV)
@@ -211,8 +217,10 @@ def test_many_rows_of_thousands_of_sequences(gpu):
     assert torch.allclose(lse, ref, atol=1e-5)
 
 
-def test_two_graphs_of_one_cache(gpu):
+@pytest.mark.parametrize("rows", ["16", "128"])
+def test_two_graphs_of_one_cache(gpu, monkeypatch, rows):
     """Captured apart, replayed in any order: neither shares memory with the other."""
+    monkeypatch.setenv("F3S_OWN_ROWS", rows)
     B, n, kv, d = 3, 20, 1, 64
     gen = torch.Generator(device=DEV).manual_seed(7)
     cache = gpu.Cache.empty(300, 16, kv, d, device=DEV)
