@@ -71,8 +71,9 @@ __device__ __forceinline__ f16v zero16()
 // four neighbouring pieces of a transposed one (cols32), and so do those that store every
 // other piece of neighbouring rows (attend_many.h).  A swizzle that moved
 // neighbouring rows apart by two pieces made the latter meet each bank twice (two
-// sequences of 8,100 tokens, window 1,024, 16 heads of 128 over 4: 792 us a training step instead of 713;
-// 2 x 4,050 tokens over 8,100 keys, 32 heads over 8: 1,080 us instead of 1,060).
+// sequences of 8,100 tokens, window 1,024, 16 heads of 128 over 4: 792 us a training step
+// instead of 713; 2 x 4,050 tokens over 8,100 keys, 32 heads over 8: 1,080 us instead of
+// 1,060).
 // Other d: through registers, into padded rows.
 template <int D, int R = many_keys(D)>
 struct ManyTile {
