@@ -221,7 +221,8 @@ bool divide_window(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int3
         // whole rounds of workgroups, and what the pieces' results cost
         const int64_t slots = own_slots(c.d, a->own_rows);
         double best = INFINITY;
-        for (int64_t n = 1; n == 1 || (n <= units / f3s::kLeastUnits && one * n <= 4 * slots); ++n) {
+        for (int64_t n = 1;
+             n == 1 || (n <= units / f3s::kLeastUnits && one * n <= 4 * slots); ++n) {
             const double join = n == 1 ? 0.0
                                        : 2 + (double)one * n * tile * (c.d + 2) * 8 /
                                                  kPartRate / (kUnitTime * c.d / 128);
@@ -241,8 +242,8 @@ bool divide_window(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int3
         //   64 sequences, 64 units: 104 whole, 117 (2), 107 (3), 113 (4)
         //   16 sequences, 256 units: 222 whole, 105 (4), 103 (6), 110 (16)
         const int64_t aim = kUnits * f3s::few_waves(c.d, true);
-        splits = std::min(aim / one, units / (one < kUnits ? (int64_t)f3s::kLeastUnits : kWorthUnits));
-        splits = std::max<int64_t>(splits, 1);
+        const int64_t least = one < kUnits ? (int64_t)f3s::kLeastUnits : kWorthUnits;
+        splits = std::max<int64_t>(std::min(aim / one, units / least), 1);
     }
     a->splits = (int32_t)splits;
     a->direct = splits == 1;

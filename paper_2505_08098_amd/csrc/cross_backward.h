@@ -14,8 +14,9 @@
 // the operand of the second in place, each wave has 32 rows of its own side in
 // registers, and tiles of 32 rows of the other side (d = 32: 64) pass through LDS
 // for all four waves in two buffers.  As in the forward power is the bound, and in
-// k_cross_dkv LDS reads (one operand of every product, and V): 2 x 4,050 x 4,050, 16 heads of 128 over 4,
-// bf16, takes 413 us for dQ and 558 for dK and dV, 970 TFLOP/s of the 7 products.
+// k_cross_dkv LDS reads (one operand of every product, and V): 2 x 4,050 x 4,050, 16
+// heads of 128 over 4, bf16, takes 413 us for dQ and 558 for dK and dV, 970 TFLOP/s of the
+// 7 products.
 //
 // P and dS enter the second products in the inputs' type, as P does in the forward,
 // and for its reasons; delta comes from the rounded O, since the exact one would take

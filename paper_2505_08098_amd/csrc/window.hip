@@ -51,19 +51,22 @@ f3s_window_plan_t make_plan(const int32_t *q_ptr, const int32_t *k_ptr, const in
     const WindowRule rule = {std::min(window, kMostWindow), std::min(sinks, kMostWindow)};
     const int64_t g = n_heads / n_kv, tile = f3s::kWindowTile;
     static_assert(f3s::kWindowTile == f3s::kManyRows, "");
-    double tiles = 0;
+    double q_tiles = 0, k_tiles = 0;
     for (int32_t b = 0; b < n; ++b) {
         if (q_ptr[b + 1] < q_ptr[b] || k_ptr[b + 1] < k_ptr[b]) return nullptr;
         const int64_t q = q_ptr[b + 1] - (int64_t)q_ptr[b], k = k_ptr[b + 1] - (int64_t)k_ptr[b];
         const int64_t ql = q_len ? q_len[b] : q, kl = k_len ? k_len[b] : k;
         if (ql < 0 || ql > q || kl < 0 || kl > k) return nullptr;
-        tiles += (double)(f3s::ceil_div(q * g, tile) + f3s::ceil_div(k, tile) + 4);
+        q_tiles += (double)(f3s::ceil_div(ql * g, tile) + f3s::ceil_div((q - ql) * g, tile));
+        // (the sinks' tiles are their own)
+        k_tiles += (double)(f3s::ceil_div(kl, tile) + f3s::ceil_div(k - kl, tile)) +
+                   (sinks && window < kl ? 1 : 0);
     }
     *st = F3S_ERR_TOO_LARGE;
     // (a row's number and a tile add up to less than 2^31)
     if (q_ptr[n] * g > 0x7FFFF000 || k_ptr[n] > 0x7FFFF000 ||
         (double)q_ptr[n] * n_heads / 16 + n_heads > 2147483647.0 ||
-        tiles * n_kv > Division::kMostTiles)
+        std::max(q_tiles, k_tiles) * n_kv > Division::kMostTiles)
         return nullptr;
     const f3s::WindowRanges r = f3s::window_ranges(q_ptr, k_ptr, q_len, k_len, n, g, rule);
     Division f, dq, dkv;

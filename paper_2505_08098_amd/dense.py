@@ -624,10 +624,14 @@ class PagePool:
         _check_device_tensor(count, "count", torch.int32, free.device)
         if free.dim() != 1 or count.numel() != 1 or not 1 <= free.numel() <= _MOST:
             raise ValueError("free must be [pages], count one number")
-        self.free, self.count = free, count
+        self._tensors = (free, count)
         self.device = free.device
         self.page_size = _size(page_size, "page_size")
         self._bytes = {}  # workspace of a call, by its sizes
+
+    # (read-only: what they were checked for)
+    free = property(lambda self: self._tensors[0])
+    count = property(lambda self: self._tensors[1])
 
     @classmethod
     def full(cls, n_pages, page_size, device="cuda"):
@@ -650,7 +654,7 @@ def pages_assign(pool, table, lens, new_lens, n=0):
     n = _size(n, "n")
     if n < 0:
         raise ValueError("n must not be negative")
-    free, device = pool.free, pool.device
+    (free, count), device = pool._tensors, pool.device
     sizes = (B, pages, n)
     nbytes = pool._bytes.get(sizes)
     if nbytes is None:
@@ -661,7 +665,7 @@ def pages_assign(pool, table, lens, new_lens, n=0):
     slots = torch.empty((B, n), dtype=torch.int64, device=device)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
     rc = _lib().f3s_pages_assign(
-        free.data_ptr(), pool.count.data_ptr(), free.numel(), table.data_ptr(), pages,
+        free.data_ptr(), count.data_ptr(), free.numel(), table.data_ptr(), pages,
         lens.data_ptr(), new_lens.data_ptr(), got.data_ptr(), slots.data_ptr() if n else None,
         B, n, pool.page_size, ws.data_ptr() if nbytes else None, nbytes,
         _raw_stream(device.index))
