@@ -87,8 +87,8 @@ f3s_status_t f3s_cache_read(const f3s_cache_t *cache, void *K, void *V, f3s_dtyp
  * nothing is moved onto one.  The places behind the new length hold what they held or
  * what was moved away.  Every page of the n_new tokens belongs to one sequence.  The
  * cache's four parts must not share memory with each other or with the other arguments,
- * nor new_lens with any of them.  Asynchronous on `stream`; no allocation, no
- * synchronisation; deterministic.
+ * nor new_lens with any of them.  F3S_ERR_TOO_LARGE beyond 2^30 picks of a sequence.
+ * Asynchronous on `stream`; no allocation, no synchronisation; deterministic.
  */
 f3s_status_t f3s_cache_keep(const f3s_cache_t *cache, const int32_t *table, int32_t max_pages,
                             const int32_t *lens, int32_t n_seqs, int32_t n_new,

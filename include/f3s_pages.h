@@ -47,10 +47,11 @@ extern "C" {
  *   workspace            device, at least f3s_pages_assign_workspace_bytes(n_seqs,
  *                        max_pages, n_new) bytes, 16-byte aligned; needs no
  *                        initialisation; NULL if that is 0
- * What is written must not overlap anything else of the call.  F3S_ERR_TOO_LARGE from
- * 2^24 sequences on.  Whole numbers in a fixed order: deterministic.  Asynchronous on
- * `stream`; no allocation, no synchronisation: it can be captured, and a replay takes
- * its lengths from the device.  Calls on one pool or table follow one another.
+ * What is written must not overlap anything else of the call.  F3S_ERR_TOO_LARGE beyond
+ * 2^24 sequences or 2^30 new tokens.  Whole numbers in a fixed order: deterministic.
+ * Asynchronous on `stream`; no allocation, no synchronisation: it can be captured, and a
+ * replay takes its lengths from the device.  Calls on one pool or table follow one
+ * another.
  */
 f3s_status_t f3s_pages_assign(int32_t *free_pages, int32_t *n_free, int32_t n_pages,
                               int32_t *table, int32_t max_pages, const int32_t *lens,

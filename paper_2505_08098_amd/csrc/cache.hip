@@ -149,6 +149,7 @@ struct KeepArgs {
 // order, kAhead at a time, all loaded before the first is stored: no thread reads what
 // another writes.  The places of a round of picks are looked up once, a thread each.
 constexpr int kKeepAhead = 8;
+constexpr int32_t kMostPicks = 1 << 30;  // (their indexes stay below 2^31)
 
 __global__ __launch_bounds__(kThreads) void k_cache_keep(KeepArgs a)
 {
@@ -395,6 +396,7 @@ f3s_status_t f3s_cache_keep(const f3s_cache_t *cache, const int32_t *table, int3
         !f3s::aligned(lens, 4) || !f3s::aligned(new_lens, 4) || !f3s::aligned(table, 4) ||
         !f3s::aligned(picks, 4) || f3s::folded(*cache, false))
         return f3s::set_status(F3S_ERR_INVALID_VALUE);
+    if (n_picks > f3s::kMostPicks) return f3s::set_status(F3S_ERR_TOO_LARGE);
     const int64_t threads = (int64_t)cache->n_kv_heads * (cache->d / 8);
     const int64_t blocks = (threads + f3s::kThreads - 1) / f3s::kThreads;
     if ((double)blocks * n_seqs > (double)f3s::kMostGrid || threads > 0x7FFFFFFF - f3s::kThreads)

@@ -31,6 +31,7 @@ constexpr int64_t kAloneSeqs = kThreads;
 constexpr int64_t kAloneEntries = 1 << 17;
 constexpr int64_t kAloneSlots = 1 << 15;
 constexpr int32_t kMostSeqs = 1 << 24;
+constexpr int32_t kMostNew = 1 << 30;  // (a thread's index of a token stays below 2^31)
 
 struct PageArgs {
     int32_t *free_pages, *n_free;
@@ -400,7 +401,7 @@ extern "C" {
 size_t f3s_pages_assign_workspace_bytes(int32_t n_seqs, int32_t max_pages, int32_t n_new)
 {
     if (n_seqs < 1 || max_pages < 0 || n_new < 0 || n_seqs > f3s::kMostSeqs ||
-        f3s::alone(n_seqs, max_pages, n_new))
+        n_new > f3s::kMostNew || f3s::alone(n_seqs, max_pages, n_new))
         return 0;
     return 16 + f3s::list_bytes(n_seqs) + 16 * ((size_t)f3s::blocks_of(n_seqs) + 1);
 }
@@ -418,7 +419,8 @@ f3s_status_t f3s_pages_assign(int32_t *free_pages, int32_t *n_free, int32_t n_pa
     if (n_pages < 1 || max_pages < 0 || n_seqs < 0 || n_new < 0)
         return set_status(F3S_ERR_INVALID_VALUE);
     if (n_seqs == 0) return F3S_OK;
-    if (n_seqs > f3s::kMostSeqs || (int64_t)max_pages * page_size > 1 << 30)
+    if (n_seqs > f3s::kMostSeqs || n_new > f3s::kMostNew ||
+        (int64_t)max_pages * page_size > 1 << 30)
         return set_status(F3S_ERR_TOO_LARGE);
     if (!free_pages || !n_free || !lens || !new_lens || !got_lens || (max_pages && !table) ||
         (n_new && !slots) || !aligned(free_pages, 4) || !aligned(n_free, 4) ||

@@ -32,6 +32,7 @@ def test_keep_caches(change, status):
     (dict(new=A), INVALID), (dict(lens=2 * A + 64), INVALID), (dict(table=3 * A), INVALID),
     (dict(picks=4 * A - 4), INVALID),
     (dict(B=0), OK), (dict(B=0, lens=None, new=None), OK),
+    (dict(m=(1 << 30) + 1), TOO_LARGE), (dict(m=2**31 - 1), TOO_LARGE),
     (dict(m=0, picks=None), HIP), (dict(n=0), HIP), (dict(pages=0, table=None), HIP),
     (dict(new=7 * A + 48), HIP), (dict(), HIP),
 ])
@@ -65,6 +66,7 @@ def _assign(free=A, count=2 * A, n_pages=100, table=3 * A, pages=8, lens=4 * A, 
     (dict(count=A), INVALID), (dict(slots=3 * A + 88), INVALID), (dict(slots=5 * A), INVALID),
     (dict(lens=A), INVALID),
     (dict(pages=1 << 26, page=32), TOO_LARGE), (dict(B=(1 << 24) + 1), TOO_LARGE),
+    (dict(n=(1 << 30) + 1), TOO_LARGE), (dict(n=2**31 - 1, B=1), TOO_LARGE),
     (dict(B=0), OK), (dict(B=0, lens=None), OK),
     (dict(new=4 * A), HIP),                                  # the same lengths
     (dict(n=0, slots=None), HIP), (dict(ws=None, nbytes=0), HIP), (dict(), HIP),
@@ -84,5 +86,6 @@ def test_assign_workspace():
         assert size(*more) > 4 * more[0]
         assert _assign(B=more[0], pages=more[1], n=more[2], nbytes=size(*more)) == HIP
         assert _assign(B=more[0], pages=more[1], n=more[2], nbytes=size(*more) - 1) == INVALID
-    for bad in ((0, 5, 5), (-1, 5, 5), (5, -1, 5), (5, 5, -1), (2**31 - 1, 5, 5)):
+    for bad in ((0, 5, 5), (-1, 5, 5), (5, -1, 5), (5, 5, -1), (2**31 - 1, 5, 5),
+                (1, 5, (1 << 30) + 1)):
         assert size(*bad) == 0
