@@ -164,6 +164,22 @@ struct WindowItem : DenseItem {
 };
 static_assert(sizeof(WindowItem) == 64, "WindowItem must be 64 bytes");
 
+// ---- a tree of drafted tokens -------------------------------------------------------
+
+// Tokens of a tree, and the words that hold a bit for each: one of ones ahead of them
+// (positions before the tree), one behind, so that 32 bits from any place are two words.
+constexpr int kTreeTokens = 256;
+constexpr int kTreeWords = kTreeTokens / 32 + 2;
+
+// Where 32 bits from position `pos` on begin, of a tree whose first token stands at `base`:
+// bit at % 32 of word at / 32 + 1.  A tile of keys may begin or end behind the last token;
+// such places count as the last one, so that both words are the row's.
+__host__ __device__ inline int32_t tree_place(int32_t pos, int32_t base)
+{
+    const int32_t at = pos - base;
+    return at < -32 ? -32 : at > kTreeTokens - 1 ? kTreeTokens - 1 : at;
+}
+
 // ---- the cache's rules ---------------------------------------------------------
 
 // Biased exponent (the scale is 2^(byte - 127)) of a row whose largest finite

@@ -67,11 +67,6 @@ struct FewItem {
 // Which keys of its range a row sees beside the plain limit.
 constexpr int kNoMask = 0, kWindowMask = 1, kTreeMask = 2;
 
-// Tokens of a tree, and the words that hold a bit for each: one of ones ahead of them
-// (positions before the tree), one behind, so that 32 bits from any place are two words.
-constexpr int kTreeTokens = 256;
-constexpr int kTreeWords = kTreeTokens / 32 + 2;
-
 // The words of rows first .. first + kRows - 1 of a tree (row r: token r / g), by the
 // whole workgroup, ahead of a barrier.  A token's parent is one of those before it, any
 // other number none; so a walk up ends after as many steps as the token has tokens before
@@ -104,10 +99,11 @@ __device__ __forceinline__ void tree_bits(uint32_t (*bits)[kTreeWords], int32_t 
     }
     if (there) row[w + 1] = word;
 }
-// 32 of a row's bits from position `pos` on (pos - base < 256).
+// 32 of a row's bits from position `pos` on (what is said of positions behind the tree's
+// last token counts for nothing: there are no keys).
 __device__ __forceinline__ uint32_t tree_seen(const uint32_t *row, int32_t pos, int32_t base)
 {
-    const int at = max(pos - base, -32);
+    const int at = tree_place(pos, base);
     const uint32_t *w = row + (at >> 5) + 1;
     return __builtin_amdgcn_alignbit(w[1], w[0], at & 31);
 }
