@@ -366,7 +366,7 @@ class Cache:
                                     self.page_size, self.d)
         self._ref = ctypes.byref(self._struct)
         self.scale = 1.0 / math.sqrt(self.d) if self.d else 1.0
-        self._bytes = {}  # workspace of an attend call, by its sizes
+        self._bytes = {}  # workspace of a cache_attend call, by its sizes
 
     # (read-only: the struct holds their addresses)
     k = property(lambda self: self._tensors[0])
@@ -501,14 +501,10 @@ def _results(cache, Q, dtype, out, lse):
 
 def _attend_workspace(cache, name, sizes):
     """A call's workspace and its bytes (None and 0 where it needs none)."""
-    nbytes = cache._bytes.get((name, sizes))
-    if nbytes is None:
-        if max(sizes) > _MOST:
-            raise ValueError("more than 2^31 - 1 tokens or heads")
-        if len(cache._bytes) >= 64:  # (a prefix that grows)
-            cache._bytes.clear()
-        nbytes = getattr(_lib(), name + "_workspace_bytes")(cache._ref, *sizes)
-        cache._bytes[name, sizes] = nbytes
+    if max(sizes) > _MOST:
+        raise ValueError("more than 2^31 - 1 tokens or heads")
+    # (asked for at every call, 1 us: it follows F3S_OWN_ROWS too, which the call reads)
+    nbytes = getattr(_lib(), name + "_workspace_bytes")(cache._ref, *sizes)
     return (torch.empty(nbytes, dtype=torch.uint8, device=cache.device) if nbytes else None,
             nbytes)
 

@@ -1,0 +1,66 @@
+"""The workspace that the binding takes for attention over the cache with a window or a tree
+is the one that the library asks for at that call, whatever calls went before."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2505_08098_amd import dense
+from test_dense_refusals import _cache
+
+
+class _Binding:
+    """What the workspace's size and place follow from in a dense.Cache (no GPU needed)."""
+
+    def __init__(self, **sizes):
+        self._struct = _cache(**sizes)
+        self._ref = ctypes.byref(self._struct)
+        self._bytes = {}
+        self.device = torch.device("cpu")
+
+
+@pytest.mark.parametrize("name,sizes", [
+    ("f3s_cache_attend_window", (200, 4, 8, 32, 4000, 4)),
+    ("f3s_cache_attend_tree", (200, 4, 8, 32, 0)),
+])
+def test_rows_forced_between_calls(monkeypatch, name, sizes):
+    cache = _Binding(n_kv_heads=8, d=128, page_size=64)
+    need = getattr(dense._lib(), name + "_workspace_bytes")
+    seen = set()
+    for rows in (None, "128", "16", "256", None):
+        monkeypatch.delenv("F3S_OWN_ROWS", raising=False)
+        if rows:
+            monkeypatch.setenv("F3S_OWN_ROWS", rows)
+        want = need(cache._ref, *sizes)
+        ws, nbytes = dense._attend_workspace(cache, name, sizes)
+        assert nbytes == want and ws.numel() == want, rows
+        seen.add(want)
+    assert len(seen) > 1
+
+
+@pytest.mark.gpu
+def test_rows_forced_between_calls_of_one_cache(gpu, monkeypatch):
+    cache = gpu.Cache.empty(40, 64, 8, 128, device="cuda:0")
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda:0")
+    table = torch.arange(40, dtype=torch.int32, device="cuda:0").view(4, 10)
+    table = torch.cat([table] + [torch.full_like(table, -1)] * 19, 1)   # room for 200 pages
+    lens = ints([600, 30, 0, 511])
+    states = [torch.randn((4, 600, 8, 128), device="cuda:0").half() for _ in "KV"]
+    gpu.cache_write(cache, *states, table, lens)
+    Q = torch.randn((4, 8, 32, 128), device="cuda:0").half()
+    parents = ints([[-1, 0, 0, 1, 1, 2, 5, 5]] * 4)
+    K, V = gpu.cache_read(cache, table, lens, 600, torch.float32)
+    # Of each of two kernels: a result's rounding, and its probabilities', which weigh V; of
+    # lse, what 128 sums of a score in 32 bits lose (a sum of probabilities loses less).
+    u, steps = 2.0 ** -11, 128 * 2.0 ** -24
+    score = float(Q.float().norm(dim=3).max() * K.norm(dim=3).max()) * 128 ** -0.5
+    calls = [lambda: gpu.cache_attend_window(cache, Q, table, lens, 4000, 4),
+             lambda: gpu.cache_attend_tree(cache, Q, table, lens, parents)]
+    for call in calls:
+        monkeypatch.delenv("F3S_OWN_ROWS", raising=False)
+        O, lse = call()
+        for rows in ("128", "16", "256"):
+            monkeypatch.setenv("F3S_OWN_ROWS", rows)
+            O2, lse2 = call()
+            assert torch.allclose(O.float(), O2.float(), rtol=2 * u, atol=2 * u * V.abs().max())
+            assert torch.allclose(lse, lse2, rtol=0, atol=2 * steps * score)
