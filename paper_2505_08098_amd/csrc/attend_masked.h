@@ -250,7 +250,9 @@ __global__ __launch_bounds__(64 * W, W / 4 * own_groups(D, W)) void k_attend_own
 
     constexpr int kSets = code_sets(D);
     u4 kr[kSets][kLoads], vr[kSets][kLoads];
-    bool ok[kSets];  // whether the key that this lane looks after is there
+    // whether the key that this lane looks after is there (none of a tile that was never
+    // fetched: behind a walk's last tile the next one is widened all the same, for nobody)
+    bool ok[kSets] = {};
     uint32_t ke[kSets], ve[kSets];
     // pages of the rows that the next fetch brings, and of the key looked after
     int page[kLoads + 1];
