@@ -44,6 +44,17 @@ constexpr int64_t kDirectUnits = 14;
 // 3,480 and 270, with one of 131,072 among them 3,477 and 1,016 (1 key head: 597 and
 // 45, 616 and 918); 32,768 sequences 50,000 and 1,080.
 constexpr int64_t kMostDivided = 8192;
+// The same for a tree's own keys by many rows, whose workgroups go through all lengths once
+// more for every step of a search (fitted_item).  Trees of 16 tokens, in us divided and
+// whole: own keys of 100 to 4,000; of 100 to 1,000, and one sequence of 65,536 among them:
+//   8 key heads of 128, 4 heads each:  256 sequences 452, 437;  301, 1,711
+//                                    1,024 sequences 2,163, 1,478;  1,548, 2,159
+//                                    2,048 sequences 5,089, 2,910;  4,424, 2,841
+//   1 key head of 64, 8 heads:         256 sequences 61, 91;  71, 1,240
+//                                    1,024 sequences 218, 174;  163, 1,272
+//                                    4,096 sequences 1,410, 532;  1,365, 1,432
+// (8,192 of 50 to 300, 8 key heads of 64, one of 65,536 among them: 39,460 and 2,953)
+constexpr int64_t kMostFitted = 1024;
 // What a piece of the prefix costs beside its keys (queries, partial results),
 // in units of 64 keys.
 constexpr int64_t kPieceCost = 3;
@@ -129,7 +140,8 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
     if (share > most) share = most;
     if (share < 1) share = 1;
     a->share = (int32_t)share;
-    a->whole = a->direct || cap_units <= f3s::kLeastUnits || n_seqs > kMostDivided;
+    a->whole = a->direct || cap_units <= f3s::kLeastUnits ||
+               n_seqs > (own_rows > f3s::kFewRows ? kMostFitted : kMostDivided);
     a->own_items = a->whole ? n_seqs : (int32_t)(share + n_seqs);
     if (own_rows > f3s::kFewRows && !a->whole) {
         // one round of workgroups, or half as many again as sequences

@@ -150,3 +150,34 @@ def test_captured_and_on_other_streams(gpu, monkeypatch, d):
         for x in (out, got[0] + got[1], got[2] + got[3]):
             for a, b in zip(x, want):
                 assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("B", [1024, 1025])
+def test_as_many_sequences_as_are_divided_and_one_more(gpu, monkeypatch, B):
+    """A chain of tokens is plain causal attention, also where one sequence is much longer."""
+    monkeypatch.delenv("F3S_OWN_ROWS", raising=False)
+    kv, d, page, n, room = 1, 32, 16, 33, 5000
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    pages = -(-room // page)
+    cache = gpu.Cache.empty(pages, page, kv, d, device=DEV)
+    table = torch.randint(0, pages, (B, pages), generator=gen, device=DEV, dtype=torch.int32)
+    lens = torch.randint(0, 300, (B,), generator=gen, device=DEV, dtype=torch.int32)
+    lens[B // 2] = room
+    states = [torch.randn((1, pages * page, kv, d), generator=gen, device=DEV).half()
+              for _ in "KV"]
+    gpu.cache_write(cache, *states, torch.arange(pages, dtype=torch.int32, device=DEV).view(1, -1),
+                    _ints([pages * page]))
+    Q = torch.randn((B, n, 2, d), generator=gen, device=DEV).half()
+    chain = (torch.arange(n, dtype=torch.int32, device=DEV) - 1).expand(B, n).contiguous()
+    O, lse = gpu.cache_attend_tree(cache, Q, table, lens, chain)
+    want, ref = gpu.cache_attend(cache, Q, table, lens)
+    # Of each of two kernels: a result's rounding, and its probabilities', which weigh V; of
+    # lse, what 32 sums of a score in 32 bits lose (a sum of probabilities loses less).
+    u = 2.0 ** -11
+    K, V = gpu.cache_read(cache, table[B // 2: B // 2 + 1], lens[B // 2: B // 2 + 1], room,
+                          torch.float32)
+    top = max(float(x.abs().max()) for x in (V, states[1]))
+    score = float(Q.float().norm(dim=3).max()) * max(
+        float(x.float().norm(dim=3).max()) for x in (K, states[0])) * 2 / d ** 0.5
+    assert torch.allclose(O.float(), want.float(), rtol=2 * u, atol=2 * u * top)
+    assert torch.allclose(lse, ref, rtol=0, atol=2 * d * 2.0 ** -24 * score)

@@ -38,6 +38,19 @@ def test_rows_forced_between_calls(monkeypatch, name, sizes):
     assert len(seen) > 1
 
 
+@pytest.mark.parametrize("B,items", [(1024, 1024 + 512), (1025, 1025), (8192, 8192)])
+def test_trees_of_many_sequences_are_not_divided(monkeypatch, B, items):
+    """Every workgroup searches all lengths for its item: with 8,192 sequences that took 13
+    times as long as their keys.  An item has d values and two numbers a row."""
+    monkeypatch.delenv("F3S_OWN_ROWS", raising=False)
+    c = _cache(n_kv_heads=8, d=64, page_size=64)
+    n, heads = 16, 32
+    size = dense._lib().f3s_cache_attend_tree_workspace_bytes(ctypes.byref(c), 100, B, n, heads, 0)
+    up = lambda x: -(-x // 256) * 256
+    rows = items * n * heads
+    assert size == up(rows * 64 * 4) + up(rows * 8) + up(B * 8)
+
+
 @pytest.mark.gpu
 def test_rows_forced_between_calls_of_one_cache(gpu, monkeypatch):
     cache = gpu.Cache.empty(40, 64, 8, 128, device="cuda:0")
