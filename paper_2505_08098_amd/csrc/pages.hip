@@ -8,8 +8,8 @@
 // takes, not bytes.  Small batches do all of it in one workgroup and one launch, a thread
 // to a sequence where it needs a single page and a thread to a token's place; larger ones
 // in three launches (the pool's new end has to stand before any of it is taken), of which
-// every workgroup sums the counts of all before it by itself, and from 16,384 sequences
-// on in four.  256 sequences that take 5 tokens each, 5.9 us; 4,096 of up to 8,000 tokens of
+// every workgroup sums the counts of all before it by itself, and beyond 16,384 sequences
+// in four.  256 sequences that take 5 tokens each, 5.2 us; 4,096 of up to 8,000 tokens of
 // which a quarter end and a quarter begin, pages of 16, with 256 places each, 19 us.
 #include "dense_common.h"
 #include "f3s_pages.h"
@@ -22,14 +22,24 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;  // sequences of a workgroup, in launches over them
 // Sequences, entries of the table and places up to which one workgroup does it all.  A call
 // in which few sequences change their pages takes half of what the launches do, one in
-// which half of a batch ends or begins several times as long; the former is what a step of
-// generation does.  Us of a call, alone and in launches: 256 sequences of up to 8,000 tokens,
-// one more each, 5.2 and 11.6; half of them turned over, pages of 64, 25 and 13; 1,000 of up
-// to 2,000, pages of 16, 7.0 and 11.9, half turned over 31 and 13.5; 64 of up to 32,000, half
-// turned over, 256 places each, 134 and 22.
+// which many do several times as long, since a wave goes through those of its 64 sequences
+// one behind the other; the former is what a step of generation does.  Us of a call in
+// graphs, alone and in launches (one more token each; n more each; half of the batch ends
+// or begins; lengths of up to 2,000, pages of 16, n places each):
+//      8 sequences, n = 8:    4.7, 10.0;    6.9, 11.1;    7.7, 11.9
+//                   n = 256:  5.4, 10.6;    9.5, 11.6;    9.0, 12.4
+//     64 sequences, n = 8:    5.7, 11.8;   17.4, 12.2;   29.4, 13.2
+//                   n = 64:   7.1, 11.9;   42.9, 12.4;   42.1, 13.4
+//                   n = 256: 12.1, 12.7;   47.4, 13.1;   45.6, 14.3
+//    256 sequences, n = 1:    8.4, 12.2;    9.4, 13.0;   28.0, 13.7
+//                   n = 64:  14.9, 12.2;   50.3, 13.4;   53.1, 13.7
+//  1,000 sequences, n = 8:   11.6, 12.4;   28.3, 13.6;   46.3, 13.9
+// (64 of up to 32,000 tokens, half turned over: 80.6, 21.3).  Beyond kAloneNew places a
+// sequence, which a prompt's part has and a step has not, it loses unless there are few.
 constexpr int64_t kAloneSeqs = kThreads;
 constexpr int64_t kAloneEntries = 1 << 17;
-constexpr int64_t kAloneSlots = 1 << 15;
+constexpr int64_t kAloneNew = 32;
+constexpr int64_t kAloneSlots = 2048;
 constexpr int32_t kMostSeqs = 1 << 24;
 constexpr int32_t kMostNew = 1 << 30;  // (a thread's index of a token stays below 2^31)
 
@@ -377,7 +387,7 @@ __global__ __launch_bounds__(kThreads) void k_pages_take(PageArgs a)
 bool alone(int32_t n_seqs, int32_t max_pages, int32_t n_new)
 {
     return n_seqs <= kAloneSeqs && (int64_t)n_seqs * max_pages <= kAloneEntries &&
-           (int64_t)n_seqs * n_new <= kAloneSlots;
+           (n_new <= kAloneNew || (int64_t)n_seqs * n_new <= kAloneSlots);
 }
 
 bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
