@@ -517,23 +517,8 @@ def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, o
     pages ``prefix`` (int32, shared by all sequences) and to their own cached
     keys up to themselves; ``stream=`` as cache_write.  Returns (O, lse): O
     like Q, lse fp32 [sequences, n, heads]."""
-    B, pages = _sequences(cache, table, lens)
-    dtype = _dtype_of(Q, "Q")
-    if Q.dim() != 4 or Q.shape[2] < 1 or Q.shape[2] % cache.kv_heads:
-        raise ValueError("Q must be [sequences, n, heads, d], heads a multiple of kv_heads")
-    _, n, heads, _ = shape = Q.shape
-    device = cache.device
-    _check(Q, "Q", dtype, device, (B, n, heads, cache.d))
-    if prefix is None:
-        if prefix_len != 0:
-            raise ValueError("prefix and a positive prefix_len come together")
-    else:
-        prefix_len = _size(prefix_len, "prefix_len")
-        _check_device_tensor(prefix, "prefix", torch.int32, device)
-        if prefix_len < 1:
-            raise ValueError("prefix and a positive prefix_len come together")
-        if prefix.dim() != 1 or prefix.numel() * cache.page_size < prefix_len:
-            raise ValueError("prefix must name enough pages for prefix_len tokens")
+    dtype, B, n, heads, pages = _queries(cache, Q, table, lens)
+    prefix_len = _prefix(cache, prefix, prefix_len)
     sizes = (pages, B, n, heads, prefix_len)
     nbytes = cache._bytes.get(sizes)
     if nbytes is None:
@@ -543,15 +528,8 @@ def cache_attend(cache, Q, table, lens, prefix=None, prefix_len=0, scale=None, o
             cache._bytes.clear()
         nbytes = _lib().f3s_cache_attend_workspace_bytes(cache._ref, *sizes)
         cache._bytes[sizes] = nbytes
-    if out is None:
-        out = _empty_like(Q, dtype)
-    else:
-        _check(out, "out", dtype, device, shape)
-    if lse is None:
-        lse = torch.empty((B, n, heads), dtype=torch.float32, device=device)
-    else:
-        _check(lse, "lse", torch.float32, device, (B, n, heads))
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    out, lse = _results(cache, Q, dtype, out, lse)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device) if nbytes else None
     rc = _lib().f3s_cache_attend(
         cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
         table.data_ptr(), pages, lens.data_ptr(), B, n, heads,
