@@ -102,10 +102,19 @@ int64_t own_slots(int32_t d, int own_rows)
 // partial results does (2.7 us a unit of 128 values; 5 TB/s).
 constexpr int64_t kOwnCost = 4;
 constexpr double kUnitTime = 2.7e-6, kPartRate = 5e12;
-// Units of a piece of a prefix that fills up what the own keys of a tree leave idle (16
-// trees of 63 tokens, 32 heads of 128 over 8, own keys of 8 to 128 units behind 32: 157 us
-// with pieces of 16, 161 of 11, 168 of 8, 171 whole).
+// A prefix in the launch of a tree's own keys fills up what these leave idle: in pieces of
+// this many units, but no more of them than make two rounds of workgroups (a long prefix
+// has work enough, and every piece of a row is joined).  Us a call in graphs, trees of 63
+// tokens, 32 heads of 128 over 8, in pieces of 16 units; by two rounds; in a launch apart:
+//   16 trees, own keys of 500 to 8,192 behind 2,001:   155, 153, 173;  behind 16,000: 470, 414, 411
+//   4 behind 4,001: 77, 76, 82;  32 of 500 to 4,000 behind 4,001: 309, 288, 297
+//   16 of 100 to 500 behind 8,001: 208, 193, 186;  64 of 100 to 3,000 behind 6,001: 718, 622, 632
+//   64 of 32 tokens, d = 64, behind 8,001: 255, 239, 242;  2 of 200 behind 60,000: 818, 725, 733
+// (8 units and two rounds: 162 for the first, 71 instead of 78 for 8 trees, 16 heads of 96
+// over 2, behind 4,001; of three rounds, none but 16 trees of 256 tokens and 16 heads over 1
+// gains: 520 for 551)
 constexpr int64_t kBesideUnits = 16;
+constexpr int64_t kBesideRounds = 2;
 // Units of a piece of a window, at least, where the workgroups fill the GPU without it.
 constexpr int64_t kWorthUnits = 16;
 
@@ -165,7 +174,9 @@ bool divide(const f3s_cache_t &c, int32_t max_pages, int32_t n_seqs, int32_t n_n
         const int64_t one = (int64_t)c.n_kv_heads * a->prefix_blocks;  // workgroups, unsplit
         int64_t per;
         if (beside) {
-            per = ceil_div(units, ceil_div(units, kBesideUnits));
+            const int64_t fill = kBesideRounds * own_slots(c.d, own_rows) / one;
+            per = ceil_div(units, std::min(ceil_div(units, kBesideUnits),
+                                           std::max<int64_t>(fill, 1)));
         } else if (a->prefix_many) {
             // pieces that fill their rounds, at most kMostChunk keys each
             const int64_t slots = kUnits * f3s::many_waves(c.d);

@@ -77,3 +77,39 @@ def test_rows_forced_between_calls_of_one_cache(gpu, monkeypatch):
             O2, lse2 = call()
             assert torch.allclose(O.float(), O2.float(), rtol=2 * u, atol=2 * u * V.abs().max())
             assert torch.allclose(lse, lse2, rtol=0, atol=2 * steps * score)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(),
+                    reason="made-up addresses: only where nothing can launch")
+@pytest.mark.parametrize("B,n,kv,g,d,P,pieces", [
+    (16, 63, 8, 4, 128, 2001, 2),      # of 16 units
+    (16, 63, 8, 4, 128, 16000, 4),     # 1,024 workgroups: two rounds
+    (16, 63, 8, 4, 128, 1 << 20, 4),
+    (4, 63, 8, 4, 128, 4001, 4), (32, 63, 8, 4, 128, 4001, 2),
+    (64, 256, 8, 4, 128, 6001, 1),     # one piece fills more
+    (4, 63, 2, 8, 256, 30000, 16), (64, 32, 8, 4, 64, 8001, 3),
+])
+def test_pieces_of_a_prefix_beside_the_own_keys(monkeypatch, B, n, kv, g, d, P, pieces):
+    """A piece of a prefix has d values and two numbers for every row: what the least workspace
+    of a call with a prefix has more than that of one without."""
+    monkeypatch.setenv("F3S_PREFIX_ROWS", "128")
+    monkeypatch.setenv("F3S_OWN_ROWS", "128")
+    A = 1 << 44                        # (an address that is never read)
+    c = _cache(n_kv_heads=kv, d=d, page_size=64)
+    heads = kv * g
+
+    def least(prefix_len):
+        def refused(nbytes):
+            return dense._lib().f3s_cache_attend_tree(
+                ctypes.byref(c), A, 0, 2 * A, 3 * A, 4 * A, 2000, 5 * A, B, n, heads, 6 * A,
+                7 * A if prefix_len else None, prefix_len, 0.1, 8 * A, nbytes, None) == 1
+        lo, hi = 0, 1 << 40
+        assert not refused(hi) and refused(256)
+        while hi - lo > 1:
+            mid = (lo + hi) // 2
+            lo, hi = (mid, hi) if refused(mid) else (lo, mid)
+        return hi
+
+    rows = B * n * heads
+    more = least(P) - least(0)
+    assert abs(more - pieces * rows * (d + 2) * 4) <= 3 * 256
