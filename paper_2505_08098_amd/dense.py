@@ -366,7 +366,7 @@ class Cache:
                                     self.page_size, self.d)
         self._ref = ctypes.byref(self._struct)
         self.scale = 1.0 / math.sqrt(self.d) if self.d else 1.0
-        self._bytes = {}  # workspace of a cache_attend call, by its sizes
+        self._bytes = {}  # workspace of an attend call, by its sizes
 
     # (read-only: the struct holds their addresses)
     k = property(lambda self: self._tensors[0])
@@ -500,13 +500,34 @@ def _results(cache, Q, dtype, out, lse):
 
 
 def _attend_workspace(cache, name, sizes):
-    """A call's workspace and its bytes (None and 0 where it needs none)."""
+    """The workspace that a call needs now, and its bytes (None and 0 where it needs none)."""
     if max(sizes) > _MOST:
         raise ValueError("more than 2^31 - 1 tokens or heads")
-    # (asked for at every call, 1 us: it follows F3S_OWN_ROWS too, which the call reads)
     nbytes = getattr(_lib(), name + "_workspace_bytes")(cache._ref, *sizes)
     return (torch.empty(nbytes, dtype=torch.uint8, device=cache.device) if nbytes else None,
             nbytes)
+
+
+def _attend(cache, name, sizes, *args):
+    """The library's function ``name`` on ``args``, a workspace and the current stream.  How
+    large it has to be is asked once for all calls of the same sizes (1 us), and again where
+    the library refuses a call with that: it follows F3S_OWN_ROWS too, which the library
+    reads at every call."""
+    call, stream = getattr(_lib(), name), _raw_stream(cache.device.index)
+    known = cache._bytes.get((name, sizes))
+    rc = 1  # (invalid value)
+    if known is not None:
+        ws = torch.empty(known, dtype=torch.uint8, device=cache.device) if known else None
+        rc = call(*args, ws.data_ptr() if known else None, known, stream)
+    if rc == 1:
+        ws, nbytes = _attend_workspace(cache, name, sizes)
+        if nbytes != known:
+            if len(cache._bytes) >= 64:  # (a prefix that grows)
+                cache._bytes.clear()
+            cache._bytes[name, sizes] = nbytes
+            rc = call(*args, ws.data_ptr() if nbytes else None, nbytes, stream)
+    if rc:
+        _fail(rc, name)
 
 
 @_on_its_device
@@ -549,16 +570,11 @@ def cache_attend_window(cache, Q, table, lens, window, sinks=0, scale=None, out=
     window, sinks = _size(window, "window"), _size(sinks, "sinks")
     if window < 0 or sinks < 0:
         raise ValueError("window and sinks must not be negative")
-    ws, nbytes = _attend_workspace(cache, "f3s_cache_attend_window",
-                                   (pages, B, n, heads, window, sinks))
     out, lse = _results(cache, Q, dtype, out, lse)
-    rc = _lib().f3s_cache_attend_window(
-        cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
-        table.data_ptr(), pages, lens.data_ptr(), B, n, heads, window, sinks,
-        cache.scale if scale is None else float(scale), ws.data_ptr() if nbytes else None,
-        nbytes, _raw_stream(cache.device.index))
-    if rc:
-        _fail(rc, "f3s_cache_attend_window")
+    _attend(cache, "f3s_cache_attend_window", (pages, B, n, heads, window, sinks),
+            cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
+            table.data_ptr(), pages, lens.data_ptr(), B, n, heads, window, sinks,
+            cache.scale if scale is None else float(scale))
     return out, lse
 
 
@@ -572,17 +588,12 @@ def cache_attend_tree(cache, Q, table, lens, parents, prefix=None, prefix_len=0,
     dtype, B, n, heads, pages = _queries(cache, Q, table, lens)
     _check(parents, "parents", torch.int32, cache.device, (B, n))
     prefix_len = _prefix(cache, prefix, prefix_len)
-    ws, nbytes = _attend_workspace(cache, "f3s_cache_attend_tree",
-                                   (pages, B, n, heads, prefix_len))
     out, lse = _results(cache, Q, dtype, out, lse)
-    rc = _lib().f3s_cache_attend_tree(
-        cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
-        table.data_ptr(), pages, lens.data_ptr(), B, n, heads, parents.data_ptr(),
-        None if prefix is None else prefix.data_ptr(), prefix_len,
-        cache.scale if scale is None else float(scale), ws.data_ptr() if nbytes else None,
-        nbytes, _raw_stream(cache.device.index))
-    if rc:
-        _fail(rc, "f3s_cache_attend_tree")
+    _attend(cache, "f3s_cache_attend_tree", (pages, B, n, heads, prefix_len),
+            cache._ref, Q.data_ptr(), _DTYPE_CODE[dtype], out.data_ptr(), lse.data_ptr(),
+            table.data_ptr(), pages, lens.data_ptr(), B, n, heads, parents.data_ptr(),
+            None if prefix is None else prefix.data_ptr(), prefix_len,
+            cache.scale if scale is None else float(scale))
     return out, lse
 
 

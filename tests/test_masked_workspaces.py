@@ -113,3 +113,48 @@ def test_pieces_of_a_prefix_beside_the_own_keys(monkeypatch, B, n, kv, g, d, P, 
     rows = B * n * heads
     more = least(P) - least(0)
     assert abs(more - pieces * rows * (d + 2) * 4) <= 3 * 256
+
+
+def test_a_size_is_asked_again_where_it_does_not_do(monkeypatch):
+    """A call that the library refuses with the size known so far is made once more with the
+    size that it asks for now; one that it refuses for another reason is not."""
+    cache, calls = _Binding(n_kv_heads=8, d=128, page_size=64), []
+    sizes = (200, 4, 8, 32, 4000, 4)
+
+    class Library:
+        need = 512
+
+        def f3s_cache_attend_window_workspace_bytes(self, *args):
+            calls.append("size")
+            return self.need
+
+        def f3s_cache_attend_window(self, wrong, ws, nbytes, stream):
+            calls.append(nbytes)
+            return 1 if wrong or nbytes < self.need else 0
+
+    lib = Library()
+    monkeypatch.setattr(dense, "_lib", lambda: lib)
+    monkeypatch.setattr(dense, "_raw_stream", lambda index: 0)
+    attend = lambda wrong: dense._attend(cache, "f3s_cache_attend_window", sizes, wrong)
+    attend(False)
+    attend(False)
+    assert calls == ["size", 512, 512]
+    lib.need, calls[:] = 1024, []
+    attend(False)
+    attend(False)
+    assert calls == [512, "size", 1024, 1024]
+    lib.need, calls[:] = 256, []
+    attend(False)                       # (a larger one does)
+    assert calls == [1024]
+    calls[:] = []
+    with pytest.raises(dense.F3SError):
+        attend(True)
+    lib.need = 1024
+    calls[:] = []
+    with pytest.raises(dense.F3SError):
+        attend(True)
+    assert calls == [256, "size", 1024]
+    calls[:] = []
+    with pytest.raises(dense.F3SError):
+        attend(True)
+    assert calls == [1024, "size"]
