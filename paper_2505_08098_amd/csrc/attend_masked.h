@@ -14,10 +14,13 @@
 // on (and since both kinds in one loop would spill).  A row's result is its own, bit by
 // bit, whatever the others see.
 //
-// The vector unit bounds it, as there: 2 x 2,000 tokens over a window of 4,000, 16 heads of
-// 128 over 4, 163 us (780 TFLOP/s); 16 trees of 63 tokens over 500 to 8,192 own keys and 2,001
-// shared ones, 32 heads over 8, 146 us and 13 for the join.  By 16 rows bytes bound it: one
-// token of 64 sequences over a window of 4,096, 8 key heads of 128, 90 us, 5.5 TB/s.
+// 2 x 2,000 tokens over a window of 4,000, 16 heads of 128 over 4: 159 to 166 us by card (770
+// to 800 TFLOP/s); the matrix units are busy 31% of the cycles and the vector unit issues in
+// 42%, by turns, since the eight waves of a compute unit meet at a barrier every tile.  16
+// trees of 63 tokens over 500 to 8,192 own keys and 2,001 shared ones, 32 heads over 8: 160 to
+// 166 us, of which the join takes 14 (30% and 47%; the longest pieces have 44 units where 34
+// would be even).  By 16 rows bytes bound it: one token of 64 sequences over a window of
+// 4,096, 8 key heads of 128, 90 us, 5.5 TB/s.
 #pragma once
 
 #include "attend_many.h"

@@ -14,11 +14,11 @@
 // running maximum needs one exchange a tile, between the two halves of a wave;
 // sums stay in the lane until the end.
 //
-// 2 x 4,050 tokens, 32 heads of 128 over 8, 8,100 keys, bf16: 1,076 us, 1,000
-// TFLOP/s, where a library's product of 8,192^3 reaches 1,200.  The clock falls to
-// 1.9 GHz, the matrix units are busy 48% of its cycles and the vector unit as long again;
-// more waves or earlier reads gained nothing, LDS reads without bank conflicts 2%.  Power
-// seems to be the bound.
+// 2 x 4,050 tokens, 32 heads of 128 over 8, 8,100 keys, bf16: 1,060 us, 1,010
+// TFLOP/s, where a library's product of 8,192^3 reaches 1,200 to 1,320 by card.  The
+// clock falls to 1.9 GHz, the matrix units are busy 48% of its cycles and the vector unit as
+// long again; more waves or earlier reads gained nothing, LDS reads without bank conflicts
+// 2%.  Power seems to be the bound.
 //
 // P enters the value product in the inputs' type: rounded to nearest, a bf16 result
 // is off by 0.0023 of its size instead of the 0.0017 of its own rounding (fp16 0.0003

@@ -10,10 +10,16 @@
 // query rows from its first key on to the end of its last key's window; the sinks, which
 // all later rows see, are tiles of their own.
 //
-// 32,749 tokens, 32 heads of 128 over 8, bf16, window 4,096: 2,000 us, 1,030 TFLOP/s (the
-// bound is many_rows.h's).  Training on two sequences of 8,100, 16 heads of 128 over 4,
-// window 1,024, 16 sinks: 155 us forward, 530 backward.  16 of 300 to 1,025 tokens padded, 12
-// heads of 64, causal: 114 to 124 us in all.
+// 32,749 tokens, 32 heads of 128 over 8, bf16, window 4,096: 2,010 to 2,120 us by card, 970
+// to 1,030 TFLOP/s (the bound is many_rows.h's).  Training on two sequences of 8,100, 16 heads
+// of 128 over 4, window 1,024, 16 sinks: 690 to 714 us, under the profiler 162 forward, 222 dQ,
+// 331 dK and dV, 7.5 sums.  16 of 300 to 1,025 tokens padded, 12 heads of 64, causal: 117 to
+// 124 us in all (31, 43 and 54).
+//
+// A few newest query rows leave three waves of four without any, which costs little, since
+// bytes count: one token over 8,192 keys of 64 sequences, 32 heads of 128 over 8, 352 us in
+// graphs (6.1 TB/s), 366 by the kernel of 16 rows (few_rows.h, as cross attention); of one
+// sequence, where its launch and chain count, 12.0 and 8.7.
 #pragma once
 
 #include "cross_backward.h"
